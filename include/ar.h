@@ -54,7 +54,9 @@ typedef enum {
   AR_ERR_INTERNAL = 7       /* the plan failed its own consistency check  */
 } ar_status;
 
-typedef enum { AR_INT32 = 0, AR_FLOAT32 = 1 } ar_dtype;
+/* Rank buffers hold int32 or float32; the layer operators at the end of this
+ * header take float32, float16 and bfloat16. */
+typedef enum { AR_INT32 = 0, AR_FLOAT32 = 1, AR_FLOAT16 = 2, AR_BFLOAT16 = 3 } ar_dtype;
 
 /* Combination function of Sec. 5.4.  AR_SUM on int32 wraps modulo 2^32.
  * AR_MAX keeps the received value only when it is strictly greater than the
@@ -431,6 +433,109 @@ const char* ar_status_string(ar_status s);
  * the library.  ar_last_error is the same function under a shorter name. */
 const char* ar_last_error_message(void);
 const char* ar_last_error(void);
+
+/* ---- Layer operators ------------------------------------------------------
+ *
+ * What a layer of a model runs around an Allreduce: the product that makes the
+ * vectors that are summed (gradients, or partial products of ranks that share
+ * an inner length) and what is applied to the sum.  They follow the
+ * conventions at the top; they keep nothing between calls and allocate
+ * nothing (scratch is the caller's workspace), so they may be captured into a
+ * HIP graph and may run on several streams at once.
+ *
+ * Matrices lie in rows: element (i, j) of a matrix is at data + i * ld + j (in
+ * elements, ld at least the columns), in 32-bit, 16-bit (IEEE) or bfloat
+ * floats.  Any address and ld that are multiples of the element are taken;
+ * operands on 16-byte boundaries, with an ld of whole 16 bytes, take
+ * asynchronous loads.  Rows, columns and inner lengths go from 0 to 2^30 (a
+ * matrix without elements may have NULL data; an inner length of 0 is a sum
+ * of nothing).  Products are summed in 32 bits, everything up to the store is
+ * computed in 32 bits, and a result is rounded once (to nearest, ties to
+ * even) to its matrix' type.  Results do not depend on timing: no sum's order
+ * does.  NaN and infinities go through as the formulas say. */
+typedef struct {
+  void* data;
+  int64_t ld;     /* elements from one row to the next; of a vector, unused */
+  ar_dtype dtype; /* AR_FLOAT32, AR_FLOAT16 or AR_BFLOAT16 */
+} ar_matrix;
+
+typedef enum {
+  AR_ACT_NONE = 0,
+  AR_ACT_RELU = 1,      /* max(z, 0); slope 0 at 0                             */
+  AR_ACT_GELU = 2,      /* z (1 + erf(z / sqrt 2)) / 2                         */
+  AR_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2     */
+  AR_ACT_SILU = 4       /* z / (1 + exp(-z))                                   */
+} ar_activation;
+
+/* Dropout whose mask is never stored: element (i, j) is kept, times
+ * 1 / (1 - p), where a word of a counter-based generator is below
+ * round((1 - p) * 2^32), and is 0 (whatever it held) elsewhere.  The generator
+ * is the seven-round one on four 32-bit words of Salmon et al. (2011); element
+ * (i, j) takes word j mod 4 at the counter (j / 4, row mod 2^32, row / 2^32,
+ * site), row = row0 + i, with the low and high half of seed as key.  So the
+ * mask is a function of the element's place: a gradient repeats it, a rank
+ * that holds rows from row0 on of a larger matrix draws that matrix' mask, and
+ * ranks that pass the same arguments drop the same elements.  Give every
+ * dropout of a model a site, and every step a seed. */
+typedef struct {
+  double p;      /* in [0, 1]; 0 keeps everything, 1 nothing */
+  uint64_t seed;
+  uint32_t site;
+  uint64_t row0;
+} ar_dropout;
+
+/* y = residual + drop(act(x w^T + bias)):  x [M, K], w [N, K] of one type,
+ * bias [N] of that type or float32 (NULL: none), residual [M, N] of y's type
+ * (NULL: none), y [M, N] of x's type or float32.  preact [M, N], of x's type,
+ * receives z = x w^T + bias for the gradient (NULL: not kept).  drop NULL: no
+ * dropout.  residual may be y itself (the same data and ld); otherwise what is
+ * written may not overlap anything else (AR_ERR_ALIAS).
+ *
+ * workspace: device memory of at least as many bytes as
+ * ar_linear_forward_workspace says for the same arguments (often 0, where it
+ * may be NULL), on a 16-byte boundary; it is free again when the call's work
+ * is done.  Errors: AR_ERR_INVALID_ARG (sizes, ld, pointers, p, workspace),
+ * AR_ERR_UNSUPPORTED (types), AR_ERR_ALIAS, AR_ERR_NO_DEVICE, AR_ERR_HIP. */
+ar_status ar_linear_forward(int64_t M, int64_t N, int64_t K, const ar_matrix* x, const ar_matrix* w,
+                            const ar_matrix* bias, const ar_matrix* residual, ar_activation act,
+                            const ar_dropout* drop, const ar_matrix* y, const ar_matrix* preact, void* workspace,
+                            int64_t workspace_bytes, hipStream_t stream);
+ar_status ar_linear_forward_workspace(int64_t M, int64_t N, int64_t K, const ar_matrix* x, const ar_matrix* w,
+                                      int64_t* bytes);
+
+/* The gradient of ar_linear_forward for dy [M, N], the gradient of y (of y's
+ * type), with the same x, w, act and drop, and the preact that it kept (NULL
+ * where act is AR_ACT_NONE).  dy is also the gradient of the residual.
+ *   dz = act'(preact) * drop(dy)
+ *   dx = dz w          [M, K], of x's type or float32; NULL: not computed
+ *   dw = dz^T x        [N, K], of x's type or float32; NULL: not computed
+ *   db = sum_i dz_ij   [N],    of x's type or float32; NULL: not computed
+ * With accumulate != 0 dw and db are added to what is there (gradients over
+ * several calls; a gradient buffer that is a rank buffer of a plan).  db sums
+ * dz in 32 bits.  The two products take dz in x's type, since the matrix
+ * instructions do: where act or drop is there, or dy is wider than x, dz is
+ * rounded to it, once.  x is not read without dw, nor w without dx.
+ * Workspace and errors as above. */
+ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, const ar_matrix* x,
+                             const ar_matrix* w, const ar_matrix* preact, ar_activation act, const ar_dropout* drop,
+                             const ar_matrix* dx, const ar_matrix* dw, const ar_matrix* db, int32_t accumulate,
+                             void* workspace, int64_t workspace_bytes, hipStream_t stream);
+ar_status ar_linear_backward_workspace(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, const ar_matrix* x,
+                                       const ar_matrix* w, const ar_matrix* preact, ar_activation act,
+                                       const ar_dropout* drop, const ar_matrix* dx, const ar_matrix* dw,
+                                       const ar_matrix* db, int64_t* bytes);
+
+/* y = residual + drop(x) on rows x cols matrices: x of any of the three
+ * types, y and residual (NULL: none) of any one of them.  y may be x or
+ * residual where data, ld and type are the same.  The mask is the one that
+ * ar_linear_forward draws for a result of this shape. */
+ar_status ar_dropout_forward(int64_t rows, int64_t cols, const ar_matrix* x, const ar_matrix* residual,
+                             const ar_dropout* drop, const ar_matrix* y, hipStream_t stream);
+
+/* dx = drop(dy): the gradient of ar_dropout_forward with the same drop (dy is
+ * also the residual's).  dx may be dy. */
+ar_status ar_dropout_backward(int64_t rows, int64_t cols, const ar_matrix* dy, const ar_dropout* drop,
+                              const ar_matrix* dx, hipStream_t stream);
 
 #ifdef __cplusplus
 }

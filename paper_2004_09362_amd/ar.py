@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
-from typing import Sequence
+from typing import NamedTuple, Sequence
 
 import torch  # noqa: F401  (loads the HIP runtime torch was built with, before libar.so)
 
@@ -26,12 +26,13 @@ BIND_PATH = os.path.join(_HERE, "_arbind.so")
 
 AR_OK, AR_ERR_INVALID_ARG, AR_ERR_UNSUPPORTED, AR_ERR_ALIAS = 0, 1, 2, 3
 AR_ERR_OUT_OF_MEMORY, AR_ERR_HIP, AR_ERR_NO_DEVICE, AR_ERR_INTERNAL = 4, 5, 6, 7
-AR_INT32, AR_FLOAT32 = 0, 1
+AR_INT32, AR_FLOAT32, AR_FLOAT16, AR_BFLOAT16 = 0, 1, 2, 3
 AR_SUM, AR_MAX = 0, 1
 AR_PATH_AUTO, AR_PATH_STEPWISE, AR_PATH_FUSED = 0, 1, 2
 AR_KIND_COPY, AR_KIND_REDUCE, AR_KIND_REDUCE2 = 0, 1, 2
 AR_GROUP_CYCLIC, AR_GROUP_XOR = 0, 1
 AR_SCHEDULE_BUTTERFLY, AR_SCHEDULE_RING = 0, 1
+AR_ACT_NONE, AR_ACT_RELU, AR_ACT_GELU, AR_ACT_GELU_TANH, AR_ACT_SILU = 0, 1, 2, 3, 4
 
 AR_K_AUTO = -1
 
@@ -41,6 +42,8 @@ EXPORTS = [
     "ar_last_error_message", "ar_model_time", "ar_model_best_k", "ar_plan_model_time", "ar_execute_timed",
     "ar_plan_dump", "ar_model_default_params", "ar_plan_model_seconds", "ar_plan_create_auto",
     "ar_execute_noalloc",
+    "ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward", "ar_linear_backward_workspace",
+    "ar_dropout_forward", "ar_dropout_backward",
 ]
 
 
@@ -77,6 +80,29 @@ class ModelParams(ctypes.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class Matrix(ctypes.Structure):
+    """ar_matrix: a matrix of a layer operator, as the C entry points take it."""
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class DropoutArgs(ctypes.Structure):
+    """ar_dropout, as the C entry points take it."""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("site", ctypes.c_uint32),
+                ("row0", ctypes.c_uint64)]
+
+
+class Dropout(NamedTuple):
+    """A dropout whose mask is a function of the element's place: drop
+    probability ``p`` (0 to 1), a ``seed`` for the step, the ``site`` of this
+    dropout in the model, and ``row0``, the first row's place in the whole
+    matrix where a rank holds a part of its rows.  Equal arguments drop equal
+    elements, in every operator and on every rank."""
+    p: float
+    seed: int
+    site: int = 0
+    row0: int = 0
 
 
 class LaunchDesc(ctypes.Structure):
@@ -125,6 +151,17 @@ def _load():
     L.ar_plan_model_seconds.argtypes = [vp, ctypes.POINTER(ModelParams), i64, ctypes.c_int, ctypes.POINTER(dbl)]
     L.ar_plan_create_auto.argtypes = [i32, i64, ctypes.c_int, ctypes.c_int, ctypes.c_int, i64, ctypes.c_int,
                                       ctypes.POINTER(ModelParams), ctypes.POINTER(vp)]
+    mp, dp = ctypes.POINTER(Matrix), ctypes.POINTER(DropoutArgs)
+    L.ar_linear_forward.argtypes = [i64, i64, i64, mp, mp, mp, mp, ctypes.c_int, dp, mp, mp, vp, i64, vp]
+    L.ar_linear_forward_workspace.argtypes = [i64, i64, i64, mp, mp, ctypes.POINTER(i64)]
+    L.ar_linear_backward.argtypes = [i64, i64, i64, mp, mp, mp, mp, ctypes.c_int, dp, mp, mp, mp, i32, vp, i64, vp]
+    L.ar_linear_backward_workspace.argtypes = [i64, i64, i64, mp, mp, mp, mp, ctypes.c_int, dp, mp, mp, mp,
+                                               ctypes.POINTER(i64)]
+    L.ar_dropout_forward.argtypes = [i64, i64, mp, mp, dp, mp, vp]
+    L.ar_dropout_backward.argtypes = [i64, i64, mp, dp, mp, vp]
+    for name in ("ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward",
+                 "ar_linear_backward_workspace", "ar_dropout_forward", "ar_dropout_backward"):
+        getattr(L, name).restype = ctypes.c_int
     for name in ("ar_plan_create", "ar_plan_create_ex", "ar_plan_set_path", "ar_execute", "ar_execute_batched", "ar_plan_stats",
                  "ar_plan_num_launches", "ar_plan_launch", "ar_model_time", "ar_model_best_k", "ar_plan_model_time",
                  "ar_plan_dump", "ar_execute_timed", "ar_model_default_params", "ar_plan_model_seconds",
@@ -143,10 +180,14 @@ def _load_bind():
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
     mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.ar_execute_batched, lib.ar_execute_noalloc)))
+    mod.bind_layers(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.ar_linear_forward, lib.ar_linear_forward_workspace, lib.ar_linear_backward,
+        lib.ar_linear_backward_workspace, lib.ar_dropout_forward)))
     return mod
 
 
-_bind_execute = _load_bind().execute
+_bind = _load_bind()
+_bind_execute = _bind.execute
 
 
 def status_name(s: int) -> str:
@@ -496,3 +537,89 @@ class Plan:
             self.close()
         except Exception:
             pass
+
+
+# ---- layer operators (include/ar.h, "Layer operators") ----
+
+_ACTIVATIONS = {"none": AR_ACT_NONE, "relu": AR_ACT_RELU, "gelu": AR_ACT_GELU, "gelu_tanh": AR_ACT_GELU_TANH,
+                "silu": AR_ACT_SILU}
+_FLOAT_CODES = {None: -1, torch.float32: AR_FLOAT32, torch.float16: AR_FLOAT16, torch.bfloat16: AR_BFLOAT16}
+
+
+def _activation_code(activation) -> int:
+    code = _ACTIVATIONS.get(activation)
+    if code is None:
+        raise ArError(AR_ERR_INVALID_ARG, "activation", "one of %s, got %r" % (", ".join(_ACTIVATIONS), activation))
+    return code
+
+
+def _float_code(dtype, where: str) -> int:
+    code = _FLOAT_CODES.get(dtype)
+    if code is None:
+        raise ArError(AR_ERR_UNSUPPORTED, where, "float32, float16 or bfloat16 only, got %r" % (dtype,))
+    return code
+
+
+def _layer_call(where: str, fn, args, stream):
+    """fn(*args, device, stream) on ``stream`` (default: the current one),
+    which is made current so that what the call allocates belongs to it."""
+    if stream is not None:
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream))
+        with torch.cuda.stream(stream):
+            return _layer_call(where, fn, args, None)
+    if torch.cuda.is_initialized():
+        dev = torch._C._cuda_getDevice()
+        got = fn(*args, dev, torch._C._cuda_getCurrentRawStream(dev))
+    else:  # no GPU tensor exists: the checks name the fault
+        got = fn(*args, -1, 0)
+    if type(got) is str:
+        raise ArError(AR_ERR_INVALID_ARG, where, got)
+    if type(got) is int:
+        _check(got, where)
+    return got
+
+
+def ar_linear_forward(x, w, bias=None, residual=None, *, activation: str = "none", dropout: Dropout | None = None,
+                      out=None, out_dtype=None, preact=None, stream=None):
+    """y = residual + drop(act(x w^T + bias)) for x [M, K], w [N, K].
+
+    ``activation``: "none", "relu", "gelu", "gelu_tanh" or "silu".  y is
+    ``out`` (which may be ``residual``) or a new tensor of ``out_dtype``: x's
+    type (the default) or float32, as for partial products that an Allreduce
+    sums.  With ``preact`` (a tensor, or True for a new one) the
+    pre-activation x w^T + bias is kept for :func:`ar_linear_backward` and
+    (y, preact) is returned.  Rows may have any distance; their elements are
+    consecutive."""
+    return _layer_call("ar_linear_forward", _bind.linear_forward,
+                       (x, w, bias, residual, out, preact, _activation_code(activation),
+                        _float_code(out_dtype, "out_dtype"), dropout), stream)
+
+
+def ar_linear_backward(dy, x, w, *, preact=None, activation: str = "none", dropout: Dropout | None = None, dx=True,
+                       dw=True, db=True, accumulate: bool = False, dx_dtype=None, dw_dtype=None, stream=None):
+    """The gradient of :func:`ar_linear_forward`: (dx, dw, db) for the same x,
+    w, activation and dropout, and the preact that it kept.
+
+    Each of ``dx``, ``dw`` and ``db`` is a tensor to write, True for a new
+    one, or False (None in the result).  New ones have x's type, or
+    ``dx_dtype`` / ``dw_dtype`` (dw and db): float32, as for rank buffers of a
+    :class:`Plan`.  ``accumulate`` adds to the dw and db given.  dy is the
+    residual's gradient as well."""
+    return _layer_call("ar_linear_backward", _bind.linear_backward,
+                       (dy, x, w, preact, _activation_code(activation), dropout, dx, dw, db,
+                        _float_code(dx_dtype, "dx_dtype"), _float_code(dw_dtype, "dw_dtype"), bool(accumulate)), stream)
+
+
+def ar_dropout_forward(x, dropout: Dropout, residual=None, *, out=None, out_dtype=None, stream=None):
+    """y = residual + drop(x), y of ``out_dtype`` (default x's type; the
+    residual has y's) or written to ``out``, which may be x or residual."""
+    return _layer_call("ar_dropout_forward", _bind.dropout,
+                       (x, residual, out, _float_code(out_dtype, "out_dtype"), dropout), stream)
+
+
+def ar_dropout_backward(dy, dropout: Dropout, *, out=None, out_dtype=None, stream=None):
+    """dx = drop(dy), the gradient of :func:`ar_dropout_forward` with the
+    same dropout (dy is the residual's gradient as well)."""
+    return _layer_call("ar_dropout_backward", _bind.dropout,
+                       (dy, None, out, _float_code(out_dtype, "out_dtype"), dropout), stream)

@@ -18,9 +18,11 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libar.so")
 SOURCES = [os.path.join(CSRC, f) for f in ["plan.cpp", "capi.cpp", "kernels.hip", "fused_lo.hip", "fused_group.hip",
                                            "fused_free.hip", "fused_small.hip",
-                                           "broadcast.hip", "noalloc.hip"]]
+                                           "broadcast.hip", "noalloc.hip", "layers.cpp", "gemm_bf16.hip",
+                                           "gemm_f16.hip", "gemm_f32.hip", "gemm_few.hip", "rowwise.hip"]]
 HEADERS = [os.path.join(CSRC, f) for f in ("ar_internal.hpp", "device_common.hpp", "fused_col.hpp",
-                                               "fused_free.hpp", "free_shape.hpp")] + [
+                                               "fused_free.hpp", "free_shape.hpp", "layers.hpp",
+                                               "layer_device.hpp", "gemm.hpp")] + [
     os.path.join(ROOT, "include", "ar.h")]
 # The native part of the Python binding: host code only, against torch's and Python's headers.
 BIND_SOURCE = os.path.join(CSRC, "bind.cpp")
@@ -131,9 +133,10 @@ def build(verbose: bool = False, incremental: bool = False) -> str:
     unit unless ``incremental`` (then only units older than their sources)."""
     t0 = time.time()
     os.makedirs(OBJDIR, exist_ok=True)
-    # the longest units first: the XOR/Ring unit, then the column units, then the rest
-    group = [f for f in SOURCES if os.path.basename(f) == "fused_group.hip"]
-    units = group + col_units() + [f for f in SOURCES if f not in group]
+    # the longest units first: the XOR/Ring unit and the products, then the column units, then the rest
+    first = [f for f in SOURCES if os.path.basename(f) in ("fused_group.hip", "gemm_bf16.hip", "gemm_f16.hip",
+                                                           "gemm_f32.hip")]
+    units = first + col_units() + [f for f in SOURCES if f not in first]
     workers = max(1, min(len(units), int(os.environ.get("MAX_JOBS", os.cpu_count() or 1))))
     with concurrent.futures.ThreadPoolExecutor(max_workers=workers) as ex:
         bind = ex.submit(_build_bind, incremental)
@@ -166,6 +169,8 @@ FAMILIES = {
     "free": ["fused_free.hip", "fused_free.hpp", "free_shape.hpp"],
     "small": ["fused_small.hip"],
     "bcast": ["broadcast.hip"],
+    "layer": ["layers.cpp", "layers.hpp", "layer_device.hpp", "gemm.hpp", "gemm_bf16.hip", "gemm_f16.hip",
+              "gemm_f32.hip", "gemm_few.hip", "rowwise.hip"],
 }
 
 
@@ -178,7 +183,9 @@ def kernel_families(kernel: str) -> list[str]:
                             ("fused_mid_kernel", "col"), ("fused_rot_kernel", "col"), ("fused_xor_kernel", "group"),
                             ("fused_ring_kernel", "group"), ("fused_free_kernel", "free"),
                             ("fused_small_kernel", "small"), ("fused_wide_kernel", "col"),
-                            ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast")):
+                            ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast"),
+                            ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer"),
+                            ("column_sums_kernel", "layer")):
             if part.startswith(prefix):
                 out.append(fam)
                 break

@@ -381,4 +381,8 @@ int noalloc_scratch(int device, void** ptr);
 int step_grid(int64_t total_tiles);
 int64_t step_tile_elems();
 
+// What ar_last_error_message returns on the calling thread from now on: for
+// the entry points outside capi.cpp.
+void set_failure_text(const char* text) noexcept;
+
 }  // namespace ar

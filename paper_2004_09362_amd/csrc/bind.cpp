@@ -1,4 +1,5 @@
-// bind.cpp -- the execute calls of the Python binding (ar.py) in native code.
+// bind.cpp -- the execute calls and the layer operators of the Python binding
+// (ar.py) in native code.
 //
 // A call passes up to 128 rank tensors.  Checking each of them and reading
 // its address in Python cost 0.14 us per rank and 4 us per call, most of the
@@ -7,9 +8,12 @@
 // call to the next).  Whatever fails one, or is no plain torch tensor in a
 // list or tuple -- raw addresses, subclasses, other sequences -- is answered
 // with None, and the caller takes the Python path, which names the fault.
+#include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <exception>
+#include <string>
 
 #include "../../include/ar.h"
 
@@ -96,7 +100,298 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   Py_RETURN_NONE;
 }
 
+// ---- layer operators ----
+//
+// The layer calls read their tensors, allocate what they return and the
+// workspace, and call the library, all on the current device and stream (the
+// Python side makes a given stream current).  A failed check is a Fault: its
+// text is returned, and ar.py raises it; the library's own status is returned
+// as a number.
+
+ar_status (*g_linear_forward)(int64_t, int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*,
+                              const ar_matrix*, ar_activation, const ar_dropout*, const ar_matrix*, const ar_matrix*,
+                              void*, int64_t, hipStream_t) = nullptr;
+ar_status (*g_linear_forward_workspace)(int64_t, int64_t, int64_t, const ar_matrix*, const ar_matrix*,
+                                        int64_t*) = nullptr;
+ar_status (*g_linear_backward)(int64_t, int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*,
+                               const ar_matrix*, ar_activation, const ar_dropout*, const ar_matrix*, const ar_matrix*,
+                               const ar_matrix*, int32_t, void*, int64_t, hipStream_t) = nullptr;
+ar_status (*g_linear_backward_workspace)(int64_t, int64_t, int64_t, const ar_matrix*, const ar_matrix*,
+                                         const ar_matrix*, const ar_matrix*, ar_activation, const ar_dropout*,
+                                         const ar_matrix*, const ar_matrix*, const ar_matrix*, int64_t*) = nullptr;
+ar_status (*g_dropout_forward)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_dropout*,
+                               const ar_matrix*, hipStream_t) = nullptr;
+
+struct Fault {
+  std::string text;
+};
+
+// What a call needs to know of where it runs.
+struct Place {
+  int64_t device, stream;
+  hipStream_t hip() const { return reinterpret_cast<hipStream_t>(stream); }
+};
+
+int64_t number(PyObject* o, const char* name) {
+  int64_t v;
+  if (!as_int(o, &v)) throw Fault{std::string(name) + " must be an integer"};
+  return v;
+}
+
+ar_dtype dtype_of(const at::Tensor& t, const char* name) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return AR_FLOAT32;
+    case at::kHalf: return AR_FLOAT16;
+    case at::kBFloat16: return AR_BFLOAT16;
+    default: throw Fault{std::string(name) + " must be float32, float16 or bfloat16"};
+  }
+}
+at::ScalarType scalar_of(int64_t code, at::ScalarType otherwise) {
+  switch (code) {
+    case -1: return otherwise;
+    case AR_FLOAT32: return at::kFloat;
+    case AR_FLOAT16: return at::kHalf;
+    case AR_BFLOAT16: return at::kBFloat16;
+    default: throw Fault{"results are float32, float16 or bfloat16"};
+  }
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name) {
+  if (!THPVariable_Check(o)) throw Fault{std::string(name) + " must be a tensor"};
+  return THPVariable_Unpack(o);
+}
+
+// A tensor of `dims` dimensions (2, or 1: a vector) with consecutive elements
+// in a row, on the call's device; rows and cols < 0 are not checked.
+ar_matrix view(const at::Tensor& t, const char* name, int dims, int64_t rows, int64_t cols, const Place& at_) {
+  const std::string n(name);
+  if (t.layout() != at::kStrided) throw Fault{n + " must be a dense tensor"};
+  if (!t.is_cuda()) throw Fault{n + " is not on a GPU"};
+  if (t.get_device() != at_.device)
+    throw Fault{n + " is on cuda:" + std::to_string(t.get_device()) + ", the current device is cuda:" +
+                std::to_string(at_.device)};
+  if (t.dim() != dims) throw Fault{n + " must have " + std::to_string(dims) + " dimension" + (dims > 1 ? "s" : "")};
+  ar_matrix m;
+  m.dtype = dtype_of(t, name);
+  const int64_t r = dims == 2 ? t.size(0) : 1, c = t.size(dims - 1);
+  if ((rows >= 0 && r != rows) || (cols >= 0 && c != cols))
+    throw Fault{n + " is " + std::to_string(r) + " x " + std::to_string(c) + ", the call needs " +
+                (rows >= 0 ? std::to_string(rows) : std::string("any")) + " x " +
+                (cols >= 0 ? std::to_string(cols) : std::string("any"))};
+  if (c > 1 && t.stride(dims - 1) != 1) throw Fault{n + "'s rows must have consecutive elements"};
+  if (r > 1 && t.stride(0) < c) throw Fault{n + "'s rows overlap"};
+  m.ld = r > 1 ? t.stride(0) : c;
+  m.data = t.numel() > 0 ? t.data_ptr() : nullptr;
+  return m;
+}
+
+// None or (p, seed, site, row0).
+const ar_dropout* dropout_of(PyObject* o, ar_dropout* d) {
+  if (o == Py_None) return nullptr;
+  if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) throw Fault{"dropout must be a Dropout"};
+  d->p = PyFloat_AsDouble(PyTuple_GET_ITEM(o, 0));
+  const bool bad_p = PyErr_Occurred() != nullptr;
+  PyErr_Clear();
+  if (bad_p) throw Fault{"dropout's p must be a number"};
+  uint64_t v[3];
+  for (int i = 0; i < 3; ++i) {
+    PyObject* x = PyTuple_GET_ITEM(o, i + 1);
+    v[i] = PyLong_Check(x) ? PyLong_AsUnsignedLongLong(x) : 0;
+    const bool bad = !PyLong_Check(x) || PyErr_Occurred() != nullptr;
+    PyErr_Clear();
+    if (bad) throw Fault{"dropout's seed, site and row0 must be integers from 0 to 2^64 - 1"};
+  }
+  if (v[1] >> 32) throw Fault{"dropout's site must be below 2^32"};
+  d->seed = v[0];
+  d->site = uint32_t(v[1]);
+  d->row0 = v[2];
+  return d;
+}
+
+at::Tensor workspace(int64_t bytes, const at::Tensor& like) {
+  return bytes > 0 ? at::empty({bytes}, like.options().dtype(at::kByte)) : at::Tensor();
+}
+void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// Runs a call's body; what it throws becomes the text that ar.py raises.
+template <typename F>
+PyObject* answer(F&& body) {
+  try {
+    return body();
+  } catch (const Fault& f) {
+    return PyUnicode_FromString(f.text.c_str());
+  } catch (const std::bad_alloc&) {
+    return PyErr_NoMemory();
+  } catch (const std::exception& e) {  // torch's own, of an allocation
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// linear_forward(x, w, bias, residual, out, preact, activation, out dtype, dropout, device, stream)
+// -> y, (y, z) where preact is a tensor or True, a status, or a text.
+PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 11 || !g_linear_forward) throw Fault{"linear_forward takes 11 arguments"};
+    const Place at_{number(args[9], "device"), number(args[10], "stream")};
+    const at::Tensor& x = tensor(args[0], "x");
+    const at::Tensor& w = tensor(args[1], "w");
+    const ar_matrix mx = view(x, "x", 2, -1, -1, at_);
+    const int64_t M = x.size(0), K = x.size(1);
+    const ar_matrix mw = view(w, "w", 2, -1, K, at_);
+    const int64_t N = w.size(0);
+    ar_matrix mb, mr, mz;
+    if (args[2] != Py_None) mb = view(tensor(args[2], "bias"), "bias", 1, 1, N, at_);
+    if (args[3] != Py_None) mr = view(tensor(args[3], "residual"), "residual", 2, M, N, at_);
+    const int64_t act = number(args[6], "activation"), code = number(args[7], "out dtype");
+    ar_dropout d;
+    const ar_dropout* drop = dropout_of(args[8], &d);
+    at::Tensor y, z;
+    if (args[4] != Py_None) y = tensor(args[4], "out");
+    else y = at::empty({M, N}, x.options().dtype(scalar_of(code, x.scalar_type())));
+    if (args[5] == Py_True) z = at::empty({M, N}, x.options());
+    else if (args[5] != Py_None && args[5] != Py_False) z = tensor(args[5], "preact");
+    const ar_matrix my = view(y, "out", 2, M, N, at_);
+    if (z.defined()) mz = view(z, "preact", 2, M, N, at_);
+    int64_t bytes = 0;
+    ar_status st = g_linear_forward_workspace(M, N, K, &mx, &mw, &bytes);
+    if (st == AR_OK) {
+      const at::Tensor ws = workspace(bytes, x);
+      Py_BEGIN_ALLOW_THREADS
+      st = g_linear_forward(M, N, K, &mx, &mw, args[2] != Py_None ? &mb : nullptr, args[3] != Py_None ? &mr : nullptr,
+                            ar_activation(act), drop, &my, z.defined() ? &mz : nullptr, address(ws), bytes, at_.hip());
+      Py_END_ALLOW_THREADS
+    }
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    PyObject* py = THPVariable_Wrap(y);
+    if (!z.defined() || !py) return py;
+    PyObject* pz = THPVariable_Wrap(z);
+    PyObject* both = pz ? PyTuple_Pack(2, py, pz) : nullptr;
+    Py_DECREF(py);
+    Py_XDECREF(pz);
+    return both;
+  });
+}
+
+// None and False: not wanted; True: a new tensor; else the tensor given.
+at::Tensor wanted(PyObject* o, const char* name, at::IntArrayRef shape, const at::TensorOptions& options) {
+  if (o == Py_None || o == Py_False) return at::Tensor();
+  if (o == Py_True) return at::empty(shape, options);
+  return tensor(o, name);
+}
+
+// linear_backward(dy, x, w, preact, activation, dropout, dx, dw, db, dx dtype, dw dtype, accumulate, device, stream)
+// -> (dx, dw, db) with None for what was not wanted, a status, or a text.
+PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 14 || !g_linear_backward) throw Fault{"linear_backward takes 14 arguments"};
+    const Place at_{number(args[12], "device"), number(args[13], "stream")};
+    const at::Tensor& dy = tensor(args[0], "dy");
+    const at::Tensor& x = tensor(args[1], "x");
+    const at::Tensor& w = tensor(args[2], "w");
+    const ar_matrix mdy = view(dy, "dy", 2, -1, -1, at_);
+    const int64_t M = dy.size(0), N = dy.size(1);
+    const ar_matrix mx = view(x, "x", 2, M, -1, at_);
+    const int64_t K = x.size(1);
+    const ar_matrix mw = view(w, "w", 2, N, K, at_);
+    ar_matrix mz, mdx, mdw, mdb;
+    const bool has_z = args[3] != Py_None;
+    if (has_z) mz = view(tensor(args[3], "preact"), "preact", 2, M, N, at_);
+    const int64_t act = number(args[4], "activation");
+    ar_dropout d;
+    const ar_dropout* drop = dropout_of(args[5], &d);
+    const auto same = x.options();
+    const auto other = same.dtype(scalar_of(number(args[10], "dw dtype"), x.scalar_type()));
+    const bool accumulate = args[11] == Py_True;
+    if (accumulate && (args[7] == Py_True || args[8] == Py_True))
+      throw Fault{"accumulate adds to the dw and db that are given: they must be tensors"};
+    const at::Tensor dx =
+        wanted(args[6], "dx", {M, K}, same.dtype(scalar_of(number(args[9], "dx dtype"), x.scalar_type())));
+    const at::Tensor dw = wanted(args[7], "dw", {N, K}, other), db = wanted(args[8], "db", {N}, other);
+    if (dx.defined()) mdx = view(dx, "dx", 2, M, K, at_);
+    if (dw.defined()) mdw = view(dw, "dw", 2, N, K, at_);
+    if (db.defined()) mdb = view(db, "db", 1, 1, N, at_);
+    const ar_matrix* pz = has_z ? &mz : nullptr;
+    const ar_matrix* pdx = dx.defined() ? &mdx : nullptr;
+    const ar_matrix* pdw = dw.defined() ? &mdw : nullptr;
+    const ar_matrix* pdb = db.defined() ? &mdb : nullptr;
+    int64_t bytes = 0;
+    ar_status st = g_linear_backward_workspace(M, N, K, &mdy, &mx, &mw, pz, ar_activation(act), drop, pdx, pdw, pdb,
+                                               &bytes);
+    if (st == AR_OK) {
+      const at::Tensor ws = workspace(bytes, dy);
+      Py_BEGIN_ALLOW_THREADS
+      st = g_linear_backward(M, N, K, &mdy, &mx, &mw, pz, ar_activation(act), drop, pdx, pdw, pdb, accumulate,
+                             address(ws), bytes, at_.hip());
+      Py_END_ALLOW_THREADS
+    }
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    PyObject* got = PyTuple_New(3);
+    const at::Tensor* const parts[] = {&dx, &dw, &db};
+    for (int i = 0; got && i < 3; ++i) {
+      PyObject* o = Py_None;
+      if (parts[i]->defined()) o = THPVariable_Wrap(*parts[i]);
+      else Py_INCREF(o);
+      if (!o) {
+        Py_DECREF(got);
+        return nullptr;
+      }
+      PyTuple_SET_ITEM(got, i, o);
+    }
+    return got;
+  });
+}
+
+// dropout(x, residual, out, out dtype, dropout, device, stream) -> y, a status, or a text.
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 7 || !g_dropout_forward) throw Fault{"dropout takes 7 arguments"};
+    const Place at_{number(args[5], "device"), number(args[6], "stream")};
+    const at::Tensor& x = tensor(args[0], "x");
+    const ar_matrix mx = view(x, "x", 2, -1, -1, at_);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    ar_matrix mr;
+    if (args[1] != Py_None) mr = view(tensor(args[1], "residual"), "residual", 2, rows, cols, at_);
+    const int64_t code = number(args[3], "out dtype");
+    at::Tensor y;
+    if (args[2] != Py_None) y = tensor(args[2], "out");
+    else y = at::empty({rows, cols}, x.options().dtype(scalar_of(code, x.scalar_type())));
+    const ar_matrix my = view(y, "out", 2, rows, cols, at_);
+    ar_dropout d;
+    const ar_dropout* drop = dropout_of(args[4], &d);
+    ar_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = g_dropout_forward(rows, cols, &mx, args[1] != Py_None ? &mr : nullptr, drop, &my, at_.hip());
+    Py_END_ALLOW_THREADS
+    return st == AR_OK ? THPVariable_Wrap(y) : PyLong_FromLong(long(st));
+  });
+}
+
+// bind_layers(addresses of the five functions above, in their order)
+PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  int64_t a[5];
+  for (int i = 0; i < 5; ++i) {
+    if (nargs != 5 || !as_int(args[i], &a[i])) {
+      PyErr_SetString(PyExc_TypeError, "bind_layers takes five addresses");
+      return nullptr;
+    }
+  }
+  g_linear_forward = reinterpret_cast<decltype(g_linear_forward)>(a[0]);
+  g_linear_forward_workspace = reinterpret_cast<decltype(g_linear_forward_workspace)>(a[1]);
+  g_linear_backward = reinterpret_cast<decltype(g_linear_backward)>(a[2]);
+  g_linear_backward_workspace = reinterpret_cast<decltype(g_linear_backward_workspace)>(a[3]);
+  g_dropout_forward = reinterpret_cast<decltype(g_dropout_forward)>(a[4]);
+  Py_RETURN_NONE;
+}
+
+template <typename F>
+PyCFunction fastcall(F f) { return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)); }
+
 PyMethodDef kMethods[] = {
+    {"linear_forward", fastcall(linear_forward), METH_FASTCALL, nullptr},
+    {"linear_backward", fastcall(linear_backward), METH_FASTCALL, nullptr},
+    {"dropout", fastcall(dropout), METH_FASTCALL, nullptr},
+    {"bind_layers", fastcall(bind_layers), METH_FASTCALL, nullptr},
     {"execute", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(execute)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -286,6 +286,22 @@ ar_status hip_fail(hipError_t e, const char* what) {
   return AR_ERR_HIP;
 }
 
+}  // namespace
+
+namespace ar {
+
+void set_failure_text(const char* text) noexcept {
+  try {
+    g_err = text;
+  } catch (...) {
+    g_err.clear();
+  }
+}
+
+}  // namespace ar
+
+namespace {
+
 int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
 
 // Check the table of rank pointers: non-null, 4-byte aligned, no overlap.

@@ -1,0 +1,455 @@
+// gemm.hpp -- the tiled matrix product of the linear layer and its gradient,
+// with the epilogue in its registers.  Instantiated per element type in
+// gemm_f32.hip, gemm_f16.hip and gemm_bf16.hip.
+//
+// v[m][n] = sum_k a(m, k) b(n, k), sums in 32 bits.  A workgroup of WM x WN
+// waves computes a tile of TM x TN, each wave (16 MT) x (16 NT) of it in
+// 16 x 16 matrix instructions.  The instructions take b's rows as their first
+// operand and a's as their second, so that a lane's sums are consecutive
+// columns n of one row m and leave in 16-byte pieces.
+//
+// Inner lengths of 128 bytes at a time are staged in LDS, two buffers, every
+// operand in the order that it has in memory:
+//   k-major:  one row m (or n) is 128 bytes, 8 chunks of 16; a fragment is one
+//             16-byte read (8 halves for one 16x16x32 instruction, 4 floats
+//             for four 16x16x4);
+//   otherwise one inner index k is a row of TM (or TN) elements; a fragment of
+//             halves is two transposing 8-byte reads, one of floats four
+//             4-byte reads.
+// Both orders give lane group g = lane / 16 the same inner indices (8 g to
+// 8 g + 7, or 4 g to 4 g + 3, of a 64-byte slice), so they can be mixed.
+// Chunks lie at a position XORed with a function of their row (swz_a, swz_b
+// below), which spreads a fragment read's lanes over all banks.
+//
+// Columns of the wave are dealt to instructions so that tiles 2j and 2j + 1
+// together give a lane 8 consecutive ones: row 4 p + r of tile t is column
+// 32 (t / 2) + 8 p + 4 (t % 2) + r of the wave where b is k-major, and
+// 32 (t / 2) + 8 p + 4 ((t + p) % 2) + r otherwise (there the four 8-byte
+// pieces that a row of the transposing read takes, and its four rows, then
+// fall on different banks; odd lane groups swap the two tiles' sums).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "layer_device.hpp"
+
+namespace ar {
+
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4v __attribute__((ext_vector_type(4)));
+typedef short s16x4v __attribute__((ext_vector_type(4)));
+typedef short s16x8v __attribute__((ext_vector_type(8)));
+typedef f16 f16x8v __attribute__((ext_vector_type(8)));
+typedef bf16 bf16x8v __attribute__((ext_vector_type(8)));
+
+// One 64-byte slice of inner length of a 16 x 16 product; the operands are
+// the lanes' 16 bytes.
+template <typename T>
+__device__ __forceinline__ f32x4v mma(const i32x4v& rows_n, const i32x4v& rows_m, f32x4v acc) {
+  if constexpr (elem_of<T>() == kBF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, rows_n),
+                                                   __builtin_bit_cast(bf16x8v, rows_m), acc, 0, 0, 0);
+  } else if constexpr (elem_of<T>() == kF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8v, rows_n),
+                                                  __builtin_bit_cast(f16x8v, rows_m), acc, 0, 0, 0);
+  } else {
+    const f32x4v n4 = __builtin_bit_cast(f32x4v, rows_n), m4 = __builtin_bit_cast(f32x4v, rows_m);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(n4[e], m4[e], acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// 16 bytes of a row, elements past `have` zero.
+template <typename T>
+__device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have) {
+  constexpr int V = 16 / int(sizeof(T));
+  typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  typedef T W __attribute__((ext_vector_type(V)));
+  if (have >= V) {
+    const U u = *reinterpret_cast<const U*>(p);
+    return __builtin_bit_cast(i32x4v, W(u));
+  }
+  W w;
+#pragma unroll
+  for (int i = 0; i < V; ++i) w[i] = i < have ? p[i] : T(0);
+  return __builtin_bit_cast(i32x4v, w);
+}
+
+using LdsPtr = __attribute__((address_space(3))) char*;
+
+__device__ __forceinline__ uint32_t lds_offset(const char* p) {
+  return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
+}
+
+// 64 lanes' 16 bytes from base + voff to 1024 consecutive bytes of LDS, past
+// the registers.  The compiler's own form of this instruction makes every
+// later LDS read wait for it; here the caller waits (wait_all), one tile
+// later.  It has no register outputs, and nothing else here uses m0.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base)
+               : "memory");
+}
+
+// All of this wave's loads have arrived, its LDS reads and writes are done,
+// and so are those of the workgroup's other waves.
+__device__ __forceinline__ void wait_all() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// An operand's tile: R rows of the output, 128 bytes of inner length each.
+// FIRST: the operand b, whose rows are dealt to instructions as above.
+template <typename T, bool KMAJOR, bool FIRST, int R, int THREADS>
+struct Operand {
+  static constexpr int kElems = 16 / int(sizeof(T));          // elements of a chunk
+  static constexpr int kInner = kTileKBytes / int(sizeof(T));  // inner indices of a tile
+  static constexpr int kChunks = R * 8;
+  static constexpr int kSlots = kChunks / THREADS;
+  static constexpr int kRowChunks = KMAJOR ? 8 : R / kElems;   // chunks of a row of the tile
+  static constexpr int kRowBytes = 16 * kRowChunks;
+  static constexpr int kSlotRows = THREADS / kRowChunks;       // tile rows between a thread's slots
+  static constexpr int kBytes = R * kTileKBytes;
+  static_assert(kSlots * THREADS == kChunks && kSlotRows * kRowChunks == THREADS, "whole slots");
+
+  // Chunk c of tile row r lies at position c ^ swz(r).
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (KMAJOR) return FIRST ? (r & 3) | ((r >> 1) & 4) : r & 7;
+    else if constexpr (sizeof(T) == 2) return FIRST ? ((r & 1) << 2) | ((r >> 1) & 1) : (r & 3) << 1;
+    else return FIRST ? ((r >> 2) & 1) | (r & 8) : (r & 12);
+  }
+
+  const char* base;   // element (first row, first inner index of the split)
+  int64_t ld;         // bytes between rows of the matrix
+  int32_t rows;       // rows of the output left from the tile's first one
+  uint32_t voff[kSlots];
+
+  // Byte offsets of this thread's chunks from the tile's first element.  A
+  // chunk of rows past the last is read from the last (k-major) or the first
+  // (otherwise): its products land in sums that are never stored.
+  __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int tid) {
+    ld = ld_elems * int64_t(sizeof(T));
+    rows = int32_t(nrows - row0 < R ? nrows - row0 : R);
+    base = reinterpret_cast<const char*>(p) +
+           (KMAJOR ? row0 * ld + k0 * int64_t(sizeof(T)) : k0 * ld + row0 * int64_t(sizeof(T)));
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
+      if constexpr (KMAJOR) voff[i] = uint32_t(r < rows ? r : rows - 1) * uint32_t(ld) + uint32_t(c * 16);
+      else voff[i] = uint32_t(r) * uint32_t(ld) + uint32_t(c * kElems < rows ? c * 16 : 0);
+    }
+  }
+
+  // The start of inner tile t.
+  __device__ __forceinline__ const char* at(int32_t t) const {
+    return base + (KMAJOR ? int64_t(t) * kTileKBytes : int64_t(t) * kInner * ld);
+  }
+
+  // Starts the asynchronous loads of whole tile t into LDS.
+  template <int I0, int I1>
+  __device__ __forceinline__ void issue(int32_t t, uint32_t lds, int wave) const {
+    const char* p = at(t);
+#pragma unroll
+    for (int i = I0; i < I1; ++i) load_to_lds(p, voff[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
+  }
+
+  // This thread's chunk i of tile t, of which k_have inner indices exist.
+  __device__ __forceinline__ i32x4v chunk(int i, int32_t t, int64_t k_have, int tid) const {
+    const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
+    const int64_t have = KMAJOR ? (r < rows ? k_have - c * kElems : 0) : (r < k_have ? rows - c * kElems : 0);
+    return load_chunk(reinterpret_cast<const T*>(at(t) + int64_t(r) * ld + c * 16), have);
+  }
+  __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) reg[i] = chunk(i, t, k_have, tid);
+  }
+  __device__ __forceinline__ void store(const i32x4v (&reg)[kSlots], char* lds, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) *reinterpret_cast<i32x4v*>(lds + (i * THREADS + tid) * 16) = reg[i];
+  }
+  __device__ __forceinline__ void copy(int32_t t, int64_t k_have, char* lds, int tid) const {
+#pragma unroll 1
+    for (int i = 0; i < kSlots; ++i) *reinterpret_cast<i32x4v*>(lds + (i * THREADS + tid) * 16) = chunk(i, t, k_have, tid);
+  }
+};
+
+// Reads of a wave's fragments from an operand's tile in LDS.
+template <typename T, bool KMAJOR, bool FIRST, int R>
+struct Fragments {
+  static constexpr int kRowBytes = KMAJOR ? kTileKBytes : R * int(sizeof(T));
+  uint32_t off[4];
+
+  // w0: the wave's first row in the tile (a multiple of 64).
+  __device__ __forceinline__ void init(int w0, int lane) {
+    const int i = lane & 15, g = lane >> 4;
+    using Op = Operand<T, KMAJOR, FIRST, R, R>;
+    if constexpr (KMAJOR) {
+      const int row = w0 + (FIRST ? 8 * (i >> 2) + (i & 3) : i);  // of tile t = 0; the others keep swz
+      off[0] = uint32_t(row * kTileKBytes + ((g ^ Op::swz(row)) * 16));
+      off[1] = off[0] ^ 64;
+    } else if constexpr (sizeof(T) == 2) {
+      const int k = 8 * g + (i >> 2);  // and k + 4: the same swz
+      const int p = i & 3;             // the 8-byte piece that this lane fetches
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        const int col = w0 + (FIRST ? 8 * p + 4 * ((odd ^ p) & 1) : 16 * odd + 4 * p);
+        const int c = col / 8;
+        off[odd] = uint32_t(k * kRowBytes + ((c ^ Op::swz(k)) * 16) + (col % 8) * 2);
+      }
+    } else {
+      const int p = i >> 2;
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        const int col = w0 + (FIRST ? 8 * p + 4 * ((odd ^ p) & 1) : 16 * odd + 4 * p) + (i & 3);
+        const int c = col / 4;
+        const int k = 4 * g;  // to 4 g + 3: the same swz; slice 1 is 16 rows further
+        off[odd] = uint32_t(k * kRowBytes + ((c ^ Op::swz(k)) * 16) + (col % 4) * 4);
+      }
+    }
+  }
+
+  // The fragment of tile t (16 rows of the wave), slice s.
+  __device__ __forceinline__ i32x4v read(const char* lds, int t, int s) const {
+    if constexpr (KMAJOR) {
+      const int row = FIRST ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t;
+      return *reinterpret_cast<const i32x4v*>(lds + off[s] + row * kTileKBytes);
+    } else if constexpr (sizeof(T) == 2) {
+      // tiles 2j and 2j + 1 take 32 rows: 64 bytes = 4 chunks of a tile row;
+      // the XOR of swz stays within 8 chunks (see off), so whole groups of 8
+      // chunks are added and the lower bit of j is XORed in
+      const int j = t >> 1;
+      const char* p = lds + ((off[t & 1] ^ uint32_t((j & 1) * 64)) + uint32_t((j >> 1) * 128 + s * 32 * kRowBytes));
+      typedef __attribute__((address_space(3))) s16x4v Lds4;
+      const s16x4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)p);
+      const s16x4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds4*)(p + 4 * kRowBytes));
+      return __builtin_bit_cast(i32x4v, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else {
+      // 32 rows are 128 bytes: 8 chunks; the XOR stays within 16
+      const int j = t >> 1;
+      const char* p = lds + ((off[t & 1] ^ uint32_t((j & 1) * 128)) + uint32_t((j >> 1) * 256 + s * 16 * kRowBytes));
+      i32x4v v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const int32_t*>(p + e * kRowBytes);
+      return v;
+    }
+  }
+};
+
+// Order of the tiles: each XCD (workgroups go round the eight) takes a
+// contiguous share of a list that walks the columns in groups of 8 rows of
+// tiles, so that its L2 serves the operands that its tiles share.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t& m, uint32_t& n) {
+  const uint32_t total = tm * tn, x = id & 7, per = total >> 3, more = total & 7;
+  const uint32_t t = x * per + (x < more ? x : more) + (id >> 3);
+  constexpr uint32_t G = 8;
+  const uint32_t group = t / (G * tn), first = group * G;
+  const uint32_t h = tm - first < G ? tm - first : G, in = t - group * G * tn;
+  m = first + in % h;
+  n = in / h;
+}
+
+template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC>
+__global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kernel(GemmArgs g) {
+  constexpr int THREADS = WM * WN * 64, TM = WM * MT * 16, TN = WN * NT * 16;
+  using OpA = Operand<T, AK, false, TM, THREADS>;
+  using OpB = Operand<T, BK, true, TN, THREADS>;
+  constexpr int kBuf = OpA::kBytes + OpB::kBytes;
+  constexpr int kInner = OpA::kInner;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  uint32_t im, in;
+  tile_of(blockIdx.x, uint32_t(g.tiles_m), uint32_t(g.tiles_n), im, in);
+  const int32_t m0 = int32_t(im) * TM, n0 = int32_t(in) * TN;
+  const int32_t k0 = int32_t(blockIdx.y) * g.k_split;
+  const int32_t klen = g.K - k0 < g.k_split ? g.K - k0 : g.k_split;
+
+  OpA a;
+  OpB b;
+  a.init(static_cast<const T*>(g.a), g.lda, m0, k0, g.e.M, tid);
+  b.init(static_cast<const T*>(g.b), g.ldb, n0, k0, g.e.N, tid);
+  Fragments<T, AK, false, TM> ra;
+  Fragments<T, BK, true, TN> rb;
+  ra.init(wm * MT * 16, lane);
+  rb.init(wn * NT * 16, lane);
+
+  f32x4v acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const int32_t tiles = (klen + kInner - 1) / kInner;
+  auto buf_a = [&](int t) { return lds + (t & 1) * kBuf; };
+  auto buf_b = [&](int t) { return lds + (t & 1) * kBuf + OpA::kBytes; };
+  // a tile through registers: its last, partial one, and every one where the
+  // operands' alignment rules the asynchronous loads out
+  auto stage = [&](int32_t t) {
+    a.copy(t, klen - int64_t(t) * kInner, buf_a(t), tid);
+    b.copy(t, klen - int64_t(t) * kInner, buf_b(t), tid);
+  };
+
+  if constexpr (ASYNC) {
+    const uint32_t lds0 = lds_offset(lds);
+    auto issue = [&](int32_t t) {
+      if ((t + 1) * kInner <= klen) {
+        a.template issue<0, OpA::kSlots>(t, lds0 + (t & 1) * kBuf, wave);
+        b.template issue<0, OpB::kSlots>(t, lds0 + (t & 1) * kBuf + OpA::kBytes, wave);
+      } else if (t < tiles) {
+        stage(t);
+      }
+    };
+    // Slice 0 of a tile is multiplied while slice 1 is read, and slice 1
+    // while slice 0 of the next tile is; the tile after that is on its way
+    // from the moment that every wave has read the whole of this one.
+    i32x4v fa[2][MT], fb[2][NT];
+    issue(0);
+    wait_all();
+    issue(1);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[0][i] = ra.read(buf_a(0), i, 0);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) fb[0][j] = rb.read(buf_b(0), j, 0);
+    for (int32_t t = 0; t < tiles; ++t) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[1][i] = ra.read(buf_a(t), i, 1);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fb[1][j] = rb.read(buf_b(t), j, 1);
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[0][j], fa[0][i], acc[i][j]);
+      wait_all();
+      issue(t + 2);
+      if (t + 1 < tiles) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[0][i] = ra.read(buf_a(t + 1), i, 0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[0][j] = rb.read(buf_b(t + 1), j, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[1][j], fa[1][i], acc[i][j]);
+    }
+  } else {
+    stage(0);
+    wait_all();
+    for (int32_t t = 0; t < tiles; ++t) {
+      i32x4v xa[OpA::kSlots], xb[OpB::kSlots];
+      if (t + 1 < tiles) {
+        a.load(xa, t + 1, klen - int64_t(t + 1) * kInner, tid);
+        b.load(xb, t + 1, klen - int64_t(t + 1) * kInner, tid);
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        i32x4v fa[MT], fb[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[i] = ra.read(buf_a(t), i, s);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = rb.read(buf_b(t), j, s);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
+      }
+      if (t + 1 < tiles) {
+        a.store(xa, buf_a(t + 1), tid);
+        b.store(xb, buf_b(t + 1), tid);
+      }
+      wait_all();
+    }
+  }
+
+  // The sums leave through LDS, each wave by itself in its share of the
+  // buffers: a lane of tiles 2j, 2j + 1 writes its 8 columns (32 j + 8 p on)
+  // of a row as one 32-byte unit, at a place XORed with the row so that 16
+  // rows fall on different banks, and then takes 8 columns of one row whose
+  // other columns its neighbours take: whole lines of y, z and the residual.
+  constexpr int kUnits = NT * 2;                                // 8-column units of a wave's row
+  constexpr int kRows = 2 * kBuf / (WM * WN) / (kUnits * 32);   // rows of the share
+  constexpr int kRounds = MT * 16 > kRows ? MT * 16 / kRows : 1, kTilesRound = MT / kRounds;
+  constexpr int kPassRows = 64 / kUnits, kPasses = kTilesRound * 16 / kPassRows, kAhead = 4;
+  static_assert(kTilesRound * kRounds == MT && kPasses % kAhead == 0, "whole rounds");
+  char* share = lds + wave * (2 * kBuf / (WM * WN));
+  const bool swap = !BK && (lane & 16);
+  const int32_t unit = lane % kUnits, n = n0 + wn * NT * 16 + 8 * unit;
+  const int have = g.e.N - n;
+  float* part = g.part + int64_t(blockIdx.y) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
+  float bias[8];
+  load_bias<T, 8>(bias, g.e, n);
+#pragma unroll
+  for (int round = 0; round < kRounds; ++round) {
+    if (round == 0) wait_all();
+    else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kTilesRound; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT / 2; ++j) {
+        const f32x4v x = acc[round * kTilesRound + i][2 * j], y = acc[round * kTilesRound + i][2 * j + 1];
+        const int r = 16 * i + (lane & 15), u = (4 * j + (lane >> 4)) ^ (r & (kUnits - 1));
+        f32x4v* q = reinterpret_cast<f32x4v*>(share + (r * kUnits + u) * 32);
+        q[0] = swap ? y : x;
+        q[1] = swap ? x : y;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int32_t mw = m0 + (wm * MT + round * kTilesRound) * 16 + lane / kUnits;
+    for (int pass = 0; pass < kPasses; pass += kAhead) {
+      float v[kAhead][8], res[kAhead][8];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int r = (pass + q) * kPassRows + lane / kUnits;
+        const f32x4v* w = reinterpret_cast<const f32x4v*>(share + (r * kUnits + (unit ^ (r & (kUnits - 1)))) * 32);
+        const f32x4v x = w[0], y = w[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[q][e] = x[e];
+          v[q][4 + e] = y[e];
+        }
+        const int32_t m = mw + (pass + q) * kPassRows;
+        if (g.splits == 1 && m < g.e.M) load_residual<T, 8>(res[q], g.e, m, n);
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int32_t m = mw + (pass + q) * kPassRows;
+        if (m >= g.e.M || have <= 0) continue;
+        if (g.splits > 1) {
+          f32x4v* w = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
+          w[0] = f32x4v{v[q][0], v[q][1], v[q][2], v[q][3]};
+          w[1] = f32x4v{v[q][4], v[q][5], v[q][6], v[q][7]};
+        } else {
+          emit<T, 8>(v[q], bias, res[q], g.e, m, n);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, bool AK, bool BK>
+int launch_layout(const GemmArgs& g, bool aligned, int32_t shape, hipStream_t st) {
+  const dim3 grid(uint32_t(g.tiles_m) * uint32_t(g.tiles_n), uint32_t(g.splits));
+  if (shape == kTile256) {
+    if (!aligned) return int(hipErrorInvalidValue);
+    gemm_kernel<T, AK, BK, 8, 8, 2, 2, true><<<grid, dim3(256), 0, st>>>(g);
+  } else if (aligned) {
+    gemm_kernel<T, AK, BK, 4, 4, 2, 2, true><<<grid, dim3(256), 0, st>>>(g);
+  } else {
+    gemm_kernel<T, AK, BK, 4, 4, 2, 2, false><<<grid, dim3(256), 0, st>>>(g);
+  }
+  return int(hipGetLastError());
+}
+
+template <typename T>
+int launch_gemm_of(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (a_kmajor) return b_kmajor ? launch_layout<T, true, true>(g, aligned, shape, st)
+                                : launch_layout<T, true, false>(g, aligned, shape, st);
+  return b_kmajor ? int(hipErrorInvalidValue) : launch_layout<T, false, false>(g, aligned, shape, st);
+}
+
+}  // namespace ar

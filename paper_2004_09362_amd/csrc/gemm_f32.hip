@@ -1,0 +1,10 @@
+// gemm_f32.hip -- the tiled matrix product (gemm.hpp) for operands of type float.
+#include "gemm.hpp"
+
+namespace ar {
+
+int launch_gemm_f32(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream) {
+  return launch_gemm_of<float>(g, a_kmajor, b_kmajor, aligned, shape, stream);
+}
+
+}  // namespace ar

@@ -1,0 +1,100 @@
+// layers.hpp -- types shared by the C ABI of the layer operators (layers.cpp)
+// and their kernels: the linear layer with its epilogue, its gradient, and
+// dropout from a counter-based generator.
+#pragma once
+
+#include <cstdint>
+
+namespace ar {
+
+// Element types as the kernels see them (ar_dtype without int32).
+enum Elem : int32_t { kF32 = 0, kF16 = 1, kBF16 = 2 };
+enum Act : int32_t { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 };
+
+// Dropout: element (i, j) is kept where its generator word is at most `last`.
+// none = 1 keeps nothing (p = 1).  on = 0: no dropout.
+struct DropArgs {
+  int32_t on, none;
+  uint32_t last, site, k0, k1;
+  float scale;
+  uint64_t row0;
+};
+
+// What follows a product: y = res + drop(act(v + bias)), z = v + bias.
+struct Epilogue {
+  void* y;           // [M, ldy], float where y_f32, else the operands' type
+  const void* bias;  // [N], float where bias_f32, else the operands' type; or NULL
+  const void* res;   // [M, ldr] of y's type, or NULL (y itself: accumulate)
+  void* z;           // [M, ldz] of the operands' type, or NULL
+  int64_t ldy, ldr, ldz;
+  int32_t M, N;
+  int32_t y_f32, bias_f32, act;
+  DropArgs drop;
+};
+
+// One product: v[m][n] = sum over k of a(m, k) b(n, k).  An operand that is
+// "k-major" holds k consecutively (row m, element k at m * lda + k);
+// otherwise its rows are the inner index (row k, element m at k * lda + m).
+struct GemmArgs {
+  const void* a;
+  const void* b;
+  int64_t lda, ldb;
+  int32_t K;
+  int32_t tiles_m, tiles_n;
+  int32_t splits, k_split;  // inner length dealt out: split s takes [s * k_split, min(K, (s + 1) * k_split))
+  float* part;              // splits > 1: partial sums [splits][M][ldp]
+  int64_t ldp;
+  Epilogue e;
+};
+
+enum GemmShape : int32_t { kTile256 = 0, kTile128 = 1 };
+
+// Tile geometry that the host needs: rows and columns of a workgroup's tile,
+// and the bytes of inner length it takes at a time.
+constexpr int32_t kTileKBytes = 128;
+constexpr int32_t tile_rows(int32_t shape) { return shape == kTile256 ? 256 : 128; }
+
+// elem: Elem; a_kmajor / b_kmajor as above (a k-major b with a not is not
+// provided); aligned: whether the asynchronous loads apply (see gemm.hpp).
+int launch_gemm(const GemmArgs& g, int32_t elem, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
+int launch_gemm_f32(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
+int launch_gemm_f16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
+int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
+
+// Products of few rows (both operands k-major): gemm_few.hip.
+constexpr int32_t kFewMaxRows = 64;
+int launch_gemm_few(const GemmArgs& g, int32_t elem, void* stream);
+
+// y of a product whose inner length was split: the parts summed in order,
+// then the epilogue (g.part, g.splits, g.ldp, g.e).
+int launch_gemm_join(const GemmArgs& g, int32_t elem, void* stream);
+
+// y = res + drop(x), element types xe (x) and ye (y, res).
+struct DropCall {
+  const void* x;
+  const void* res;
+  void* y;
+  int64_t ldx, ldr, ldy, rows, cols;
+  DropArgs drop;
+};
+int launch_dropout(const DropCall& c, int32_t xe, int32_t ye, void* stream);
+
+// dz = act'(z) * drop(dy) in dz's type, and the sums of its columns before
+// that rounding: parts [chunks][N] of `rows_per` rows each.
+struct SlopeCall {
+  const void* dy;
+  const void* z;  // NULL without an activation
+  void* dz;       // NULL: sums only
+  float* sums;    // NULL: dz only
+  int64_t lddy, ldz, lddz, M, N;
+  int32_t act;
+  int32_t chunks;
+  int64_t rows_per;
+  DropArgs drop;
+};
+int launch_slope(const SlopeCall& c, int32_t dye, int32_t ze, void* stream);
+
+// db[n] = (accumulate ? db[n] : 0) + sum over chunks of sums[chunk][n]
+int launch_column_sums(const float* sums, int32_t chunks, int64_t N, void* db, int32_t dbe, bool accumulate, void* stream);
+
+}  // namespace ar

@@ -1,0 +1,190 @@
+// rowwise.hip -- the layer operators that read and write each element once:
+// dropout, the gradient through an activation and dropout with its column
+// sums, and the joins of split products and sums.
+//
+// All are bound by memory.  A thread takes 8 consecutive columns of a row (16
+// bytes of halves), at any alignment; 8 columns are two counters of the
+// generator.
+#include "layer_device.hpp"
+
+namespace ar {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Threads along a row: a power of two, as many as 8-column groups, at most a
+// workgroup's.
+int threads_per_row(int64_t cols) {
+  int t = 1;
+  while (t < kThreads && int64_t(t) * 8 < cols) t *= 2;
+  return t;
+}
+
+template <typename X, typename Y>
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, int log_tpr, uint32_t across) {
+  const int tpr = 1 << log_tpr, rpb = kThreads >> log_tpr;
+  const uint32_t down = gridDim.x / across, by = blockIdx.x / across;
+  const int64_t col = (int64_t(blockIdx.x - by * across) * tpr + (threadIdx.x & (tpr - 1))) * 8;
+  if (col >= c.cols) return;
+  const int have = c.cols - col < 8 ? int(c.cols - col) : 8;
+  for (int64_t row = int64_t(by) * rpb + (threadIdx.x >> log_tpr); row < c.rows; row += int64_t(down) * rpb) {
+    float v[8], r[8];
+    load_some<8>(v, static_cast<const X*>(c.x) + row * c.ldx + col, have);
+    load_some<8>(r, static_cast<const Y*>(c.res) + row * c.ldr + col, c.res ? have : 0);
+    if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    store_some<8>(static_cast<Y*>(c.y) + row * c.ldy + col, v, have);
+  }
+}
+
+// A workgroup takes 256 columns (32 threads of 8) of one chunk of rows, 8
+// rows at a time; the sums of its 8 row threads meet in LDS in their order.
+template <typename D, typename Z>
+__global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
+  __shared__ float part[8][32][9];
+  const int ct = threadIdx.x & 31, rt = threadIdx.x >> 5;
+  const int64_t col = (int64_t(blockIdx.x) * 32 + ct) * 8;
+  const int have = c.N - col < 8 ? int(c.N - col > 0 ? c.N - col : 0) : 8;
+  const int64_t r0 = int64_t(blockIdx.y) * c.rows_per;
+  const int64_t r1 = r0 + c.rows_per < c.M ? r0 + c.rows_per : c.M;
+  float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (have > 0) {
+#pragma unroll 2
+    for (int64_t row = r0 + rt; row < r1; row += 8) {
+      float v[8], z[8];
+      load_some<8>(v, static_cast<const D*>(c.dy) + row * c.lddy + col, have);
+      load_some<8>(z, static_cast<const Z*>(c.z) + row * c.ldz + col, c.z ? have : 0);
+      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+      if (c.z) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= act_slope(z[i], c.act);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += i < have ? v[i] : 0.0f;
+      if (c.dz) store_some<8>(static_cast<Z*>(c.dz) + row * c.lddz + col, v, have);
+    }
+  }
+  if (!c.sums) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[rt][ct][i] = s[i];
+  __syncthreads();
+  const int64_t out = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (out < c.N) {
+    float t = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) t += part[r][threadIdx.x >> 3][threadIdx.x & 7];
+    c.sums[int64_t(blockIdx.y) * c.N + out] = t;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void column_sums_kernel(const float* sums, int32_t chunks, int64_t N, T* db,
+                                                               int accumulate) {
+  const int64_t n = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (n >= N) return;
+  float s = accumulate ? float(db[n]) : 0.0f;
+  for (int32_t c = 0; c < chunks; ++c) s += sums[int64_t(c) * N + n];
+  db[n] = T(s);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log_tpr) {
+  const int tpr = 1 << log_tpr, rpb = kThreads >> log_tpr;
+  const int64_t n = (int64_t(blockIdx.y) * tpr + (threadIdx.x & (tpr - 1))) * 8;
+  const int64_t m = int64_t(blockIdx.x) * rpb + (threadIdx.x >> log_tpr);
+  if (n >= g.e.N || m >= g.e.M) return;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8], res[8];
+  load_bias<T, 8>(bias, g.e, int32_t(n));
+  load_residual<T, 8>(res, g.e, int32_t(m), int32_t(n));
+#pragma unroll 4
+  for (int32_t s = 0; s < g.splits; ++s) {
+    const float4* p = reinterpret_cast<const float4*>(g.part + (int64_t(s) * g.e.M + m) * g.ldp + n);
+    const float4 a = p[0], b = p[1];
+    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+    v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+  }
+  emit<T, 8>(v, bias, res, g.e, int32_t(m), int32_t(n));
+}
+
+int log2_of(int v) {
+  int l = 0;
+  while ((1 << l) < v) ++l;
+  return l;
+}
+
+template <typename X>
+int launch_dropout_x(const DropCall& c, int32_t ye, hipStream_t st) {
+  const int tpr = threads_per_row(c.cols), lg = log2_of(tpr), rpb = kThreads / tpr;
+  // workgroups across a row (at most 2^19) times those down the rows, 2^22 or
+  // one pass over the rows at most
+  const int64_t across = (c.cols + int64_t(tpr) * 8 - 1) / (int64_t(tpr) * 8), blocks = (c.rows + rpb - 1) / rpb;
+  const int64_t most = (int64_t(1) << 22) / across > 0 ? (int64_t(1) << 22) / across : 1;
+  const dim3 grid(uint32_t(across * (blocks < most ? blocks : most)));
+  switch (ye) {
+    case kF32: dropout_kernel<X, float><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
+    case kF16: dropout_kernel<X, f16><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
+    case kBF16: dropout_kernel<X, bf16><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
+    default: return int(hipErrorInvalidValue);
+  }
+  return int(hipGetLastError());
+}
+
+template <typename Z>
+int launch_slope_z(const SlopeCall& c, int32_t dye, hipStream_t st) {
+  const dim3 grid(uint32_t((c.N + 255) / 256), uint32_t(c.chunks));
+  if (dye == elem_of<Z>()) slope_kernel<Z, Z><<<grid, dim3(kThreads), 0, st>>>(c);
+  else if (dye == kF32) slope_kernel<float, Z><<<grid, dim3(kThreads), 0, st>>>(c);
+  else return int(hipErrorInvalidValue);
+  return int(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_dropout(const DropCall& c, int32_t xe, int32_t ye, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  switch (xe) {
+    case kF32: return launch_dropout_x<float>(c, ye, st);
+    case kF16: return launch_dropout_x<f16>(c, ye, st);
+    case kBF16: return launch_dropout_x<bf16>(c, ye, st);
+  }
+  return int(hipErrorInvalidValue);
+}
+
+int launch_slope(const SlopeCall& c, int32_t dye, int32_t ze, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  switch (ze) {
+    case kF32: return launch_slope_z<float>(c, dye, st);
+    case kF16: return launch_slope_z<f16>(c, dye, st);
+    case kBF16: return launch_slope_z<bf16>(c, dye, st);
+  }
+  return int(hipErrorInvalidValue);
+}
+
+int launch_column_sums(const float* sums, int32_t chunks, int64_t N, void* db, int32_t dbe, bool accumulate, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const dim3 grid(uint32_t((N + kThreads - 1) / kThreads));
+  switch (dbe) {
+    case kF32: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<float*>(db), accumulate); break;
+    case kF16: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<f16*>(db), accumulate); break;
+    case kBF16: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<bf16*>(db), accumulate); break;
+    default: return int(hipErrorInvalidValue);
+  }
+  return int(hipGetLastError());
+}
+
+int launch_gemm_join(const GemmArgs& g, int32_t elem, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const int tpr = threads_per_row(g.e.N), lg = log2_of(tpr), rpb = kThreads / tpr;
+  const dim3 grid(uint32_t((int64_t(g.e.M) + rpb - 1) / rpb), uint32_t((g.e.N + int64_t(tpr) * 8 - 1) / (int64_t(tpr) * 8)));
+  switch (elem) {
+    case kF32: gemm_join_kernel<float><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
+    case kF16: gemm_join_kernel<f16><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
+    case kBF16: gemm_join_kernel<bf16><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
+    default: return int(hipErrorInvalidValue);
+  }
+  return int(hipGetLastError());
+}
+
+}  // namespace ar
