@@ -62,6 +62,27 @@ __device__ __forceinline__ f32x4v mma(const i32x4v& rows_n, const i32x4v& rows_m
   }
 }
 
+// The same in place, with the sums pinned to accumulation registers: for the
+// wave tile whose 256 sums fill them.  Left to itself the compiler moves such
+// sums between the two halves of the register file in the loop.  It does not
+// know these to be matrix instructions, so the wait states that it would
+// insert are here: 2 after an ordinary instruction wrote an operand (s_nop 1,
+// hidden behind the instruction before), and mma_done() before the sums are
+// read.
+template <typename T>
+__device__ __forceinline__ void mma_pinned(const i32x4v& rows_n, const i32x4v& rows_m, f32x4v& acc) {
+  if constexpr (elem_of<T>() == kBF16) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
+  } else if constexpr (elem_of<T>() == kF16) {
+    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      asm volatile("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n[e]), "v"(rows_m[e]));
+  }
+}
+__device__ __forceinline__ void mma_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+
 // 16 bytes of a row, elements past `have` zero.
 template <typename T>
 __device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have) {
@@ -258,6 +279,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   using OpB = Operand<T, BK, true, TN, THREADS>;
   constexpr int kBuf = OpA::kBytes + OpB::kBytes;
   constexpr int kInner = OpA::kInner;
+  constexpr bool kPinned = MT * NT == 64;
   __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -307,35 +329,49 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
     // while slice 0 of the next tile is; the tile after that is on its way
     // from the moment that every wave has read the whole of this one.
     i32x4v fa[2][MT], fb[2][NT];
+    // row i of the wave tile's products of slice s
+    auto products = [&](int s, int i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
+        else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
+      }
+    };
+    auto read_slice = [&](int s, int32_t t) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) fb[s][j] = rb.read(buf_b(t), j, s);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) fa[s][i] = ra.read(buf_a(t), i, s);
+    };
     issue(0);
     wait_all();
     issue(1);
+    read_slice(0, 0);
+    const int32_t whole = klen / kInner;
+    int32_t t = 0;
+    for (; t + 2 < whole; ++t) {
+      read_slice(1, t);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) fa[0][i] = ra.read(buf_a(0), i, 0);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) fb[0][j] = rb.read(buf_b(0), j, 0);
-    for (int32_t t = 0; t < tiles; ++t) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) fa[1][i] = ra.read(buf_a(t), i, 1);
-#pragma unroll
-      for (int j = 0; j < NT; ++j) fb[1][j] = rb.read(buf_b(t), j, 1);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[0][j], fa[0][i], acc[i][j]);
+      for (int i = 0; i < MT; ++i) products(0, i);
       wait_all();
-      issue(t + 2);
-      if (t + 1 < tiles) {
+      const uint32_t to = lds0 + (t & 1) * kBuf;
+      a.template issue<0, OpA::kSlots>(t + 2, to, wave);
+      b.template issue<0, OpB::kSlots>(t + 2, to + OpA::kBytes, wave);
+      read_slice(0, t + 1);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fa[0][i] = ra.read(buf_a(t + 1), i, 0);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) fb[0][j] = rb.read(buf_b(t + 1), j, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[1][j], fa[1][i], acc[i][j]);
+      for (int i = 0; i < MT; ++i) products(1, i);
     }
+    for (; t < tiles; ++t) {  // the last two, and one that is not whole
+      read_slice(1, t);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) products(0, i);
+      wait_all();
+      if (t + 2 < tiles) stage(t + 2);
+      if (t + 1 < tiles) read_slice(0, t + 1);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) products(1, i);
+    }
+    if constexpr (kPinned) mma_done();
   } else {
     stage(0);
     wait_all();
@@ -399,31 +435,45 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     const int32_t mw = m0 + (wm * MT + round * kTilesRound) * 16 + lane / kUnits;
-    for (int pass = 0; pass < kPasses; pass += kAhead) {
-      float v[kAhead][8], res[kAhead][8];
+    auto unit_at = [&](int r) { return share + (r * kUnits + (unit ^ (r & (kUnits - 1)))) * 32; };
+    if (have >= 8) {
+      for (int pass = 0; pass < kPasses; pass += kAhead) {
+        float v[kAhead][8], res[kAhead][8];
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const int r = (pass + q) * kPassRows + lane / kUnits;
-        const f32x4v* w = reinterpret_cast<const f32x4v*>(share + (r * kUnits + (unit ^ (r & (kUnits - 1)))) * 32);
-        const f32x4v x = w[0], y = w[1];
+        for (int q = 0; q < kAhead; ++q) {
+          const f32x4v* w = reinterpret_cast<const f32x4v*>(unit_at((pass + q) * kPassRows + lane / kUnits));
+          const f32x4v x = w[0], y = w[1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[q][e] = x[e];
-          v[q][4 + e] = y[e];
+          for (int e = 0; e < 4; ++e) {
+            v[q][e] = x[e];
+            v[q][4 + e] = y[e];
+          }
+          const int32_t m = mw + (pass + q) * kPassRows;
+          if (g.splits == 1 && m < g.e.M) load_residual<T, 8>(res[q], g.e, m, n);
         }
-        const int32_t m = mw + (pass + q) * kPassRows;
-        if (g.splits == 1 && m < g.e.M) load_residual<T, 8>(res[q], g.e, m, n);
-      }
 #pragma unroll
-      for (int q = 0; q < kAhead; ++q) {
-        const int32_t m = mw + (pass + q) * kPassRows;
-        if (m >= g.e.M || have <= 0) continue;
-        if (g.splits > 1) {
-          f32x4v* w = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
-          w[0] = f32x4v{v[q][0], v[q][1], v[q][2], v[q][3]};
-          w[1] = f32x4v{v[q][4], v[q][5], v[q][6], v[q][7]};
-        } else {
-          emit<T, 8>(v[q], bias, res[q], g.e, m, n);
+        for (int q = 0; q < kAhead; ++q) {
+          const int32_t m = mw + (pass + q) * kPassRows;
+          if (m >= g.e.M) continue;
+          if (g.splits > 1) {
+            f32x4v* w = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
+            w[0] = f32x4v{v[q][0], v[q][1], v[q][2], v[q][3]};
+            w[1] = f32x4v{v[q][4], v[q][5], v[q][6], v[q][7]};
+          } else {
+            emit<T, 8>(v[q], bias, res[q], g.e, m, n);
+          }
+        }
+      }
+    } else {  // the lanes of a row's last, partial unit
+#pragma unroll 1
+      for (int pass = 0; pass < kPasses; ++pass) {
+        const int32_t m = mw + pass * kPassRows;
+        if (m >= g.e.M) break;
+        const float* w = reinterpret_cast<const float*>(unit_at(pass * kPassRows + lane / kUnits));
+#pragma unroll 1
+        for (int i = 0; i < have; ++i) {
+          if (g.splits > 1) part[int64_t(m) * g.ldp + i] = w[i];
+          else emit_one<T>(w[i], g.e, m, n + i);
         }
       }
     }

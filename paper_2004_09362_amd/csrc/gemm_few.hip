@@ -91,6 +91,10 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
     for (int w = 1; w < kWaves; ++w) v += sums[w][tile][l];
     if (g.splits > 1) {
       *reinterpret_cast<f32x4v*>(g.part + (int64_t(blockIdx.y) * g.e.M + m) * g.ldp + n) = v;
+    } else if (g.e.N - n < 4) {
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        if (n + c < g.e.N) emit_one<T>(v[c], g.e, m, n + c);
     } else {
       float x[4] = {v[0], v[1], v[2], v[3]}, bias[4], res[4];
       load_bias<T, 4>(bias, g.e, n);

@@ -88,6 +88,14 @@ __device__ __forceinline__ void drop_some(float (&x)[V], const DropArgs& d, uint
   }
 }
 
+// drop() of one element.
+__device__ __forceinline__ float drop_one(float x, const DropArgs& d, uint64_t row, uint32_t col) {
+  if (d.none) return 0.0f;
+  const uint4 w = counter_words(col >> 2, uint32_t(row), uint32_t(row >> 32), d.site, d.k0, d.k1);
+  const uint32_t word = col & 2 ? (col & 1 ? w.w : w.z) : (col & 1 ? w.y : w.x);
+  return word <= d.last ? x * d.scale : 0.0f;
+}
+
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kGeluTanh2 = 1.5957691216057308f;      // 2 sqrt(2 / pi)
@@ -123,31 +131,42 @@ __device__ __forceinline__ float act_slope(float z, int act) {
   }
 }
 
-// The bias of V columns from n on (zeros without one, or past N).
+// The bias of V columns from n on (zeros without one, or where the row ends
+// before the last).
 template <typename T, int V>
 __device__ __forceinline__ void load_bias(float (&b)[V], const Epilogue& e, int32_t n) {
-  const int have = e.bias ? e.N - n : 0;
-  if (e.bias_f32) load_some<V>(b, static_cast<const float*>(e.bias) + n, have);
-  else load_some<V>(b, static_cast<const T*>(e.bias) + n, have);
+  if (!e.bias || e.N - n < V) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = 0.0f;
+  } else if (e.bias_f32) {
+    load_some<V>(b, static_cast<const float*>(e.bias) + n, V);
+  } else {
+    load_some<V>(b, static_cast<const T*>(e.bias) + n, V);
+  }
 }
 
-// The residual of V columns from n on of row m < M (zeros without one).
+// The residual of V columns from n on, all within the row, of row m (zeros
+// without one).
 template <typename T, int V>
 __device__ __forceinline__ void load_residual(float (&r)[V], const Epilogue& e, int32_t m, int32_t n) {
-  const int have = e.res ? e.N - n : 0;
-  if (e.y_f32) load_some<V>(r, static_cast<const float*>(e.res) + int64_t(m) * e.ldr + n, have);
-  else load_some<V>(r, static_cast<const T*>(e.res) + int64_t(m) * e.ldr + n, have);
+  if (!e.res) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) r[i] = 0.0f;
+  } else if (e.y_f32) {
+    load_some<V>(r, static_cast<const float*>(e.res) + int64_t(m) * e.ldr + n, V);
+  } else {
+    load_some<V>(r, static_cast<const T*>(e.res) + int64_t(m) * e.ldr + n, V);
+  }
 }
 
-// The epilogue of V (4 or 8) columns from n < N on (n a multiple of V) of row
-// m < M; v holds the product's sums.
+// The epilogue of V (4 or 8) columns from n on (a multiple of V), all within
+// the row, of row m; v holds the product's sums.
 template <typename T, int V>
 __device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const float (&r)[V], const Epilogue& e,
                                      int32_t m, int32_t n) {
-  const int have = e.N - n;
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] += b[i];
-  if (e.z) store_some<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, have);
+  if (e.z) store_some<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, V);
   if (e.act != kActNone) {
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = act_value(v[i], e.act);
@@ -155,8 +174,25 @@ __device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const f
   if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] += r[i];
-  if (e.y_f32) store_some<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, have);
-  else store_some<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, have);
+  if (e.y_f32) store_some<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, V);
+  else store_some<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, V);
+}
+
+// The same for one element, where a row ends inside a group of columns.
+template <typename T>
+__device__ __forceinline__ void emit_one(float v, const Epilogue& e, int32_t m, int32_t n) {
+  if (e.bias) v += e.bias_f32 ? static_cast<const float*>(e.bias)[n] : float(static_cast<const T*>(e.bias)[n]);
+  if (e.z) static_cast<T*>(e.z)[int64_t(m) * e.ldz + n] = T(v);
+  v = act_value(v, e.act);
+  if (e.drop.on) v = drop_one(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
+  const int64_t ry = int64_t(m) * e.ldr + n, yy = int64_t(m) * e.ldy + n;
+  if (e.y_f32) {
+    if (e.res) v += static_cast<const float*>(e.res)[ry];
+    static_cast<float*>(e.y)[yy] = v;
+  } else {
+    if (e.res) v += float(static_cast<const T*>(e.res)[ry]);
+    static_cast<T*>(e.y)[yy] = T(v);
+  }
 }
 
 }  // namespace ar

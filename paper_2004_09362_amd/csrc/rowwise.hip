@@ -95,12 +95,22 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log
   const int64_t n = (int64_t(blockIdx.y) * tpr + (threadIdx.x & (tpr - 1))) * 8;
   const int64_t m = int64_t(blockIdx.x) * rpb + (threadIdx.x >> log_tpr);
   if (n >= g.e.N || m >= g.e.M) return;
+  const float* part = g.part + m * g.ldp + n;
+  const int64_t step = int64_t(g.e.M) * g.ldp;
+  if (g.e.N - n < 8) {
+    for (int i = 0; i < int(g.e.N - n); ++i) {
+      float v = 0.0f;
+      for (int32_t s = 0; s < g.splits; ++s) v += part[s * step + i];
+      emit_one<T>(v, g.e, int32_t(m), int32_t(n) + i);
+    }
+    return;
+  }
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8], res[8];
   load_bias<T, 8>(bias, g.e, int32_t(n));
   load_residual<T, 8>(res, g.e, int32_t(m), int32_t(n));
 #pragma unroll 4
   for (int32_t s = 0; s < g.splits; ++s) {
-    const float4* p = reinterpret_cast<const float4*>(g.part + (int64_t(s) * g.e.M + m) * g.ldp + n);
+    const float4* p = reinterpret_cast<const float4*>(part + s * step);
     const float4 a = p[0], b = p[1];
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
     v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
