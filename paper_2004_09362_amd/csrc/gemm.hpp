@@ -66,21 +66,23 @@ __device__ __forceinline__ f32x4v mma(const i32x4v& rows_n, const i32x4v& rows_m
 // wave tile whose 256 sums fill them.  Left to itself the compiler moves such
 // sums between the two halves of the register file in the loop.  It does not
 // know these to be matrix instructions, so the wait states that it would
-// insert are here: 2 after an ordinary instruction wrote an operand (s_nop 1,
-// hidden behind the instruction before), and mma_done() before the sums are
-// read.
+// insert are the caller's: mma_ready() after ordinary instructions may have
+// written an operand (in the loops none does: fragments come from LDS, and
+// tests/test_gemm_code.py looks at what was compiled), mma_done() before the
+// sums are read.
 template <typename T>
 __device__ __forceinline__ void mma_pinned(const i32x4v& rows_n, const i32x4v& rows_m, f32x4v& acc) {
   if constexpr (elem_of<T>() == kBF16) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
   } else if constexpr (elem_of<T>() == kF16) {
-    asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      asm volatile("s_nop 1\n\tv_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n[e]), "v"(rows_m[e]));
+      asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n[e]), "v"(rows_m[e]));
   }
 }
+__device__ __forceinline__ void mma_ready() { asm volatile("s_nop 1"); }
 __device__ __forceinline__ void mma_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // 16 bytes of a row, elements past `have` zero.
@@ -110,8 +112,7 @@ __device__ __forceinline__ uint32_t lds_offset(const char* p) {
 // later LDS read wait for it; here the caller waits (wait_all), one tile
 // later.  It has no register outputs, and nothing else here uses m0.
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base)
-               : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base));
 }
 
 // All of this wave's loads have arrived, its LDS reads and writes are done,
@@ -169,12 +170,10 @@ struct Operand {
     return base + (KMAJOR ? int64_t(t) * kTileKBytes : int64_t(t) * kInner * ld);
   }
 
-  // Starts the asynchronous loads of whole tile t into LDS.
-  template <int I0, int I1>
-  __device__ __forceinline__ void issue(int32_t t, uint32_t lds, int wave) const {
-    const char* p = at(t);
-#pragma unroll
-    for (int i = I0; i < I1; ++i) load_to_lds(p, voff[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
+  // Starts the asynchronous load of this thread's chunk i of a whole tile (p:
+  // its start) into LDS.
+  __device__ __forceinline__ void issue(const char* p, int i, uint32_t lds, int wave) const {
+    load_to_lds(p, voff[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
   }
 
   // This thread's chunk i of tile t, of which k_have inner indices exist.
@@ -319,8 +318,10 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
     const uint32_t lds0 = lds_offset(lds);
     auto issue = [&](int32_t t) {
       if ((t + 1) * kInner <= klen) {
-        a.template issue<0, OpA::kSlots>(t, lds0 + (t & 1) * kBuf, wave);
-        b.template issue<0, OpB::kSlots>(t, lds0 + (t & 1) * kBuf + OpA::kBytes, wave);
+#pragma unroll
+        for (int i = 0; i < OpA::kSlots; ++i) a.issue(a.at(t), i, lds0 + (t & 1) * kBuf, wave);
+#pragma unroll
+        for (int i = 0; i < OpB::kSlots; ++i) b.issue(b.at(t), i, lds0 + (t & 1) * kBuf + OpA::kBytes, wave);
       } else if (t < tiles) {
         stage(t);
       }
@@ -331,45 +332,59 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
     i32x4v fa[2][MT], fb[2][NT];
     // row i of the wave tile's products of slice s
     auto products = [&](int s, int i) {
+      if constexpr (kPinned) mma_ready();
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
         else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
       }
     };
-    auto read_slice = [&](int s, int32_t t) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) fb[s][j] = rb.read(buf_b(t), j, s);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) fa[s][i] = ra.read(buf_a(t), i, s);
+    // fragment i of each operand
+    auto read = [&](int s, int32_t t, int i) {
+      fb[s][i] = rb.read(buf_b(t), i, s);
+      fa[s][i] = ra.read(buf_a(t), i, s);
     };
+    static_assert(MT == NT && OpA::kSlots == MT && OpB::kSlots == NT, "a row's products go with one read and one load each");
     issue(0);
     wait_all();
     issue(1);
-    read_slice(0, 0);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) read(0, 0, i);
     const int32_t whole = klen / kInner;
     int32_t t = 0;
     for (; t + 2 < whole; ++t) {
-      read_slice(1, t);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) products(0, i);
+      for (int i = 0; i < MT; ++i) {
+        read(1, t, i);
+        products(0, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       wait_all();
       const uint32_t to = lds0 + (t & 1) * kBuf;
-      a.template issue<0, OpA::kSlots>(t + 2, to, wave);
-      b.template issue<0, OpB::kSlots>(t + 2, to + OpA::kBytes, wave);
-      read_slice(0, t + 1);
+      const char* pa = a.at(t + 2);
+      const char* pb = b.at(t + 2);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) products(1, i);
+      for (int i = 0; i < MT; ++i) {
+        read(0, t + 1, i);
+        a.issue(pa, i, to, wave);
+        b.issue(pb, i, to + OpA::kBytes, wave);
+        products(1, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     for (; t < tiles; ++t) {  // the last two, and one that is not whole
-      read_slice(1, t);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) products(0, i);
+      for (int i = 0; i < MT; ++i) {
+        read(1, t, i);
+        products(0, i);
+      }
       wait_all();
       if (t + 2 < tiles) stage(t + 2);
-      if (t + 1 < tiles) read_slice(0, t + 1);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) products(1, i);
+      for (int i = 0; i < MT; ++i) {
+        if (t + 1 < tiles) read(0, t + 1, i);
+        products(1, i);
+      }
     }
     if constexpr (kPinned) mma_done();
   } else {
