@@ -32,6 +32,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <utility>
 
 #include "layer_device.hpp"
 
@@ -101,7 +102,11 @@ __device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have) {
   return __builtin_bit_cast(i32x4v, w);
 }
 
-using LdsPtr = __attribute__((address_space(3))) char*;
+// f(0), f(1), ... f(N - 1) with the index a constant in each.
+template <typename F, int... I>
+__device__ __forceinline__ void unrolled(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
 
 __device__ __forceinline__ uint32_t lds_offset(const char* p) {
   return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)p));
@@ -111,14 +116,17 @@ __device__ __forceinline__ uint32_t lds_offset(const char* p) {
 // the registers.  The compiler's own form of this instruction makes every
 // later LDS read wait for it; here the caller waits (wait_all), one tile
 // later.  It has no register outputs, and nothing else here uses m0.
-__device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(base));
+// lds_target() names the place, one instruction at least before.
+__device__ __forceinline__ void lds_target(uint32_t lds) { asm volatile("s_mov_b32 m0, %0" ::"s"(lds)); }
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff) {
+  asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base));
 }
 
 // All of this wave's loads have arrived, its LDS reads and writes are done,
 // and so are those of the workgroup's other waves.
 __device__ __forceinline__ void wait_all() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -165,16 +173,19 @@ struct Operand {
     }
   }
 
+  // Bytes from an inner tile to the next.
+  __device__ __forceinline__ int64_t step() const { return KMAJOR ? int64_t(kTileKBytes) : kInner * ld; }
   // The start of inner tile t.
   __device__ __forceinline__ const char* at(int32_t t) const {
-    return base + (KMAJOR ? int64_t(t) * kTileKBytes : int64_t(t) * kInner * ld);
+    return base + t * step();
   }
 
-  // Starts the asynchronous load of this thread's chunk i of a whole tile (p:
-  // its start) into LDS.
-  __device__ __forceinline__ void issue(const char* p, int i, uint32_t lds, int wave) const {
-    load_to_lds(p, voff[i], lds + uint32_t(i * THREADS + wave * 64) * 16);
+  // The asynchronous load of this thread's chunk i of a whole tile (p: its
+  // start) into LDS: its target, and then the load itself.
+  __device__ __forceinline__ void aim(int i, uint32_t lds, int wave) const {
+    lds_target(lds + uint32_t(i * THREADS + wave * 64) * 16);
   }
+  __device__ __forceinline__ void issue(const char* p, int i) const { load_to_lds(p, voff[i]); }
 
   // This thread's chunk i of tile t, of which k_have inner indices exist.
   __device__ __forceinline__ i32x4v chunk(int i, int32_t t, int64_t k_have, int tid) const {
@@ -315,76 +326,89 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   };
 
   if constexpr (ASYNC) {
+    // Slice 0 of a tile is multiplied while slice 1 is read, and slice 1
+    // while slice 0 of the next tile is; the tile after that is on its way
+    // from the moment that every wave has read the whole of this one.
     const uint32_t lds0 = lds_offset(lds);
-    auto issue = [&](int32_t t) {
+    i32x4v fa[2][MT], fb[2][NT];
+    constexpr int kReads = MT + NT, kLoads = OpA::kSlots + OpB::kSlots, kProducts = MT * NT;
+    // fragment x of slice s, first those of b
+    auto read = [&](int s, int32_t t, int x) {
+      if (x < NT) fb[s][x] = rb.read(buf_b(t), x, s);
+      else fa[s][x - NT] = ra.read(buf_a(t), x - NT, s);
+    };
+    // chunk x of a tile, first those of a: its target and its load
+    auto aim = [&](uint32_t to, int x) {
+      if (x < OpA::kSlots) a.aim(x, to, wave);
+      else b.aim(x - OpA::kSlots, to + OpA::kBytes, wave);
+    };
+    auto load = [&](const char* pa, const char* pb, int x) {
+      if (x < OpA::kSlots) a.issue(pa, x);
+      else b.issue(pb, x - OpA::kSlots);
+    };
+    auto product = [&](int s, int x) {
+      const int i = x / NT, j = x % NT;
+      if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
+      else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
+    };
+    auto start = [&](int32_t t) {
       if ((t + 1) * kInner <= klen) {
 #pragma unroll
-        for (int i = 0; i < OpA::kSlots; ++i) a.issue(a.at(t), i, lds0 + (t & 1) * kBuf, wave);
-#pragma unroll
-        for (int i = 0; i < OpB::kSlots; ++i) b.issue(b.at(t), i, lds0 + (t & 1) * kBuf + OpA::kBytes, wave);
+        for (int x = 0; x < kLoads; ++x) {
+          aim(lds0 + (t & 1) * kBuf, x);
+          asm volatile("s_nop 0");
+          load(a.at(t), b.at(t), x);
+        }
       } else if (t < tiles) {
         stage(t);
       }
     };
-    // Slice 0 of a tile is multiplied while slice 1 is read, and slice 1
-    // while slice 0 of the next tile is; the tile after that is on its way
-    // from the moment that every wave has read the whole of this one.
-    i32x4v fa[2][MT], fb[2][NT];
-    // row i of the wave tile's products of slice s
-    auto products = [&](int s, int i) {
-      if constexpr (kPinned) mma_ready();
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
-        else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
-      }
-    };
-    // fragment i of each operand
-    auto read = [&](int s, int32_t t, int i) {
-      fb[s][i] = rb.read(buf_b(t), i, s);
-      fa[s][i] = ra.read(buf_a(t), i, s);
-    };
-    static_assert(MT == NT && OpA::kSlots == MT && OpB::kSlots == NT, "a row's products go with one read and one load each");
-    issue(0);
+    start(0);
     wait_all();
-    issue(1);
+    start(1);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) read(0, 0, i);
+    for (int x = 0; x < kReads; ++x) read(0, 0, x);
     const int32_t whole = klen / kInner;
     int32_t t = 0;
+    // The instruction stream of a tile: between two matrix instructions goes
+    // at most one other of each kind, so that the matrix unit always has its
+    // next one.  Slice 1 is read within the first half of slice 0's products;
+    // after kMeet of them the waves meet, and the loads start.
+    constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kLoadGap = kProducts >= 64 ? 3 : 2, kReadGap1 = kProducts * 3 / 4 / kReads;
+    static_assert(kReadGap >= 1 && kMeet + kLoads * kLoadGap <= 2 * kProducts, "everything within a tile");
+    const char* pa = a.at(2);
+    const char* pb = b.at(2);
     for (; t + 2 < whole; ++t) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        read(1, t, i);
-        products(0, i);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      wait_all();
       const uint32_t to = lds0 + (t & 1) * kBuf;
-      const char* pa = a.at(t + 2);
-      const char* pb = b.at(t + 2);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        read(0, t + 1, i);
-        a.issue(pa, i, to, wave);
-        b.issue(pb, i, to + OpA::kBytes, wave);
-        products(1, i);
+      if constexpr (kPinned) mma_ready();
+      unrolled([&](auto index) {
+        constexpr int x = decltype(index)::value, y = x - kProducts, z = x - kMeet;
+        if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, t, x / kReadGap);
+        if constexpr (x == kMeet) wait_all();
+        if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, t + 1, y / kReadGap1);
+        if constexpr (z >= 0 && z / kLoadGap < kLoads && z % kLoadGap == 0) aim(to, z / kLoadGap);
+        if constexpr (z >= 0 && z / kLoadGap < kLoads && z % kLoadGap == kLoadGap - 1) load(pa, pb, z / kLoadGap);
+        product(x / kProducts, x % kProducts);
         __builtin_amdgcn_sched_barrier(0);
-      }
+      }, std::make_integer_sequence<int, 2 * kProducts>{});
+      pa += a.step();
+      pb += b.step();
     }
     for (; t < tiles; ++t) {  // the last two, and one that is not whole
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        read(1, t, i);
-        products(0, i);
-      }
+      for (int x = 0; x < kReads; ++x) read(1, t, x);
+      if constexpr (kPinned) mma_ready();
+#pragma unroll
+      for (int x = 0; x < kProducts; ++x) product(0, x);
       wait_all();
       if (t + 2 < tiles) stage(t + 2);
+      if (t + 1 < tiles) {
 #pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        if (t + 1 < tiles) read(0, t + 1, i);
-        products(1, i);
+        for (int x = 0; x < kReads; ++x) read(0, t + 1, x);
       }
+      if constexpr (kPinned) mma_ready();
+#pragma unroll
+      for (int x = 0; x < kProducts; ++x) product(1, x);
     }
     if constexpr (kPinned) mma_done();
   } else {
