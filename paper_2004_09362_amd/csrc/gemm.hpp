@@ -8,8 +8,8 @@
 // operand and a's as their second, so that a lane's sums are consecutive
 // columns n of one row m and leave in 16-byte pieces.
 //
-// Inner lengths of 128 bytes at a time are staged in LDS, two buffers, every
-// operand in the order that it has in memory:
+// Inner lengths of 128 bytes at a time (a tile: 64 halves or 32 floats) are
+// staged in LDS, every operand in the order that it has in memory:
 //   k-major:  one row m (or n) is 128 bytes, 8 chunks of 16; a fragment is one
 //             16-byte read (8 halves for one 16x16x32 instruction, 4 floats
 //             for four 16x16x4);
@@ -122,11 +122,13 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff) {
   asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base));
 }
 
-// All of this wave's loads have arrived, its LDS reads and writes are done,
-// and so are those of the workgroup's other waves.
+// All but the last LOADS of this wave's loads have arrived, its LDS reads and
+// writes are done, and so it is with the workgroup's other waves.
+template <int LOADS>
 __device__ __forceinline__ void wait_all() {
+  static_assert(LOADS < 64, "the counter's range");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x70);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt((LOADS & 15) | ((LOADS >> 4) << 14) | 0x70);  // vmcnt(LOADS) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -287,10 +289,12 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   constexpr int THREADS = WM * WN * 64, TM = WM * MT * 16, TN = WN * NT * 16;
   using OpA = Operand<T, AK, false, TM, THREADS>;
   using OpB = Operand<T, BK, true, TN, THREADS>;
-  constexpr int kBuf = OpA::kBytes + OpB::kBytes;
+  // LDS: five places, each for one operand of a tile
+  constexpr uint32_t kPlace = OpA::kBytes, kRing = 5 * kPlace;
+  static_assert(OpB::kBytes == kPlace, "places of one size");
   constexpr int kInner = OpA::kInner;
   constexpr bool kPinned = MT * NT == 64;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];
+  __shared__ __attribute__((aligned(1024))) char lds[kRing];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
@@ -316,127 +320,136 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
 
   const int32_t tiles = (klen + kInner - 1) / kInner;
-  auto buf_a = [&](int t) { return lds + (t & 1) * kBuf; };
-  auto buf_b = [&](int t) { return lds + (t & 1) * kBuf + OpA::kBytes; };
-  // a tile through registers: its last, partial one, and every one where the
-  // operands' alignment rules the asynchronous loads out
-  auto stage = [&](int32_t t) {
-    a.copy(t, klen - int64_t(t) * kInner, buf_a(t), tid);
-    b.copy(t, klen - int64_t(t) * kInner, buf_b(t), tid);
-  };
-
   if constexpr (ASYNC) {
-    // Slice 0 of a tile is multiplied while slice 1 is read, and slice 1
-    // while slice 0 of the next tile is; the tile after that is on its way
-    // from the moment that every wave has read the whole of this one.
+    // Operands take the five places in turn: a of tile 0, b of tile 0, a of
+    // tile 1, and so on.  Slice 0 of tile t is multiplied while slice 1 is
+    // read, and slice 1 while slice 0 of tile t + 1 is.  Once every wave has
+    // read the whole of tile t, b of t + 2 is loaded to where a of t lay, and
+    // then a of t + 3 to where b of t lay; the waves' next meeting waits for
+    // all but the latter.
     const uint32_t lds0 = lds_offset(lds);
     i32x4v fa[2][MT], fb[2][NT];
-    constexpr int kReads = MT + NT, kLoads = OpA::kSlots + OpB::kSlots, kProducts = MT * NT;
+    constexpr int kReads = MT + NT, kProducts = MT * NT, kLoadsA = OpA::kSlots, kLoadsB = OpB::kSlots;
+    auto after = [](uint32_t place) { return place == kRing - kPlace ? 0 : place + kPlace; };
     // fragment x of slice s, first those of b
-    auto read = [&](int s, int32_t t, int x) {
-      if (x < NT) fb[s][x] = rb.read(buf_b(t), x, s);
-      else fa[s][x - NT] = ra.read(buf_a(t), x - NT, s);
-    };
-    // chunk x of a tile, first those of a: its target and its load
-    auto aim = [&](uint32_t to, int x) {
-      if (x < OpA::kSlots) a.aim(x, to, wave);
-      else b.aim(x - OpA::kSlots, to + OpA::kBytes, wave);
-    };
-    auto load = [&](const char* pa, const char* pb, int x) {
-      if (x < OpA::kSlots) a.issue(pa, x);
-      else b.issue(pb, x - OpA::kSlots);
+    auto read = [&](int s, uint32_t at_a, uint32_t at_b, int x) {
+      if (x < NT) fb[s][x] = rb.read(lds + at_b, x, s);
+      else fa[s][x - NT] = ra.read(lds + at_a, x - NT, s);
     };
     auto product = [&](int s, int x) {
       const int i = x / NT, j = x % NT;
       if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
       else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
     };
-    auto start = [&](int32_t t) {
-      if ((t + 1) * kInner <= klen) {
+    // all of an operand's tile t, through registers where it is not whole
+    const int32_t whole = klen / kInner;
+    auto start = [&](const auto& op, int32_t t, uint32_t at) {
+      if (t < whole) {
 #pragma unroll
-        for (int x = 0; x < kLoads; ++x) {
-          aim(lds0 + (t & 1) * kBuf, x);
+        for (int x = 0; x < kLoadsA; ++x) {
+          op.aim(x, lds0 + at, wave);
           asm volatile("s_nop 0");
-          load(a.at(t), b.at(t), x);
+          op.issue(op.at(t), x);
         }
       } else if (t < tiles) {
-        stage(t);
+        op.copy(t, klen - int64_t(t) * kInner, lds + at, tid);
       }
     };
-    start(0);
-    wait_all();
-    start(1);
+    static_assert(kLoadsA == kLoadsB, "operands of one size");
+    start(a, 0, 0);
+    start(b, 0, kPlace);
+    start(a, 1, 2 * kPlace);
+    start(b, 1, 3 * kPlace);
+    start(a, 2, 4 * kPlace);
+    if (whole > 2) wait_all<3 * kLoadsA>();
+    else wait_all<0>();
+    uint32_t at_a = 0, at_b = kPlace;
 #pragma unroll
-    for (int x = 0; x < kReads; ++x) read(0, 0, x);
-    const int32_t whole = klen / kInner;
+    for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
     int32_t t = 0;
     // The instruction stream of a tile: between two matrix instructions goes
     // at most one other of each kind, so that the matrix unit always has its
-    // next one.  Slice 1 is read within the first half of slice 0's products;
-    // after kMeet of them the waves meet, and the loads start.
-    constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kLoadGap = kProducts >= 64 ? 3 : 2, kReadGap1 = kProducts * 3 / 4 / kReads;
-    static_assert(kReadGap >= 1 && kMeet + kLoads * kLoadGap <= 2 * kProducts, "everything within a tile");
-    const char* pa = a.at(2);
+    // next one, and the loads are spread, since each keeps the address unit
+    // busy for 16 cycles.  Slice 1 is read within the first half of slice 0's
+    // products; after kMeet of them the waves meet.
+    constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
+    constexpr int kGapB = kProducts >= 64 ? 5 : 2, kGapA = kProducts >= 64 ? 6 : 3, kMeetA = kMeet + kGapB * kLoadsB;
+    static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA <= 2 * kProducts, "everything within a tile");
     const char* pb = b.at(2);
-    for (; t + 2 < whole; ++t) {
-      const uint32_t to = lds0 + (t & 1) * kBuf;
+    const char* pa = a.at(3);
+    for (; t + 3 < whole; ++t) {
+      const uint32_t next_a = after(at_b), next_b = after(next_a);
       if constexpr (kPinned) mma_ready();
       unrolled([&](auto index) {
-        constexpr int x = decltype(index)::value, y = x - kProducts, z = x - kMeet;
-        if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, t, x / kReadGap);
-        if constexpr (x == kMeet) wait_all();
-        if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, t + 1, y / kReadGap1);
-        if constexpr (z >= 0 && z / kLoadGap < kLoads && z % kLoadGap == 0) aim(to, z / kLoadGap);
-        if constexpr (z >= 0 && z / kLoadGap < kLoads && z % kLoadGap == kLoadGap - 1) load(pa, pb, z / kLoadGap);
+        constexpr int x = decltype(index)::value, y = x - kProducts, zb = x - kMeet, za = x - kMeetA;
+        if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, at_a, at_b, x / kReadGap);
+        if constexpr (x == kMeet) wait_all<kLoadsA>();
+        if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, next_a, next_b, y / kReadGap1);
+        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
+        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(pb, zb / kGapB);
+        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
+        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(pa, za / kGapA);
         product(x / kProducts, x % kProducts);
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, 2 * kProducts>{});
       pa += a.step();
       pb += b.step();
+      at_a = next_a;
+      at_b = next_b;
     }
-    for (; t < tiles; ++t) {  // the last two, and one that is not whole
+    for (; t < tiles; ++t) {  // the last ones
+      const uint32_t next_a = after(at_b), next_b = after(next_a);
 #pragma unroll
-      for (int x = 0; x < kReads; ++x) read(1, t, x);
+      for (int x = 0; x < kReads; ++x) read(1, at_a, at_b, x);
       if constexpr (kPinned) mma_ready();
 #pragma unroll
       for (int x = 0; x < kProducts; ++x) product(0, x);
-      wait_all();
-      if (t + 2 < tiles) stage(t + 2);
+      wait_all<0>();
+      start(b, t + 2, at_a);
+      start(a, t + 3, at_b);
       if (t + 1 < tiles) {
 #pragma unroll
-        for (int x = 0; x < kReads; ++x) read(0, t + 1, x);
+        for (int x = 0; x < kReads; ++x) read(0, next_a, next_b, x);
       }
       if constexpr (kPinned) mma_ready();
 #pragma unroll
       for (int x = 0; x < kProducts; ++x) product(1, x);
+      at_a = next_a;
+      at_b = next_b;
     }
     if constexpr (kPinned) mma_done();
   } else {
-    stage(0);
-    wait_all();
+    // a tile at a time through registers, which the next one is loaded into
+    // while it is multiplied
+    i32x4v xa[OpA::kSlots], xb[OpB::kSlots];
+    auto fetch = [&](int32_t t) {
+      a.load(xa, t, klen - int64_t(t) * kInner, tid);
+      b.load(xb, t, klen - int64_t(t) * kInner, tid);
+    };
+    auto place = [&](int32_t t) {
+      a.store(xa, lds + (t & 1) * 2 * kPlace, tid);
+      b.store(xb, lds + (t & 1) * 2 * kPlace + kPlace, tid);
+    };
+    fetch(0);
+    place(0);
+    wait_all<0>();
     for (int32_t t = 0; t < tiles; ++t) {
-      i32x4v xa[OpA::kSlots], xb[OpB::kSlots];
-      if (t + 1 < tiles) {
-        a.load(xa, t + 1, klen - int64_t(t + 1) * kInner, tid);
-        b.load(xb, t + 1, klen - int64_t(t + 1) * kInner, tid);
-      }
+      const char* at = lds + (t & 1) * 2 * kPlace;
+      if (t + 1 < tiles) fetch(t + 1);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         i32x4v fa[MT], fb[NT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fa[i] = ra.read(buf_a(t), i, s);
+        for (int i = 0; i < MT; ++i) fa[i] = ra.read(at, i, s);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) fb[j] = rb.read(buf_b(t), j, s);
+        for (int j = 0; j < NT; ++j) fb[j] = rb.read(at + kPlace, j, s);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
           for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
       }
-      if (t + 1 < tiles) {
-        a.store(xa, buf_a(t + 1), tid);
-        b.store(xb, buf_b(t + 1), tid);
-      }
-      wait_all();
+      if (t + 1 < tiles) place(t + 1);
+      wait_all<0>();
     }
   }
 
@@ -446,11 +459,11 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   // rows fall on different banks, and then takes 8 columns of one row whose
   // other columns its neighbours take: whole lines of y, z and the residual.
   constexpr int kUnits = NT * 2;                                // 8-column units of a wave's row
-  constexpr int kRows = 2 * kBuf / (WM * WN) / (kUnits * 32);   // rows of the share
-  constexpr int kRounds = MT * 16 > kRows ? MT * 16 / kRows : 1, kTilesRound = MT / kRounds;
+  constexpr int kRounds = MT > 4 ? MT / 4 : 1, kTilesRound = MT / kRounds;
+  constexpr int kShare = kTilesRound * 16 * kUnits * 32;        // bytes of a wave's share
   constexpr int kPassRows = 64 / kUnits, kPasses = kTilesRound * 16 / kPassRows, kAhead = 4;
-  static_assert(kTilesRound * kRounds == MT && kPasses % kAhead == 0, "whole rounds");
-  char* share = lds + wave * (2 * kBuf / (WM * WN));
+  static_assert(kTilesRound * kRounds == MT && kPasses % kAhead == 0 && uint32_t(kShare * WM * WN) <= kRing, "whole rounds");
+  char* share = lds + wave * kShare;
   const bool swap = !BK && (lane & 16);
   const int32_t unit = lane % kUnits, n = n0 + wn * NT * 16 + 8 * unit;
   const int have = g.e.N - n;
@@ -459,7 +472,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   load_bias<T, 8>(bias, g.e, n);
 #pragma unroll
   for (int round = 0; round < kRounds; ++round) {
-    if (round == 0) wait_all();
+    if (round == 0) wait_all<0>();
     else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kTilesRound; ++i) {
