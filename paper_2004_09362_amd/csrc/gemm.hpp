@@ -462,7 +462,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   constexpr int kRounds = MT > 4 ? MT / 4 : 1, kTilesRound = MT / kRounds;
   constexpr int kShare = kTilesRound * 16 * kUnits * 32;        // bytes of a wave's share
   constexpr int kPassRows = 64 / kUnits, kPasses = kTilesRound * 16 / kPassRows, kAhead = 4;
-  static_assert(kTilesRound * kRounds == MT && kPasses % kAhead == 0 && uint32_t(kShare * WM * WN) <= kRing, "whole rounds");
+  static_assert(kTilesRound * kRounds == MT && kPasses % (2 * kAhead) == 0 && uint32_t(kShare * WM * WN) <= kRing, "whole rounds");
   char* share = lds + wave * kShare;
   const bool swap = !BK && (lane & 16);
   const int32_t unit = lane % kUnits, n = n0 + wn * NT * 16 + 8 * unit;
@@ -470,51 +470,61 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   float* part = g.part + int64_t(blockIdx.y) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
   float bias[8];
   load_bias<T, 8>(bias, g.e, n);
-#pragma unroll
-  for (int round = 0; round < kRounds; ++round) {
-    if (round == 0) wait_all<0>();
-    else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  auto spread = [&](auto round) {
+    constexpr int first = decltype(round)::value * kTilesRound;
 #pragma unroll
     for (int i = 0; i < kTilesRound; ++i) {
 #pragma unroll
       for (int j = 0; j < NT / 2; ++j) {
-        const f32x4v x = acc[round * kTilesRound + i][2 * j], y = acc[round * kTilesRound + i][2 * j + 1];
+        const f32x4v x = acc[first + i][2 * j], y = acc[first + i][2 * j + 1];
         const int r = 16 * i + (lane & 15), u = (4 * j + (lane >> 4)) ^ (r & (kUnits - 1));
         f32x4v* q = reinterpret_cast<f32x4v*>(share + (r * kUnits + u) * 32);
         q[0] = swap ? y : x;
         q[1] = swap ? x : y;
       }
     }
+  };
+  wait_all<0>();
+#pragma unroll 1
+  for (int round = 0; round < kRounds; ++round) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    static_assert(kRounds <= 2, "rounds");
+    if (round == 0) spread(std::integral_constant<int, 0>{});
+    else spread(std::integral_constant<int, kRounds - 1>{});
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     const int32_t mw = m0 + (wm * MT + round * kTilesRound) * 16 + lane / kUnits;
     auto unit_at = [&](int r) { return share + (r * kUnits + (unit ^ (r & (kUnits - 1)))) * 32; };
     if (have >= 8) {
-      for (int pass = 0; pass < kPasses; pass += kAhead) {
-        float v[kAhead][8], res[kAhead][8];
+      // the residual of half the passes is on its way while half are worked on
+      Residual<8> res0[kAhead], res1[kAhead];
+      auto fetch = [&](Residual<8> (&res)[kAhead], int pass) {
+        if (g.splits == 1) load_residuals<T, 8, kAhead>(res, g.e, mw + pass * kPassRows, kPassRows, n);
+      };
+      auto finish = [&](const Residual<8> (&res)[kAhead], int pass) {
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-          const f32x4v* w = reinterpret_cast<const f32x4v*>(unit_at((pass + q) * kPassRows + lane / kUnits));
-          const f32x4v x = w[0], y = w[1];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[q][e] = x[e];
-            v[q][4 + e] = y[e];
-          }
-          const int32_t m = mw + (pass + q) * kPassRows;
-          if (g.splits == 1 && m < g.e.M) load_residual<T, 8>(res[q], g.e, m, n);
-        }
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-          const int32_t m = mw + (pass + q) * kPassRows;
+          const int r = (pass + q) * kPassRows;
+          const int32_t m = mw + r;
           if (m >= g.e.M) continue;
+          const f32x4v* w = reinterpret_cast<const f32x4v*>(unit_at(r + lane / kUnits));
+          const f32x4v x = w[0], y = w[1];
           if (g.splits > 1) {
-            f32x4v* w = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
-            w[0] = f32x4v{v[q][0], v[q][1], v[q][2], v[q][3]};
-            w[1] = f32x4v{v[q][4], v[q][5], v[q][6], v[q][7]};
+            f32x4v* to = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
+            to[0] = x;
+            to[1] = y;
           } else {
-            emit<T, 8>(v[q], bias, res[q], g.e, m, n);
+            float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            emit<T, 8>(v, bias, res[q], g.e, m, n);
           }
         }
+      };
+      fetch(res0, 0);
+#pragma unroll 1
+      for (int pass = 0; pass < kPasses; pass += 2 * kAhead) {
+        fetch(res1, pass + kAhead);
+        finish(res0, pass);
+        if (pass + 2 * kAhead < kPasses) fetch(res0, pass + 2 * kAhead);
+        finish(res1, pass + kAhead);
       }
     } else {  // the lanes of a row's last, partial unit
 #pragma unroll 1

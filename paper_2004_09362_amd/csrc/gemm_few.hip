@@ -14,7 +14,7 @@ namespace ar {
 
 template <typename T, int MT, int NT>
 __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
-  constexpr int kWaves = 8, kElems = 16 / int(sizeof(T)), kStep = 4 * kElems, kBatch = MT >= 4 ? 2 : 4;
+  constexpr int kWaves = 8, kElems = 16 / int(sizeof(T)), kStep = 4 * kElems, kBatch = MT * NT >= 4 ? 2 : MT * NT == 2 ? 4 : 8;
   __shared__ f32x4v sums[kWaves][MT * NT][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, p = lane >> 4;
   const int32_t n0 = int32_t(blockIdx.x) * 16 * NT;
@@ -47,34 +47,30 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
   for (int a = 0; a < MT; ++a)
 #pragma unroll
     for (int b = 0; b < NT; ++b) acc[a][b] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
-  i32x4v wn[NT][kBatch];
-  if (b0 < b1) {
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) wn[t][q] = read(wr[t], b0, q);
-  }
-  for (int32_t b = b0; b < b1; ++b) {
-    i32x4v wc[NT][kBatch], xc[MT][kBatch];
+  // a batch of both operands is on its way while one is multiplied
+  i32x4v ws[2][NT][kBatch], xs[2][MT][kBatch];
+  auto fetch = [&](int set, int32_t batch) {
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t) xc[t][q] = read(xr[t], b, q);
+      for (int t = 0; t < NT; ++t) ws[set][t][q] = read(wr[t], batch, q);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) wc[t][q] = wn[t][q];
+      for (int t = 0; t < MT; ++t) xs[set][t][q] = read(xr[t], batch, q);
     }
-    if (b + 1 < b1) {
+  };
+  if (b0 < b1) fetch(0, b0);
+  for (int32_t b = b0; b < b1; b += 2) {
+#pragma unroll
+    for (int set = 0; set < 2; ++set) {
+      if (b + set >= b1) break;
+      if (b + set + 1 < b1) fetch(1 - set, b + set + 1);
 #pragma unroll
       for (int q = 0; q < kBatch; ++q)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) wn[t][q] = read(wr[t], b + 1, q);
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+          for (int t = 0; t < NT; ++t) acc[a][t] = mma<T>(ws[set][t][q], xs[set][a][q], acc[a][t]);
     }
-#pragma unroll
-    for (int q = 0; q < kBatch; ++q)
-#pragma unroll
-      for (int a = 0; a < MT; ++a)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[a][t] = mma<T>(wc[t][q], xc[a][q], acc[a][t]);
   }
 
 #pragma unroll
@@ -96,10 +92,11 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
       for (int c = 0; c < 3; ++c)
         if (n + c < g.e.N) emit_one<T>(v[c], g.e, m, n + c);
     } else {
-      float x[4] = {v[0], v[1], v[2], v[3]}, bias[4], res[4];
+      float x[4] = {v[0], v[1], v[2], v[3]}, bias[4];
+      Residual<4> res[1];
       load_bias<T, 4>(bias, g.e, n);
-      load_residual<T, 4>(res, g.e, m, n);
-      emit<T, 4>(x, bias, res, g.e, m, n);
+      load_residuals<T, 4, 1>(res, g.e, m, 1, n);
+      emit<T, 4>(x, bias, res[0], g.e, m, n);
     }
   }
 }

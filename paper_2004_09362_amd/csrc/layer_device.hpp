@@ -96,38 +96,103 @@ __device__ __forceinline__ float drop_one(float x, const DropArgs& d, uint64_t r
   return word <= d.last ? x * d.scale : 0.0f;
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSqrtHalf = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kGeluTanh2 = 1.5957691216057308f;      // 2 sqrt(2 / pi)
 constexpr float kGeluCubic = 0.044715f;
 
-__device__ __forceinline__ float logistic(float u) { return __builtin_amdgcn_rcpf(1.0f + __expf(-u)); }
+// 1 / (1 + 2^u).
+__device__ __forceinline__ float logistic2(float u) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u));
+}
 
+// exp(-z^2 / 2), and the normal distribution's tail beyond |z|: Abramowitz and
+// Stegun, 7.1.26 (a polynomial in 1 / (1 + p x) times exp(-x^2), x = |z| / sqrt 2),
+// off by 7.5e-8 at most and, unlike 1 + erf, small where the tail is.
+__device__ __forceinline__ float normal_tail(float z, float& gauss) {
+  const float x = __builtin_fabsf(z);
+  gauss = __builtin_amdgcn_exp2f(-0.5f * kLog2e * z * z);
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * kSqrtHalf, x, 1.0f));
+  float p = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  p = __builtin_fmaf(p, t, 0.5f * 1.421413741f);
+  p = __builtin_fmaf(p, t, 0.5f * -0.284496736f);
+  p = __builtin_fmaf(p, t, 0.5f * 0.254829592f);
+  return p * t * gauss;
+}
+
+__device__ __forceinline__ float act_relu(float z) { return z > 0.0f ? z : (z != z ? z : 0.0f); }
+__device__ __forceinline__ float act_gelu(float z) {
+  float gauss;
+  const float q = z * normal_tail(z, gauss);
+  return z > 0.0f ? z - q : q;
+}
 // (1 + tanh(u)) / 2 is the logistic function of 2 u.
-__device__ __forceinline__ float act_value(float z, int act) {
+__device__ __forceinline__ float act_gelu_tanh(float z) {
+  return z * logistic2(z * __builtin_fmaf(-kLog2e * kGeluTanh2 * kGeluCubic * z, z, -kLog2e * kGeluTanh2));
+}
+__device__ __forceinline__ float act_silu(float z) { return z * logistic2(-kLog2e * z); }
+
+__device__ __forceinline__ float slope_gelu(float z) {
+  float gauss;
+  const float q = normal_tail(z, gauss);
+  return __builtin_fmaf(z * kInvSqrt2Pi, gauss, z > 0.0f ? 1.0f - q : q);
+}
+__device__ __forceinline__ float slope_gelu_tanh(float z) {
+  const float t = z * z;
+  const float g = logistic2(z * __builtin_fmaf(-kLog2e * kGeluTanh2 * kGeluCubic, t, -kLog2e * kGeluTanh2));
+  return __builtin_fmaf(z * g * (1.0f - g), __builtin_fmaf(3.0f * kGeluCubic * kGeluTanh2, t, kGeluTanh2), g);
+}
+__device__ __forceinline__ float slope_silu(float z) {
+  const float g = logistic2(-kLog2e * z);
+  return g * __builtin_fmaf(z, 1.0f - g, 1.0f);
+}
+
+// v[i] = act(v[i]): one branch for all.
+template <int V>
+__device__ __forceinline__ void activate(float (&v)[V], int act) {
   switch (act) {
-    case kActRelu: return z > 0.0f ? z : (z != z ? z : 0.0f);
-    case kActGelu: return 0.5f * z * (1.0f + erff(z * kSqrtHalf));
-    case kActGeluTanh: return z * logistic(kGeluTanh2 * z * __builtin_fmaf(kGeluCubic * z, z, 1.0f));
-    case kActSilu: return z * logistic(z);
-    default: return z;
+    case kActRelu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = act_relu(v[i]);
+      break;
+    case kActGelu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = act_gelu(v[i]);
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = act_gelu_tanh(v[i]);
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = act_silu(v[i]);
+      break;
+    default: break;
   }
 }
 
-__device__ __forceinline__ float act_slope(float z, int act) {
+// v[i] *= act'(z[i])
+template <int V>
+__device__ __forceinline__ void times_slope(float (&v)[V], const float (&z)[V], int act) {
   switch (act) {
-    case kActRelu: return z > 0.0f ? 1.0f : 0.0f;
-    case kActGelu: return 0.5f * (1.0f + erff(z * kSqrtHalf)) + z * kInvSqrt2Pi * __expf(-0.5f * z * z);
-    case kActGeluTanh: {
-      const float t = z * z;
-      const float g = logistic(kGeluTanh2 * z * __builtin_fmaf(kGeluCubic, t, 1.0f));
-      return __builtin_fmaf(z * g * (1.0f - g), kGeluTanh2 * __builtin_fmaf(3.0f * kGeluCubic, t, 1.0f), g);
-    }
-    case kActSilu: {
-      const float g = logistic(z);
-      return g * __builtin_fmaf(z, 1.0f - g, 1.0f);
-    }
-    default: return 1.0f;
+    case kActRelu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= z[i] > 0.0f ? 1.0f : 0.0f;
+      break;
+    case kActGelu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= slope_gelu(z[i]);
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= slope_gelu_tanh(z[i]);
+      break;
+    case kActSilu:
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] *= slope_silu(z[i]);
+      break;
+    default: break;
   }
 }
 
@@ -145,35 +210,67 @@ __device__ __forceinline__ void load_bias(float (&b)[V], const Epilogue& e, int3
   }
 }
 
-// The residual of V columns from n on, all within the row, of row m (zeros
-// without one).
-template <typename T, int V>
-__device__ __forceinline__ void load_residual(float (&r)[V], const Epilogue& e, int32_t m, int32_t n) {
-  if (!e.res) {
+// V columns of a residual, as they lie in memory: 2 V bytes, and of 32-bit
+// ones the other 2 V.
+template <int V>
+struct Residual {
+  typedef uint32_t Half __attribute__((ext_vector_type(V / 2), aligned(2)));
+  uint32_t __attribute__((ext_vector_type(V / 2))) first, second;
+};
+
+// The residuals of V columns from n on, all within the row, of Q rows from m on
+// `step` apart; of rows past the last one, that one's.  The first halves of all
+// are loaded without a branch between them, so that they go out together.
+template <typename T, int V, int Q>
+__device__ __forceinline__ void load_residuals(Residual<V> (&r)[Q], const Epilogue& e, int32_t m, int32_t step, int32_t n) {
+  using Half = typename Residual<V>::Half;
+  if (!e.res) return;
+  const int shift = e.y_f32 ? 2 : 1;
+  const char* p[Q];
 #pragma unroll
-    for (int i = 0; i < V; ++i) r[i] = 0.0f;
-  } else if (e.y_f32) {
-    load_some<V>(r, static_cast<const float*>(e.res) + int64_t(m) * e.ldr + n, V);
-  } else {
-    load_some<V>(r, static_cast<const T*>(e.res) + int64_t(m) * e.ldr + n, V);
+  for (int q = 0; q < Q; ++q) {
+    const int32_t row = m + q * step < e.M ? m + q * step : e.M - 1;
+    p[q] = static_cast<const char*>(e.res) + ((int64_t(row) * e.ldr + n) << shift);
+    r[q].first = *reinterpret_cast<const Half*>(p[q]);
+  }
+  if (sizeof(T) == 4 || e.y_f32) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) r[q].second = *reinterpret_cast<const Half*>(p[q] + 2 * V);
+  }
+}
+
+// v += the residual
+template <typename T, int V>
+__device__ __forceinline__ void add_residual(float (&v)[V], const Residual<V>& r, const Epilogue& e) {
+  if (!e.res) return;
+  if (sizeof(T) == 4 || e.y_f32) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      v[i] += __builtin_bit_cast(float, uint32_t(r.first[i]));
+      v[V / 2 + i] += __builtin_bit_cast(float, uint32_t(r.second[i]));
+    }
+  } else if constexpr (sizeof(T) == 2) {
+    typedef T P __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      const P p = __builtin_bit_cast(P, uint32_t(r.first[i]));
+      v[2 * i] += float(p[0]);
+      v[2 * i + 1] += float(p[1]);
+    }
   }
 }
 
 // The epilogue of V (4 or 8) columns from n on (a multiple of V), all within
 // the row, of row m; v holds the product's sums.
 template <typename T, int V>
-__device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const float (&r)[V], const Epilogue& e,
+__device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const Residual<V>& r, const Epilogue& e,
                                      int32_t m, int32_t n) {
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] += b[i];
   if (e.z) store_some<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, V);
-  if (e.act != kActNone) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = act_value(v[i], e.act);
-  }
+  activate<V>(v, e.act);
   if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
-#pragma unroll
-  for (int i = 0; i < V; ++i) v[i] += r[i];
+  add_residual<T, V>(v, r, e);
   if (e.y_f32) store_some<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, V);
   else store_some<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, V);
 }
@@ -183,7 +280,9 @@ template <typename T>
 __device__ __forceinline__ void emit_one(float v, const Epilogue& e, int32_t m, int32_t n) {
   if (e.bias) v += e.bias_f32 ? static_cast<const float*>(e.bias)[n] : float(static_cast<const T*>(e.bias)[n]);
   if (e.z) static_cast<T*>(e.z)[int64_t(m) * e.ldz + n] = T(v);
-  v = act_value(v, e.act);
+  float a[1] = {v};
+  activate<1>(a, e.act);
+  v = a[0];
   if (e.drop.on) v = drop_one(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
   const int64_t ry = int64_t(m) * e.ldr + n, yy = int64_t(m) * e.ldy + n;
   if (e.y_f32) {

@@ -40,9 +40,11 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, int log_t
 }
 
 // A workgroup takes 256 columns (32 threads of 8) of one chunk of rows, 8
-// rows at a time; the sums of its 8 row threads meet in LDS in their order.
+// rows at a time, four of these together so that enough loads are in flight;
+// the sums of its 8 row threads meet in LDS in their order.
 template <typename D, typename Z>
 __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
+  constexpr int kRows = 4;
   __shared__ float part[8][32][9];
   const int ct = threadIdx.x & 31, rt = threadIdx.x >> 5;
   const int64_t col = (int64_t(blockIdx.x) * 32 + ct) * 8;
@@ -51,19 +53,25 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
   const int64_t r1 = r0 + c.rows_per < c.M ? r0 + c.rows_per : c.M;
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   if (have > 0) {
-#pragma unroll 2
-    for (int64_t row = r0 + rt; row < r1; row += 8) {
-      float v[8], z[8];
-      load_some<8>(v, static_cast<const D*>(c.dy) + row * c.lddy + col, have);
-      load_some<8>(z, static_cast<const Z*>(c.z) + row * c.ldz + col, c.z ? have : 0);
-      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
-      if (c.z) {
+    for (int64_t row0 = r0 + rt; row0 < r1; row0 += 8 * kRows) {
+      float v[kRows][8], z[kRows][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= act_slope(z[i], c.act);
+      for (int q = 0; q < kRows; ++q) {
+        const int64_t row = row0 + 8 * q;
+        const int there = row < r1 ? have : 0;
+        load_some<8>(v[q], static_cast<const D*>(c.dy) + row * c.lddy + col, there);
+        if (c.z) load_some<8>(z[q], static_cast<const Z*>(c.z) + row * c.ldz + col, there);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += i < have ? v[i] : 0.0f;
-      if (c.dz) store_some<8>(static_cast<Z*>(c.dz) + row * c.lddz + col, v, have);
+      for (int q = 0; q < kRows; ++q) {
+        const int64_t row = row0 + 8 * q;
+        if (row >= r1) break;
+        if (c.drop.on) drop_some<8>(v[q], c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+        if (c.z) times_slope<8>(v[q], z[q], c.act);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] += i < have ? v[q][i] : 0.0f;
+        if (c.dz) store_some<8>(static_cast<Z*>(c.dz) + row * c.lddz + col, v[q], have);
+      }
     }
   }
   if (!c.sums) return;
@@ -79,14 +87,26 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
   }
 }
 
+// 16 columns a workgroup, 16 threads to each column's chunks.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void column_sums_kernel(const float* sums, int32_t chunks, int64_t N, T* db,
                                                                int accumulate) {
-  const int64_t n = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (n >= N) return;
-  float s = accumulate ? float(db[n]) : 0.0f;
-  for (int32_t c = 0; c < chunks; ++c) s += sums[int64_t(c) * N + n];
-  db[n] = T(s);
+  __shared__ float part[16][17];
+  const int ct = threadIdx.x & 15, rt = threadIdx.x >> 4;
+  const int64_t n = int64_t(blockIdx.x) * 16 + ct;
+  float s = 0.0f;
+  if (n < N) {
+#pragma unroll 8
+    for (int32_t c = rt; c < chunks; c += 16) s += sums[int64_t(c) * N + n];
+  }
+  part[rt][ct] = s;
+  __syncthreads();
+  if (rt == 0 && n < N) {
+    float t = accumulate ? float(db[n]) : 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t += part[r][ct];
+    db[n] = T(t);
+  }
 }
 
 template <typename T>
@@ -105,9 +125,10 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log
     }
     return;
   }
-  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8], res[8];
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8];
+  Residual<8> res[1];
   load_bias<T, 8>(bias, g.e, int32_t(n));
-  load_residual<T, 8>(res, g.e, int32_t(m), int32_t(n));
+  load_residuals<T, 8, 1>(res, g.e, int32_t(m), 1, int32_t(n));
 #pragma unroll 4
   for (int32_t s = 0; s < g.splits; ++s) {
     const float4* p = reinterpret_cast<const float4*>(part + s * step);
@@ -115,7 +136,7 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
     v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
-  emit<T, 8>(v, bias, res, g.e, int32_t(m), int32_t(n));
+  emit<T, 8>(v, bias, res[0], g.e, int32_t(m), int32_t(n));
 }
 
 int log2_of(int v) {
@@ -174,7 +195,7 @@ int launch_slope(const SlopeCall& c, int32_t dye, int32_t ze, void* stream) {
 
 int launch_column_sums(const float* sums, int32_t chunks, int64_t N, void* db, int32_t dbe, bool accumulate, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid(uint32_t((N + kThreads - 1) / kThreads));
+  const dim3 grid(uint32_t((N + 15) / 16));
   switch (dbe) {
     case kF32: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<float*>(db), accumulate); break;
     case kF16: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<f16*>(db), accumulate); break;
