@@ -84,21 +84,41 @@ __device__ __forceinline__ void mma_pinned(const i32x4v& rows_n, const i32x4v& r
   }
 }
 __device__ __forceinline__ void mma_ready() { asm volatile("s_nop 1"); }
-__device__ __forceinline__ void mma_done() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
+// last: the sums of the last products, those that may still be on their way.
+__device__ __forceinline__ void mma_done(f32x4v (&last)[8]) {
+  asm volatile("s_nop 15\n\ts_nop 15"
+               : "+a"(last[0]), "+a"(last[1]), "+a"(last[2]), "+a"(last[3]), "+a"(last[4]), "+a"(last[5]), "+a"(last[6]),
+                 "+a"(last[7])::"memory");
+}
 
-// 16 bytes of a row, elements past `have` zero.
+// 16 bytes that start on any element.
 template <typename T>
-__device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have) {
+__device__ __forceinline__ i32x4v load_whole(const void* p) {
+  typedef T U __attribute__((ext_vector_type(16 / int(sizeof(T))), aligned(sizeof(T))));
+  typedef T W __attribute__((ext_vector_type(16 / int(sizeof(T)))));
+  return __builtin_bit_cast(i32x4v, W(*static_cast<const U*>(p)));
+}
+
+// 16 bytes of a row, elements past `have` zero (have may be negative: p lies
+// behind the row's end).  wide: the row has 16 bytes at least; then its last 16
+// bytes are loaded and shifted, without a branch, so that the loads of several
+// chunks go out together.
+template <typename T>
+__device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have, bool wide) {
   constexpr int V = 16 / int(sizeof(T));
-  typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-  typedef T W __attribute__((ext_vector_type(V)));
-  if (have >= V) {
-    const U u = *reinterpret_cast<const U*>(p);
-    return __builtin_bit_cast(i32x4v, W(u));
+  const int h = have < V ? int(have) : V;
+  if (wide) {
+    typedef uint64_t L __attribute__((ext_vector_type(2)));
+    const L x = __builtin_bit_cast(L, load_whole<T>(p + (h - V)));
+    const int bits = h > 0 ? (V - h) * 8 * int(sizeof(T)) : 128;  // to drop
+    const uint64_t lo = bits >= 64 ? x[1] >> (bits & 63) : bits ? x[0] >> bits | x[1] << (64 - bits) : x[0];
+    const L y = {bits >= 128 ? 0 : lo, bits >= 64 ? 0 : x[1] >> bits};
+    return __builtin_bit_cast(i32x4v, y);
   }
+  typedef T W __attribute__((ext_vector_type(V)));
   W w;
 #pragma unroll
-  for (int i = 0; i < V; ++i) w[i] = i < have ? p[i] : T(0);
+  for (int i = 0; i < V; ++i) w[i] = i < h ? p[i] : T(0);
   return __builtin_bit_cast(i32x4v, w);
 }
 
@@ -115,7 +135,8 @@ __device__ __forceinline__ uint32_t lds_offset(const char* p) {
 // 64 lanes' 16 bytes from base + voff to 1024 consecutive bytes of LDS, past
 // the registers.  The compiler's own form of this instruction makes every
 // later LDS read wait for it; here the caller waits (wait_all), one tile
-// later.  It has no register outputs, and nothing else here uses m0.
+// later.  It has no register outputs, and nothing else here uses m0.  base must
+// be settled().
 // lds_target() names the place, one instruction at least before.
 __device__ __forceinline__ void lds_target(uint32_t lds) { asm volatile("s_mov_b32 m0, %0" ::"s"(lds)); }
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t voff) {
@@ -131,6 +152,24 @@ __device__ __forceinline__ void wait_all() {
   __builtin_amdgcn_s_waitcnt((LOADS & 15) | ((LOADS >> 4) << 14) | 0x70);  // vmcnt(LOADS) lgkmcnt(0)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
+}
+
+// The workgroup's LDS writes are done; loads into registers may be on their way.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// An address that is the same for all lanes, in scalar registers that a load to
+// LDS may read: five wait states after a vector instruction wrote them, which
+// the compiler does not know to insert before the assembly that reads them.
+__device__ __forceinline__ const char* settled(const char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v)), hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
+  asm volatile("s_nop 4" : "+s"(lo), "+s"(hi));
+  return reinterpret_cast<const char*>(uint64_t(hi) << 32 | lo);
 }
 
 // An operand's tile: R rows of the output, 128 bytes of inner length each.
@@ -157,14 +196,17 @@ struct Operand {
   const char* base;   // element (first row, first inner index of the split)
   int64_t ld;         // bytes between rows of the matrix
   int32_t rows;       // rows of the output left from the tile's first one
+  bool near, wide;    // whether a tile's offsets fit 32 bits; whether the matrix' rows have 16 bytes
   uint32_t voff[kSlots];
 
   // Byte offsets of this thread's chunks from the tile's first element.  A
   // chunk of rows past the last is read from the last (k-major) or the first
   // (otherwise): its products land in sums that are never stored.
-  __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int tid) {
+  __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int64_t inner, int tid) {
     ld = ld_elems * int64_t(sizeof(T));
     rows = int32_t(nrows - row0 < R ? nrows - row0 : R);
+    near = ld <= kMaxTileLd;
+    wide = (KMAJOR ? inner : nrows) >= kElems;
     base = reinterpret_cast<const char*>(p) +
            (KMAJOR ? row0 * ld + k0 * int64_t(sizeof(T)) : k0 * ld + row0 * int64_t(sizeof(T)));
 #pragma unroll
@@ -192,10 +234,26 @@ struct Operand {
   // This thread's chunk i of tile t, of which k_have inner indices exist.
   __device__ __forceinline__ i32x4v chunk(int i, int32_t t, int64_t k_have, int tid) const {
     const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
-    const int64_t have = KMAJOR ? (r < rows ? k_have - c * kElems : 0) : (r < k_have ? rows - c * kElems : 0);
-    return load_chunk(reinterpret_cast<const T*>(at(t) + int64_t(r) * ld + c * 16), have);
+    if constexpr (KMAJOR) {  // rows past the last one: that one's, whose products are never stored
+      return load_chunk(reinterpret_cast<const T*>(at(t) + int64_t(r < rows ? r : rows - 1) * ld + c * 16),
+                        k_have - c * kElems, wide);
+    } else {  // inner indices past the last one: nothing of the tile's first
+      const bool there = r < k_have;
+      const i32x4v v = load_chunk(reinterpret_cast<const T*>(at(t) + (there ? int64_t(r) * ld : 0) + c * 16),
+                                  rows - c * kElems, wide);
+      return there ? v : i32x4v{0, 0, 0, 0};
+    }
   }
-  __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
+  // A tile into registers.  One that is not the last (and whose offsets fit 32
+  // bits) is loaded without a check, so that the loads go out together: what
+  // it takes from behind a row's end are elements of the matrix' next row, or
+  // lie between the two, and land in sums that are never stored.
+  __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t) const {
+    const char* p = at(t);
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) reg[i] = load_whole<T>(p + voff[i]);
+  }
+  __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) reg[i] = chunk(i, t, k_have, tid);
   }
@@ -203,9 +261,11 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) *reinterpret_cast<i32x4v*>(lds + (i * THREADS + tid) * 16) = reg[i];
   }
+  // A tile, of which something exists, into LDS.
   __device__ __forceinline__ void copy(int32_t t, int64_t k_have, char* lds, int tid) const {
-#pragma unroll 1
-    for (int i = 0; i < kSlots; ++i) *reinterpret_cast<i32x4v*>(lds + (i * THREADS + tid) * 16) = chunk(i, t, k_have, tid);
+    i32x4v reg[kSlots];
+    load_checked(reg, t, k_have, tid);
+    store(reg, lds, tid);
   }
 };
 
@@ -306,8 +366,8 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
 
   OpA a;
   OpB b;
-  a.init(static_cast<const T*>(g.a), g.lda, m0, k0, g.e.M, tid);
-  b.init(static_cast<const T*>(g.b), g.ldb, n0, k0, g.e.N, tid);
+  a.init(static_cast<const T*>(g.a), g.lda, m0, k0, g.e.M, g.K, tid);
+  b.init(static_cast<const T*>(g.b), g.ldb, n0, k0, g.e.N, g.K, tid);
   Fragments<T, AK, false, TM> ra;
   Fragments<T, BK, true, TN> rb;
   ra.init(wm * MT * 16, lane);
@@ -341,44 +401,44 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
       if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
       else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
     };
-    // all of an operand's tile t, through registers where it is not whole
     const int32_t whole = klen / kInner;
-    auto start = [&](const auto& op, int32_t t, uint32_t at) {
-      if (t < whole) {
+    // all of an operand's tile t, or of the last one
+    auto load_all = [&](const auto& op, int32_t t, uint32_t at) {
+      const char* p = settled(op.at(t < whole ? t : whole - 1));
 #pragma unroll
-        for (int x = 0; x < kLoadsA; ++x) {
-          op.aim(x, lds0 + at, wave);
-          asm volatile("s_nop 0");
-          op.issue(op.at(t), x);
-        }
-      } else if (t < tiles) {
-        op.copy(t, klen - int64_t(t) * kInner, lds + at, tid);
+      for (int x = 0; x < kLoadsA; ++x) {
+        op.aim(x, lds0 + at, wave);
+        asm volatile("s_nop 0");
+        op.issue(p, x);
       }
     };
     static_assert(kLoadsA == kLoadsB, "operands of one size");
-    start(a, 0, 0);
-    start(b, 0, kPlace);
-    start(a, 1, 2 * kPlace);
-    start(b, 1, 3 * kPlace);
-    start(a, 2, 4 * kPlace);
-    if (whole > 2) wait_all<3 * kLoadsA>();
-    else wait_all<0>();
     uint32_t at_a = 0, at_b = kPlace;
+    if (whole > 0) {
+      load_all(a, 0, 0);
+      load_all(b, 0, kPlace);
+      load_all(a, 1, 2 * kPlace);
+      load_all(b, 1, 3 * kPlace);
+      load_all(a, 2, 4 * kPlace);
+      wait_all<3 * kLoadsA>();
 #pragma unroll
-    for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
-    int32_t t = 0;
+      for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
+    }
     // The instruction stream of a tile: between two matrix instructions goes
     // at most one other of each kind, so that the matrix unit always has its
     // next one, and the loads are spread, since each keeps the address unit
     // busy for 16 cycles.  Slice 1 is read within the first half of slice 0's
-    // products; after kMeet of them the waves meet.
+    // products; after kMeet of them the waves meet.  The last tiles run the
+    // same stream: their loads take the last tile again, which nobody reads.
     constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
     constexpr int kGapB = kProducts >= 64 ? 5 : 2, kGapA = kProducts >= 64 ? 6 : 3, kMeetA = kMeet + kGapB * kLoadsB;
     static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA <= 2 * kProducts, "everything within a tile");
-    const char* pb = b.at(2);
-    const char* pa = a.at(3);
-    for (; t + 3 < whole; ++t) {
+    const char* pb = settled(b.at(whole > 2 ? 2 : whole - 1));
+    const char* pa = settled(a.at(whole > 3 ? 3 : whole - 1));
+    for (int32_t t = 0; t < whole; ++t) {
       const uint32_t next_a = after(at_b), next_b = after(next_a);
+      const char* const from_a = settled(pa);
+      const char* const from_b = settled(pb);
       if constexpr (kPinned) mma_ready();
       unrolled([&](auto index) {
         constexpr int x = decltype(index)::value, y = x - kProducts, zb = x - kMeet, za = x - kMeetA;
@@ -386,56 +446,47 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
         if constexpr (x == kMeet) wait_all<kLoadsA>();
         if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, next_a, next_b, y / kReadGap1);
         if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
-        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(pb, zb / kGapB);
+        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(from_b, zb / kGapB);
         if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
-        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(pa, za / kGapA);
+        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(from_a, za / kGapA);
         product(x / kProducts, x % kProducts);
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, 2 * kProducts>{});
-      pa += a.step();
-      pb += b.step();
+      pb += t + 3 < whole ? b.step() : 0;
+      pa += t + 4 < whole ? a.step() : 0;
       at_a = next_a;
       at_b = next_b;
     }
-    for (; t < tiles; ++t) {  // the last ones
-      const uint32_t next_a = after(at_b), next_b = after(next_a);
-#pragma unroll
-      for (int x = 0; x < kReads; ++x) read(1, at_a, at_b, x);
-      if constexpr (kPinned) mma_ready();
-#pragma unroll
-      for (int x = 0; x < kProducts; ++x) product(0, x);
+    if (whole < tiles) {  // what is left of the inner length, through registers
       wait_all<0>();
-      start(b, t + 2, at_a);
-      start(a, t + 3, at_b);
-      if (t + 1 < tiles) {
+      a.copy(whole, klen - int64_t(whole) * kInner, lds, tid);
+      b.copy(whole, klen - int64_t(whole) * kInner, lds + kPlace, tid);
+      wait_all<0>();
 #pragma unroll
-        for (int x = 0; x < kReads; ++x) read(0, next_a, next_b, x);
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int x = 0; x < kReads; ++x) read(s, 0, kPlace, x);
       }
       if constexpr (kPinned) mma_ready();
 #pragma unroll
-      for (int x = 0; x < kProducts; ++x) product(1, x);
-      at_a = next_a;
-      at_b = next_b;
+      for (int x = 0; x < 2 * kProducts; ++x) product(x / kProducts, x % kProducts);
     }
-    if constexpr (kPinned) mma_done();
+    if constexpr (kPinned) mma_done(acc[MT - 1]);
   } else {
-    // a tile at a time through registers, which the next one is loaded into
-    // while it is multiplied
-    i32x4v xa[OpA::kSlots], xb[OpB::kSlots];
-    auto fetch = [&](int32_t t) {
-      a.load(xa, t, klen - int64_t(t) * kInner, tid);
-      b.load(xb, t, klen - int64_t(t) * kInner, tid);
+    // Tiles go through registers, two sets of them: while tile t is
+    // multiplied, t + 2 is on its way and t + 1, which has arrived, is written
+    // to the other half of LDS, after which t + 3 is asked for.
+    i32x4v xa0[OpA::kSlots], xb0[OpB::kSlots], xa1[OpA::kSlots], xb1[OpB::kSlots];
+    auto fetch = [&](i32x4v (&xa)[OpA::kSlots], i32x4v (&xb)[OpB::kSlots], int32_t t) {
+      a.load_checked(xa, t, klen - int64_t(t) * kInner, tid);
+      b.load_checked(xb, t, klen - int64_t(t) * kInner, tid);
     };
-    auto place = [&](int32_t t) {
-      a.store(xa, lds + (t & 1) * 2 * kPlace, tid);
-      b.store(xb, lds + (t & 1) * 2 * kPlace + kPlace, tid);
+    auto place = [&](const i32x4v (&xa)[OpA::kSlots], const i32x4v (&xb)[OpB::kSlots], int half) {
+      a.store(xa, lds + half * 2 * kPlace, tid);
+      b.store(xb, lds + half * 2 * kPlace + kPlace, tid);
     };
-    fetch(0);
-    place(0);
-    wait_all<0>();
-    for (int32_t t = 0; t < tiles; ++t) {
-      const char* at = lds + (t & 1) * 2 * kPlace;
-      if (t + 1 < tiles) fetch(t + 1);
+    auto multiply = [&](int half) {
+      const char* at = lds + half * 2 * kPlace;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         i32x4v fa[MT], fb[NT];
@@ -448,8 +499,60 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
 #pragma unroll
           for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
       }
-      if (t + 1 < tiles) place(t + 1);
-      wait_all<0>();
+    };
+    const bool near = a.near && b.near;
+    int32_t t = 0;
+    if (near && tiles > 4) {
+      a.load(xa0, 0);
+      b.load(xb0, 0);
+      a.load(xa1, 1);
+      b.load(xb1, 1);
+      place(xa0, xb0, 0);
+      a.load(xa0, 2);
+      b.load(xb0, 2);
+      meet();
+      for (; t + 5 < tiles; t += 2) {  // t + 4 is not the last
+        multiply(0);
+        place(xa1, xb1, 1);
+        a.load(xa1, t + 3);
+        b.load(xb1, t + 3);
+        meet();
+        multiply(1);
+        place(xa0, xb0, 0);
+        a.load(xa0, t + 4);
+        b.load(xb0, t + 4);
+        meet();
+      }
+      // t + 1 and t + 2 are in the registers; t + 3 is the last or the last but one
+      multiply(0);
+      place(xa1, xb1, 1);
+      if (t + 4 < tiles) {
+        a.load(xa1, t + 3);
+        b.load(xb1, t + 3);
+      } else {
+        fetch(xa1, xb1, t + 3);
+      }
+      meet();
+      multiply(1);
+      place(xa0, xb0, 0);
+      if (t + 4 < tiles) fetch(xa0, xb0, t + 4);
+      meet();
+      multiply(0);
+      place(xa1, xb1, 1);
+      meet();
+      multiply(1);
+      if (t + 4 < tiles) {
+        place(xa0, xb0, 0);
+        meet();
+        multiply(0);
+      }
+    } else {
+      for (; t < tiles; ++t) {
+        fetch(xa0, xb0, t);
+        place(xa0, xb0, t & 1);
+        meet();
+        multiply(t & 1);
+      }
     }
   }
 

@@ -12,18 +12,19 @@
 
 namespace ar {
 
-template <typename T, int MT, int NT>
-__global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
-  constexpr int kWaves = 8, kElems = 16 / int(sizeof(T)), kStep = 4 * kElems, kBatch = MT * NT >= 4 ? 2 : MT * NT == 2 ? 4 : 8;
-  __shared__ f32x4v sums[kWaves][MT * NT][64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, p = lane >> 4;
-  const int32_t n0 = int32_t(blockIdx.x) * 16 * NT;
+template <typename T, int MT, int NW>
+__global__ __launch_bounds__(1024) void gemm_few_kernel(GemmArgs g) {
+  constexpr int NT = 1, kWaves = 16, kGroups = kWaves / NW, kElems = 16 / int(sizeof(T)), kStep = 4 * kElems, kBatch = MT >= 4 ? 2 : 4;
+  __shared__ f32x4v sums[kGroups][MT * NW][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, p = lane >> 4;
+  const int part = wave / NW, column = wave % NW;  // of the inner length, and of the columns
+  const int32_t n0 = int32_t(blockIdx.x) * 16 * NW;
   const int32_t K = g.K, k0 = int32_t(blockIdx.y) * g.k_split;
   const int32_t klen = K - k0 < g.k_split ? K - k0 : g.k_split;
-  // whole batches of steps for each wave
-  const int32_t steps = (klen + kStep - 1) / kStep;
-  const int32_t batches = (steps + kBatch - 1) / kBatch, per = (batches + kWaves - 1) / kWaves;
-  const int32_t b0 = wave * per, b1 = b0 + per < batches ? b0 + per : batches;
+  // batches of steps for each wave; the last of all may reach past the row
+  const int32_t batches = (klen + kStep * kBatch - 1) / (kStep * kBatch), full = klen / (kStep * kBatch);
+  const int32_t per = (batches + kGroups - 1) / kGroups;
+  const int32_t b0 = part * per, b1 = b0 + per < full ? b0 + per : full;
 
   const T* xr[MT];
   const T* wr[NT];
@@ -34,13 +35,10 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
   }
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int32_t n = n0 + 16 * t + i;
+    const int32_t n = n0 + 16 * (column * NT + t) + i;
     wr[t] = static_cast<const T*>(g.b) + int64_t(n < g.e.N ? n : g.e.N - 1) * g.ldb;
   }
-  auto read = [&](const T* row, int32_t batch, int q) {
-    const int32_t k = k0 + (batch * kBatch + q) * kStep + p * kElems;
-    return load_chunk(row + k, k0 + klen - k);
-  };
+  const int32_t kl = k0 + p * kElems;
 
   f32x4v acc[MT][NT];
 #pragma unroll
@@ -50,41 +48,63 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
   // a batch of both operands is on its way while one is multiplied
   i32x4v ws[2][NT][kBatch], xs[2][MT][kBatch];
   auto fetch = [&](int set, int32_t batch) {
+    const int32_t k = kl + batch * (kBatch * kStep);
 #pragma unroll
     for (int q = 0; q < kBatch; ++q) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) ws[set][t][q] = read(wr[t], batch, q);
+      for (int t = 0; t < NT; ++t) ws[set][t][q] = load_whole<T>(wr[t] + k + q * kStep);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) xs[set][t][q] = read(xr[t], batch, q);
+      for (int t = 0; t < MT; ++t) xs[set][t][q] = load_whole<T>(xr[t] + k + q * kStep);
     }
   };
-  if (b0 < b1) fetch(0, b0);
-  for (int32_t b = b0; b < b1; b += 2) {
+  auto multiply = [&](int set) {
 #pragma unroll
-    for (int set = 0; set < 2; ++set) {
-      if (b + set >= b1) break;
-      if (b + set + 1 < b1) fetch(1 - set, b + set + 1);
+    for (int q = 0; q < kBatch; ++q)
 #pragma unroll
-      for (int q = 0; q < kBatch; ++q)
+      for (int a = 0; a < MT; ++a)
 #pragma unroll
-        for (int a = 0; a < MT; ++a)
+        for (int t = 0; t < NT; ++t) acc[a][t] = mma<T>(ws[set][t][q], xs[set][a][q], acc[a][t]);
+  };
+  // Workgroups start at different batches, so that they do not all ask for the
+  // same part of every row, which may lie a power of two apart, at a time.
+  const int32_t mine = b1 - b0, turn = mine > 0 ? int32_t(blockIdx.x % uint32_t(mine)) : 0;
+  auto at = [&](int32_t b) { return b0 + (b + turn < mine ? b + turn : b + turn - mine); };
+  if (mine > 0) fetch(0, at(0));
+  int32_t b = 0;
+  for (; b + 2 < mine; b += 2) {
+    fetch(1, at(b + 1));
+    multiply(0);
+    fetch(0, at(b + 2));
+    multiply(1);
+  }
+  if (b + 1 < mine) fetch(1, at(b + 1));
+  if (b < mine) multiply(0);
+  if (b + 1 < mine) multiply(1);
+  if (batches > full && part == full / per) {  // what is left of the row
+#pragma unroll 1
+    for (int32_t k = kl + full * (kBatch * kStep); k - p * kElems < k0 + klen; k += kStep) {
+      i32x4v w[NT], x[MT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) acc[a][t] = mma<T>(ws[set][t][q], xs[set][a][q], acc[a][t]);
+      for (int t = 0; t < NT; ++t) w[t] = load_chunk(wr[t] + k, k0 + klen - k, K >= kElems);
+#pragma unroll
+      for (int t = 0; t < MT; ++t) x[t] = load_chunk(xr[t] + k, k0 + klen - k, K >= kElems);
+#pragma unroll
+      for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[a][t] = mma<T>(w[t], x[a], acc[a][t]);
     }
   }
 
 #pragma unroll
-  for (int a = 0; a < MT; ++a)
-#pragma unroll
-    for (int t = 0; t < NT; ++t) sums[wave][a * NT + t][lane] = acc[a][t];
+  for (int a = 0; a < MT; ++a) sums[part][a * NW + column][lane] = acc[a][0];
   __syncthreads();
-  for (int s = tid; s < MT * NT * 64; s += 512) {
+  for (int s = tid; s < MT * NW * 64; s += kWaves * 64) {
     const int tile = s >> 6, l = s & 63;
-    const int32_t m = 16 * (tile / NT) + (l & 15), n = n0 + 16 * (tile % NT) + 4 * (l >> 4);
+    const int32_t m = 16 * (tile / NW) + (l & 15), n = n0 + 16 * (tile % NW) + 4 * (l >> 4);
     if (m >= g.e.M || n >= g.e.N) continue;
     f32x4v v = sums[0][tile][l];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) v += sums[w][tile][l];
+    for (int w = 1; w < kGroups; ++w) v += sums[w][tile][l];
     if (g.splits > 1) {
       *reinterpret_cast<f32x4v*>(g.part + (int64_t(blockIdx.y) * g.e.M + m) * g.ldp + n) = v;
     } else if (g.e.N - n < 4) {
@@ -101,15 +121,120 @@ __global__ __launch_bounds__(512) void gemm_few_kernel(GemmArgs g) {
   }
 }
 
+// Both operands through LDS, for rows on 16-byte boundaries: a workgroup takes
+// TM rows and 64 columns, and a ring of tiles (128 bytes of inner length each)
+// is on its way asynchronously, up to 144 KB, so that w streams at the rate of
+// memory whatever the products wait for.  Every row of x is read once for 64
+// columns; in the kernel above, whose waves read it for 16, that traffic out
+// of the L2s bounds M > 16.
+template <typename T, int TM>
+__global__ __launch_bounds__(256) void gemm_stream_kernel(GemmArgs g) {
+  constexpr int kThreads = 256, kCols = 64, MT = TM / 16;
+  using OpA = Operand<T, true, false, TM, kThreads>;
+  using OpB = Operand<T, true, false, kCols, kThreads>;
+  constexpr int kTile = OpA::kBytes + OpB::kBytes, kRing = 147456 / kTile < 12 ? 147456 / kTile : 12;
+  constexpr int kLoads = OpA::kSlots + OpB::kSlots, kInner = OpA::kInner;
+  __shared__ __attribute__((aligned(1024))) char lds[kRing * kTile];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int32_t n0 = int32_t(blockIdx.x) * kCols, k0 = int32_t(blockIdx.y) * g.k_split;
+  const int32_t klen = g.K - k0 < g.k_split ? g.K - k0 : g.k_split;
+  const int32_t tiles = (klen + kInner - 1) / kInner, whole = klen / kInner;
+  OpA a;
+  OpB b;
+  a.init(static_cast<const T*>(g.a), g.lda, 0, k0, g.e.M, g.K, tid);
+  b.init(static_cast<const T*>(g.b), g.ldb, n0, k0, g.e.N, g.K, tid);
+  Fragments<T, true, false, TM> ra;
+  Fragments<T, true, false, kCols> rb;
+  ra.init(0, lane);
+  rb.init(wave * 16, lane);
+  f32x4v acc[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i) acc[i] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const uint32_t lds0 = lds_offset(lds);
+  // Workgroups start at different tiles, so that they do not all ask for the
+  // same 128 bytes of every row, which may lie a power of two apart, at a time
+  // (w of 16384 x 4096 bf16: 27 us against 31), while x stays in the L2s.
+  const bool apart = int64_t(g.e.M) * g.K * int64_t(sizeof(T)) <= (int64_t(2) << 20);
+  const int32_t turn = apart && whole > 0 ? int32_t((blockIdx.x * 5u + blockIdx.y) % uint32_t(whole)) : 0;
+  auto start = [&](int32_t t, uint32_t at) {
+    const int32_t k = t + turn < whole ? t + turn : t + turn - whole;
+    const char* pa = settled(a.at(k));
+    const char* pb = settled(b.at(k));
+#pragma unroll
+    for (int x = 0; x < kLoads; ++x) {
+      if (x < OpB::kSlots) b.aim(x, lds0 + at + OpA::kBytes, wave);
+      else a.aim(x - OpB::kSlots, lds0 + at, wave);
+      asm volatile("s_nop 0");
+      if (x < OpB::kSlots) b.issue(pb, x);
+      else a.issue(pa, x - OpB::kSlots);
+    }
+  };
+  auto multiply = [&](uint32_t at) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const i32x4v fb = rb.read(lds + at + OpA::kBytes, 0, s);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[i] = mma<T>(fb, ra.read(lds + at, i, s), acc[i]);
+    }
+  };
+  auto after = [](uint32_t at) { return at == (kRing - 1) * kTile ? 0 : at + kTile; };
+  // tile t lies at place t mod kRing; the one after the ring's last is loaded
+  // to where tile t - 1 lay, once every wave has read that
+  uint32_t at = 0, free = (kRing - 1) * kTile;
+#pragma unroll 1
+  for (int32_t t = 0; t < kRing - 1 && t < whole; ++t) start(t, uint32_t(t) * kTile);
+  int32_t t = 0;
+  for (; t + kRing - 1 < whole; ++t) {
+    wait_all<(kRing - 2) * kLoads>();
+    start(t + kRing - 1, free);
+    multiply(at);
+    free = at;
+    at = after(at);
+  }
+  for (; t < tiles; ++t) {
+    if (t == whole) {  // the last tile, not whole: through registers, to a place that nothing is read from
+      wait_all<0>();
+      a.copy(t, klen - int64_t(t) * kInner, lds + at, tid);
+      b.copy(t, klen - int64_t(t) * kInner, lds + at + OpA::kBytes, tid);
+    }
+    wait_all<0>();
+    multiply(at);
+    at = after(at);
+  }
+
+  // lane (i, p): columns 4 p to 4 p + 3 of the wave's 16, row 16 t + i
+  const int32_t n = n0 + 16 * wave + 4 * (lane >> 4);
+  float bias[4];
+  load_bias<T, 4>(bias, g.e, n);
+#pragma unroll
+  for (int i = 0; i < MT; ++i) {
+    const int32_t m = 16 * i + (lane & 15);
+    if (m >= g.e.M || n >= g.e.N) continue;
+    if (g.splits > 1) {
+      *reinterpret_cast<f32x4v*>(g.part + (int64_t(blockIdx.y) * g.e.M + m) * g.ldp + n) = acc[i];
+    } else if (g.e.N - n < 4) {
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        if (n + c < g.e.N) emit_one<T>(acc[i][c], g.e, m, n + c);
+    } else {
+      float x[4] = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
+      Residual<4> res[1];
+      load_residuals<T, 4, 1>(res, g.e, m, 1, n);
+      emit<T, 4>(x, bias, res[0], g.e, m, n);
+    }
+  }
+}
+
 namespace {
 
 template <typename T, int MT>
 int launch_few(const GemmArgs& g, hipStream_t st) {
-  // two tiles of 16 columns a workgroup where that still fills the chip
-  const bool two = g.e.N >= 16 * 2 * 512;
-  const dim3 grid(uint32_t((g.e.N + (two ? 31 : 15)) / (two ? 32 : 16)), uint32_t(g.splits));
-  if (two) gemm_few_kernel<T, MT, 2><<<grid, dim3(512), 0, st>>>(g);
-  else gemm_few_kernel<T, MT, 1><<<grid, dim3(512), 0, st>>>(g);
+  const int32_t tiles = (g.e.N + 15) / 16, nw = tiles >= 4 * 256 ? 4 : tiles >= 2 * 256 ? 2 : 1;
+  const dim3 grid(uint32_t((tiles + nw - 1) / nw), uint32_t(g.splits));
+  if (nw == 4) gemm_few_kernel<T, MT, 4><<<grid, dim3(1024), 0, st>>>(g);
+  else if (nw == 2) gemm_few_kernel<T, MT, 2><<<grid, dim3(1024), 0, st>>>(g);
+  else gemm_few_kernel<T, MT, 1><<<grid, dim3(1024), 0, st>>>(g);
   return int(hipGetLastError());
 }
 
@@ -129,6 +254,29 @@ int launch_gemm_few(const GemmArgs& g, int32_t elem, void* stream) {
     case kF32: return launch_few_of<float>(g, st);
     case kF16: return launch_few_of<f16>(g, st);
     case kBF16: return launch_few_of<bf16>(g, st);
+  }
+  return int(hipErrorInvalidValue);
+}
+
+namespace {
+
+template <typename T>
+int launch_stream_of(const GemmArgs& g, hipStream_t st) {
+  const dim3 grid(uint32_t((g.e.N + 63) / 64), uint32_t(g.splits));
+  if (g.e.M <= 32) gemm_stream_kernel<T, 32><<<grid, dim3(256), 0, st>>>(g);
+  else gemm_stream_kernel<T, 64><<<grid, dim3(256), 0, st>>>(g);
+  return int(hipGetLastError());
+}
+
+}  // namespace
+
+int launch_gemm_stream(const GemmArgs& g, int32_t elem, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (g.e.M < 1 || g.e.M > kFewMaxRows) return int(hipErrorInvalidValue);
+  switch (elem) {
+    case kF32: return launch_stream_of<float>(g, st);
+    case kF16: return launch_stream_of<f16>(g, st);
+    case kBF16: return launch_stream_of<bf16>(g, st);
   }
   return int(hipErrorInvalidValue);
 }

@@ -173,44 +173,90 @@ struct Operand {
 bool can_load_async(const Operand& o, int64_t elem_bytes) {
   const int64_t per = 16 / elem_bytes;
   return reinterpret_cast<uintptr_t>(o.data) % 16 == 0 && o.ld % per == 0 && (o.kmajor || o.rows % per == 0) &&
-         o.ld * elem_bytes <= (int64_t(1) << 23);
+         o.ld * elem_bytes <= ar::kMaxTileLd;
 }
 
-// How a product runs.
+// How a product runs: on which kernel, in how many parts of the inner length.
+enum Kind { kTiles, kFew, kStream };
 struct Product {
-  bool few = false, aligned = false;
+  Kind kind = kTiles;
+  bool aligned = false;
   int32_t shape = ar::kTile128, splits = 1, k_split = 0, tiles_m = 0, tiles_n = 0;
   int64_t ldp = 0;
 };
 
+// What a product on tiles takes, in microseconds, on this library's kernels at
+// the rates that they measured on MI355X: a tile of 128 x 128 costs `fixed` and
+// then `one` for every 128 bytes of inner length where it has a compute unit to
+// itself, `two` where two share one (256 x 256: one always does).  Parts of a
+// split inner length are written and read again by one more launch.
+struct TileCost {
+  double fixed, one, two;
+};
+constexpr TileCost kCost256 = {10.0, 1.42, 1.42};
+constexpr TileCost kCost128[2][2] = {{{5.0, 0.90, 1.55}, {5.0, 0.68, 1.18}},   // halves: through registers, asynchronous
+                                     {{5.0, 2.10, 4.00}, {5.0, 1.90, 3.60}}};  // floats
+constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 5e6;
+
+double tile_micros(const TileCost& c, int64_t workgroups, int64_t steps, bool shared) {
+  const int64_t at_once = shared ? 2 * kCus : kCus, rounds = workgroups / at_once, rest = workgroups % at_once;
+  const double last = rest == 0 ? 0.0 : c.fixed + double(steps) * (rest > kCus ? c.two : c.one);
+  return double(rounds) * (c.fixed + double(steps) * c.two) + last;
+}
+
 Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Operand& a, const Operand& b) {
   Product p;
-  const int64_t eb = size_of(type), inner = ar::kTileKBytes / eb;
+  const int64_t eb = size_of(type), inner = ar::kTileKBytes / eb, steps = std::max<int64_t>(1, ceil_div(K, inner));
   p.ldp = round_up(N, 8);
-  p.few = a.kmajor && b.kmajor && M <= ar::kFewMaxRows;
-  int64_t workgroups, want;
-  if (p.few) {
-    workgroups = ceil_div(N, 16);
-    want = kCus;
+  p.aligned = can_load_async(a, eb) && can_load_async(b, eb);
+  int64_t splits = 1;
+  const bool rows = a.kmajor && b.kmajor && M <= ar::kFewMaxRows;
+  // Few rows.  Aligned, both kernels read w at the rate of memory; the one
+  // through LDS keeps it up with more rows and longer inner lengths, the other
+  // starts sooner.  w of 4096 x 4096 bf16, M = 1 / 16 / 24 / 64, us: registers
+  // 9.0 / 10.8 / 12.7 / 21, LDS 11.4 / 11.9 / 11.9 / 13.4; of 16384 x 4096 28 /
+  // 34 / 41 / 75 and 28 / 27 / 27 / 29; of 4096 x 16384 29 / 36 / 43 / 78 and
+  // 27 / 27 / 28 / 31; K = 1024 and less 5.5-7 and 5.5-8.  Off the 16-byte
+  // boundaries the registers' kernel (4096 x 4096: 27 at M = 16, 63 at 64)
+  // leaves large ones to the tiles (20 and 22; 2047 x 1023: 6.5 against 15).
+  const int64_t row_tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  if (rows && p.aligned && (M <= 16 ? N >= 8192 || K * eb > 16384 : K * eb > 2048)) {
+    p.kind = kStream;
+    splits = std::min(kCus / ceil_div(N, 64), steps / 8);
+  } else if (rows && (p.aligned || N * K * (1 + row_tiles) <= 20000000)) {
+    p.kind = kFew;
+    splits = std::min(kCus / ceil_div(N, 16), steps / 64);
   } else {
-    p.aligned = can_load_async(a, eb) && can_load_async(b, eb);
-    const int64_t big = ceil_div(M, 256) * ceil_div(N, 256);
-    p.shape = p.aligned && big >= kCus * 3 / 4 ? ar::kTile256 : ar::kTile128;
+    const int64_t small = ceil_div(M, 128) * ceil_div(N, 128), large = ceil_div(M, 256) * ceil_div(N, 256);
+    if (small >= (int64_t(1) << 31)) refuse(AR_ERR_UNSUPPORTED, "the product would need 2^31 or more tiles");
+    const TileCost& cost = kCost128[type == AR_FLOAT32][p.aligned];
+    double best = 0.0;
+    for (int64_t s = 1; s <= std::min<int64_t>(64, std::max<int64_t>(1, steps / 2)); ++s) {
+      if (s > 1 && s * std::min(small, large) > 8 * kCus) break;  // more parts than the chip takes at once
+      const int64_t per = ceil_div(steps, s);
+      const double join = s > 1 ? kJoinMicros + double(s) * double(M) * double(p.ldp) * 8.0 / kJoinBytesPerMicro : 0.0;
+      const double t128 = tile_micros(cost, s * small, per, true) + join;
+      if (s == 1 || t128 < best) {
+        best = t128;
+        p.shape = ar::kTile128;
+        splits = s;
+      }
+      if (!p.aligned || type == AR_FLOAT32) continue;
+      const double t256 = tile_micros(kCost256, s * large, per, false) + join;
+      if (t256 < best) {
+        best = t256;
+        p.shape = ar::kTile256;
+        splits = s;
+      }
+    }
     const int64_t tile = ar::tile_rows(p.shape);
-    if (ceil_div(M, tile) * ceil_div(N, tile) >= (int64_t(1) << 31))
-      refuse(AR_ERR_UNSUPPORTED, "the product would need 2^31 or more tiles");
     p.tiles_m = int32_t(ceil_div(M, tile));
     p.tiles_n = int32_t(ceil_div(N, tile));
-    workgroups = int64_t(p.tiles_m) * p.tiles_n;
-    want = p.shape == ar::kTile256 ? kCus : 2 * kCus;
   }
-  const int64_t steps = ceil_div(K, inner);  // tiles of inner length
-  const int64_t least = p.few ? 32 : 8;      // of which a part takes at least so many
-  int64_t splits = std::min(want / std::max<int64_t>(workgroups, 1), steps / least);
   splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
-  const int64_t per = std::max<int64_t>(1, ceil_div(steps, splits));
+  const int64_t per = ceil_div(steps, splits);
   p.k_split = int32_t(std::min(per * inner, kMaxLength));
-  p.splits = int32_t(std::max<int64_t>(1, ceil_div(steps, per)));
+  p.splits = int32_t(ceil_div(steps, per));
   return p;
 }
 int64_t part_bytes(const Product& p, int64_t M) { return p.splits > 1 ? p.splits * M * p.ldp * 4 : 0; }
@@ -231,8 +277,10 @@ void run_product(const Product& p, int64_t K, ar_dtype type, const Operand& a, c
   g.ldp = p.ldp;
   g.e = e;
   const int32_t elem = elem_of(type);
-  launched(p.few ? ar::launch_gemm_few(g, elem, stream)
-                 : ar::launch_gemm(g, elem, a.kmajor, b.kmajor, p.aligned, p.shape, stream), what);
+  launched(p.kind == kFew      ? ar::launch_gemm_few(g, elem, stream)
+           : p.kind == kStream ? ar::launch_gemm_stream(g, elem, stream)
+                               : ar::launch_gemm(g, elem, a.kmajor, b.kmajor, p.aligned, p.shape, stream),
+           what);
   if (p.splits > 1) launched(ar::launch_gemm_join(g, elem, stream), what);
 }
 

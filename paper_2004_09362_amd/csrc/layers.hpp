@@ -54,6 +54,9 @@ enum GemmShape : int32_t { kTile256 = 0, kTile128 = 1 };
 constexpr int32_t kTileKBytes = 128;
 constexpr int32_t tile_rows(int32_t shape) { return shape == kTile256 ? 256 : 128; }
 
+// The largest distance of two rows in bytes at which a tile's offsets fit 32 bits.
+constexpr int64_t kMaxTileLd = int64_t(1) << 23;
+
 // elem: Elem; a_kmajor / b_kmajor as above (a k-major b with a not is not
 // provided); aligned: whether the asynchronous loads apply (see gemm.hpp).
 int launch_gemm(const GemmArgs& g, int32_t elem, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
@@ -64,6 +67,8 @@ int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool align
 // Products of few rows (both operands k-major): gemm_few.hip.
 constexpr int32_t kFewMaxRows = 64;
 int launch_gemm_few(const GemmArgs& g, int32_t elem, void* stream);
+// the same for operands that can be loaded asynchronously
+int launch_gemm_stream(const GemmArgs& g, int32_t elem, void* stream);
 
 // y of a product whose inner length was split: the parts summed in order,
 // then the epilogue (g.part, g.splits, g.ldp, g.e).
