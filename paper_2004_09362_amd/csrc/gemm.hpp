@@ -629,16 +629,22 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
         if (pass + 2 * kAhead < kPasses) fetch(res0, pass + 2 * kAhead);
         finish(res1, pass + kAhead);
       }
-    } else {  // the lanes of a row's last, partial unit
+    } else if (have > 0) {  // the lanes of a row's last, partial unit
 #pragma unroll 1
-      for (int pass = 0; pass < kPasses; ++pass) {
+      for (int pass = 0; pass < kPasses; pass += kAhead) {
         const int32_t m = mw + pass * kPassRows;
         if (m >= g.e.M) break;
-        const float* w = reinterpret_cast<const float*>(unit_at(pass * kPassRows + lane / kUnits));
-#pragma unroll 1
-        for (int i = 0; i < have; ++i) {
-          if (g.splits > 1) part[int64_t(m) * g.ldp + i] = w[i];
-          else emit_one<T>(w[i], g.e, m, n + i);
+        auto sum = [&](int q, int i) {
+          return reinterpret_cast<const float*>(unit_at((pass + q) * kPassRows + lane / kUnits))[i];
+        };
+        if (g.splits > 1) {
+#pragma unroll
+          for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+              if (m + q * kPassRows < g.e.M && i < have) part[int64_t(m + q * kPassRows) * g.ldp + i] = sum(q, i);
+        } else {
+          emit_tail<T, 8, kAhead>(sum, g.e, m, kPassRows, n, have);
         }
       }
     }

@@ -108,9 +108,7 @@ __global__ __launch_bounds__(1024) void gemm_few_kernel(GemmArgs g) {
     if (g.splits > 1) {
       *reinterpret_cast<f32x4v*>(g.part + (int64_t(blockIdx.y) * g.e.M + m) * g.ldp + n) = v;
     } else if (g.e.N - n < 4) {
-#pragma unroll
-      for (int c = 0; c < 3; ++c)
-        if (n + c < g.e.N) emit_one<T>(v[c], g.e, m, n + c);
+      emit_tail<T, 4, 1>([&](int, int c) { return v[c]; }, g.e, m, 1, n, g.e.N - n);
     } else {
       float x[4] = {v[0], v[1], v[2], v[3]}, bias[4];
       Residual<4> res[1];
@@ -214,9 +212,7 @@ __global__ __launch_bounds__(256) void gemm_stream_kernel(GemmArgs g) {
     if (g.splits > 1) {
       *reinterpret_cast<f32x4v*>(g.part + (int64_t(blockIdx.y) * g.e.M + m) * g.ldp + n) = acc[i];
     } else if (g.e.N - n < 4) {
-#pragma unroll
-      for (int c = 0; c < 3; ++c)
-        if (n + c < g.e.N) emit_one<T>(acc[i][c], g.e, m, n + c);
+      emit_tail<T, 4, 1>([&](int, int c) { return acc[i][c]; }, g.e, m, 1, n, g.e.N - n);
     } else {
       float x[4] = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
       Residual<4> res[1];

@@ -20,34 +20,35 @@ template <> constexpr Elem elem_of<f16>() { return kF16; }
 template <> constexpr Elem elem_of<bf16>() { return kBF16; }
 
 
-// The first `have` (all V where have >= V) of V elements as floats; the rest 0.
+// V elements that start on any element, as floats.
 template <int V, typename T>
-__device__ __forceinline__ void load_some(float (&x)[V], const T* p, int have) {
-  if (have >= V) {
-    typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    const U u = *reinterpret_cast<const U*>(p);
+__device__ __forceinline__ void load_group(float (&x)[V], const T* p) {
+  typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  const U u = *reinterpret_cast<const U*>(p);
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = float(u[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = i < have ? float(p[i]) : 0.0f;
-  }
+  for (int i = 0; i < V; ++i) x[i] = float(u[i]);
 }
-
 // Rounded to nearest, ties to even, where T is narrower.
 template <int V, typename T>
-__device__ __forceinline__ void store_some(T* p, const float (&x)[V], int have) {
-  if (have >= V) {
-    typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
-    U u;
+__device__ __forceinline__ void store_group(T* p, const float (&x)[V]) {
+  typedef T U __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  U u;
 #pragma unroll
-    for (int i = 0; i < V; ++i) u[i] = T(x[i]);
-    *reinterpret_cast<U*>(p) = u;
-  } else {
+  for (int i = 0; i < V; ++i) u[i] = T(x[i]);
+  *reinterpret_cast<U*>(p) = u;
+}
+// The first `have` < V of V elements, where a row ends; the rest 0.
+template <int V, typename T>
+__device__ __forceinline__ void load_tail(float (&x)[V], const T* p, int have) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < have) p[i] = T(x[i]);
-  }
+  for (int i = 0; i < V - 1; ++i) x[i] = i < have ? float(p[i]) : 0.0f;
+  x[V - 1] = 0.0f;
+}
+template <int V, typename T>
+__device__ __forceinline__ void store_tail(T* p, const float (&x)[V], int have) {
+#pragma unroll
+  for (int i = 0; i < V - 1; ++i)
+    if (i < have) p[i] = T(x[i]);
 }
 
 // The counter-based generator on four 32-bit words with seven rounds (J. K.
@@ -86,14 +87,6 @@ __device__ __forceinline__ void drop_some(float (&x)[V], const DropArgs& d, uint
     x[4 * q + 2] = w.z <= d.last ? x[4 * q + 2] * d.scale : 0.0f;
     x[4 * q + 3] = w.w <= d.last ? x[4 * q + 3] * d.scale : 0.0f;
   }
-}
-
-// drop() of one element.
-__device__ __forceinline__ float drop_one(float x, const DropArgs& d, uint64_t row, uint32_t col) {
-  if (d.none) return 0.0f;
-  const uint4 w = counter_words(col >> 2, uint32_t(row), uint32_t(row >> 32), d.site, d.k0, d.k1);
-  const uint32_t word = col & 2 ? (col & 1 ? w.w : w.z) : (col & 1 ? w.y : w.x);
-  return word <= d.last ? x * d.scale : 0.0f;
 }
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -204,9 +197,9 @@ __device__ __forceinline__ void load_bias(float (&b)[V], const Epilogue& e, int3
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] = 0.0f;
   } else if (e.bias_f32) {
-    load_some<V>(b, static_cast<const float*>(e.bias) + n, V);
+    load_group<V>(b, static_cast<const float*>(e.bias) + n);
   } else {
-    load_some<V>(b, static_cast<const T*>(e.bias) + n, V);
+    load_group<V>(b, static_cast<const T*>(e.bias) + n);
   }
 }
 
@@ -267,30 +260,50 @@ __device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const R
                                      int32_t m, int32_t n) {
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] += b[i];
-  if (e.z) store_some<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, V);
+  if (e.z) store_group<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v);
   activate<V>(v, e.act);
   if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
   add_residual<T, V>(v, r, e);
-  if (e.y_f32) store_some<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, V);
-  else store_some<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, V);
+  if (e.y_f32) store_group<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v);
+  else store_group<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v);
 }
 
-// The same for one element, where a row ends inside a group of columns.
-template <typename T>
-__device__ __forceinline__ void emit_one(float v, const Epilogue& e, int32_t m, int32_t n) {
-  if (e.bias) v += e.bias_f32 ? static_cast<const float*>(e.bias)[n] : float(static_cast<const T*>(e.bias)[n]);
-  if (e.z) static_cast<T*>(e.z)[int64_t(m) * e.ldz + n] = T(v);
-  float a[1] = {v};
-  activate<1>(a, e.act);
-  v = a[0];
-  if (e.drop.on) v = drop_one(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
-  const int64_t ry = int64_t(m) * e.ldr + n, yy = int64_t(m) * e.ldy + n;
-  if (e.y_f32) {
-    if (e.res) v += static_cast<const float*>(e.res)[ry];
-    static_cast<float*>(e.y)[yy] = v;
-  } else {
-    if (e.res) v += float(static_cast<const T*>(e.res)[ry]);
-    static_cast<T*>(e.y)[yy] = T(v);
+// The same for the `have` < V columns of a row's end, of Q rows from m on `step`
+// apart, whose sums sum(q, i) gives; all loads of the Q rows go out before the
+// first is used.
+template <typename T, int V, int Q, typename F>
+__device__ __forceinline__ void emit_tail(F&& sum, const Epilogue& e, int32_t m, int32_t step, int32_t n, int have) {
+  float b[V], r[Q][V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) b[i] = 0.0f;
+  if (e.bias) {
+    if (e.bias_f32) load_tail<V>(b, static_cast<const float*>(e.bias) + n, have);
+    else load_tail<V>(b, static_cast<const T*>(e.bias) + n, have);
+  }
+  if (e.res) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int64_t at = int64_t(m + q * step < e.M ? m + q * step : e.M - 1) * e.ldr + n;
+      if (e.y_f32) load_tail<V>(r[q], static_cast<const float*>(e.res) + at, have);
+      else load_tail<V>(r[q], static_cast<const T*>(e.res) + at, have);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < Q; ++q) {
+    const int32_t row = m + q * step;
+    if (row >= e.M) break;
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = i < have ? sum(q, i) + b[i] : 0.0f;
+    if (e.z) store_tail<V>(static_cast<T*>(e.z) + int64_t(row) * e.ldz + n, v, have);
+    activate<V>(v, e.act);
+    if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(row), uint32_t(n));
+    if (e.res) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] += r[q][i];
+    }
+    if (e.y_f32) store_tail<V>(static_cast<float*>(e.y) + int64_t(row) * e.ldy + n, v, have);
+    else store_tail<V>(static_cast<T*>(e.y) + int64_t(row) * e.ldy + n, v, have);
   }
 }
 

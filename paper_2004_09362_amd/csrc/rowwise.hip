@@ -26,16 +26,32 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, int log_t
   const int tpr = 1 << log_tpr, rpb = kThreads >> log_tpr;
   const uint32_t down = gridDim.x / across, by = blockIdx.x / across;
   const int64_t col = (int64_t(blockIdx.x - by * across) * tpr + (threadIdx.x & (tpr - 1))) * 8;
-  if (col >= c.cols) return;
-  const int have = c.cols - col < 8 ? int(c.cols - col) : 8;
-  for (int64_t row = int64_t(by) * rpb + (threadIdx.x >> log_tpr); row < c.rows; row += int64_t(down) * rpb) {
-    float v[8], r[8];
-    load_some<8>(v, static_cast<const X*>(c.x) + row * c.ldx + col, have);
-    load_some<8>(r, static_cast<const Y*>(c.res) + row * c.ldr + col, c.res ? have : 0);
-    if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+  const X* const x = static_cast<const X*>(c.x) + col;
+  const Y* const res = static_cast<const Y*>(c.res) + col;
+  Y* const y = static_cast<Y*>(c.y) + col;
+  const int64_t step = int64_t(down) * rpb, row0 = int64_t(by) * rpb + (threadIdx.x >> log_tpr);
+  float v[8], r[8];
+  if (col + 8 <= c.cols) {
+    for (int64_t row = row0; row < c.rows; row += step) {
+      load_group<8>(v, x + row * c.ldx);
+      if (c.res) load_group<8>(r, res + row * c.ldr);
+      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+      if (c.res) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += r[i];
-    store_some<8>(static_cast<Y*>(c.y) + row * c.ldy + col, v, have);
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+      }
+      store_group<8>(y + row * c.ldy, v);
+    }
+  } else if (col < c.cols) {
+    const int have = int(c.cols - col);
+    for (int64_t row = row0; row < c.rows; row += step) {
+      load_tail<8>(v, x + row * c.ldx, have);
+      load_tail<8>(r, res + row * c.ldr, c.res ? have : 0);
+      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += r[i];
+      store_tail<8>(y + row * c.ldy, v, have);
+    }
   }
 }
 
@@ -52,26 +68,41 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
   const int64_t r0 = int64_t(blockIdx.y) * c.rows_per;
   const int64_t r1 = r0 + c.rows_per < c.M ? r0 + c.rows_per : c.M;
   float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (have > 0) {
+  const D* const dy = static_cast<const D*>(c.dy) + col;
+  const Z* const z = static_cast<const Z*>(c.z) + col;
+  Z* const dz = static_cast<Z*>(c.dz) + col;
+  if (have == 8) {
     for (int64_t row0 = r0 + rt; row0 < r1; row0 += 8 * kRows) {
-      float v[kRows][8], z[kRows][8];
+      float v[kRows][8], t[kRows][8];
 #pragma unroll
-      for (int q = 0; q < kRows; ++q) {
-        const int64_t row = row0 + 8 * q;
-        const int there = row < r1 ? have : 0;
-        load_some<8>(v[q], static_cast<const D*>(c.dy) + row * c.lddy + col, there);
-        if (c.z) load_some<8>(z[q], static_cast<const Z*>(c.z) + row * c.ldz + col, there);
+      for (int q = 0; q < kRows; ++q)  // of rows past the chunk's last, that one's
+        load_group<8>(v[q], dy + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.lddy);
+      if (c.z) {
+#pragma unroll
+        for (int q = 0; q < kRows; ++q)
+          load_group<8>(t[q], z + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.ldz);
       }
 #pragma unroll
       for (int q = 0; q < kRows; ++q) {
         const int64_t row = row0 + 8 * q;
         if (row >= r1) break;
         if (c.drop.on) drop_some<8>(v[q], c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
-        if (c.z) times_slope<8>(v[q], z[q], c.act);
+        if (c.z) times_slope<8>(v[q], t[q], c.act);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] += i < have ? v[q][i] : 0.0f;
-        if (c.dz) store_some<8>(static_cast<Z*>(c.dz) + row * c.lddz + col, v[q], have);
+        for (int i = 0; i < 8; ++i) s[i] += v[q][i];
+        if (c.dz) store_group<8>(dz + row * c.lddz, v[q]);
       }
+    }
+  } else if (have > 0) {
+    for (int64_t row = r0 + rt; row < r1; row += 8) {
+      float v[8], t[8];
+      load_tail<8>(v, dy + row * c.lddy, have);
+      load_tail<8>(t, z + row * c.ldz, c.z ? have : 0);
+      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+      if (c.z) times_slope<8>(v, t, c.act);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += i < have ? v[i] : 0.0f;
+      if (c.dz) store_tail<8>(dz + row * c.lddz, v, have);
     }
   }
   if (!c.sums) return;
@@ -118,11 +149,12 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log
   const float* part = g.part + m * g.ldp + n;
   const int64_t step = int64_t(g.e.M) * g.ldp;
   if (g.e.N - n < 8) {
-    for (int i = 0; i < int(g.e.N - n); ++i) {
-      float v = 0.0f;
-      for (int32_t s = 0; s < g.splits; ++s) v += part[s * step + i];
-      emit_one<T>(v, g.e, int32_t(m), int32_t(n) + i);
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int32_t s = 0; s < g.splits; ++s) {  // ldp is a multiple of 8: 8 columns lie there, not all written
+#pragma unroll
+      for (int i = 0; i < 7; ++i) v[i] += n + i < g.e.N ? part[s * step + i] : 0.0f;
     }
+    emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), int(g.e.N - n));
     return;
   }
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8];
