@@ -5,6 +5,7 @@
 // All are bound by memory.  A thread takes 8 consecutive columns of a row (16
 // bytes of halves), at any alignment; 8 columns are two counters of the
 // generator.
+#include "device_common.hpp"
 #include "layer_device.hpp"
 
 namespace ar {
@@ -21,37 +22,36 @@ int threads_per_row(int64_t cols) {
   return t;
 }
 
+// A thread's group of 8 columns: groups are numbered through the rows, so that
+// no thread is left over at the end of a row of any length.  A launch takes
+// rows from row0 on, with fewer than 2^32 groups.
 template <typename X, typename Y>
-__global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, int log_tpr, uint32_t across) {
-  const int tpr = 1 << log_tpr, rpb = kThreads >> log_tpr;
-  const uint32_t down = gridDim.x / across, by = blockIdx.x / across;
-  const int64_t col = (int64_t(blockIdx.x - by * across) * tpr + (threadIdx.x & (tpr - 1))) * 8;
-  const X* const x = static_cast<const X*>(c.x) + col;
-  const Y* const res = static_cast<const Y*>(c.res) + col;
-  Y* const y = static_cast<Y*>(c.y) + col;
-  const int64_t step = int64_t(down) * rpb, row0 = int64_t(by) * rpb + (threadIdx.x >> log_tpr);
+__global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, FastDiv groups, int64_t row0, uint32_t count) {
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
+  if (id >= count) return;
+  const uint32_t down = fdiv(id, groups), col = (id - down * groups.d) * 8;
+  const int64_t row = row0 + down;
+  const X* const x = static_cast<const X*>(c.x) + row * c.ldx + col;
+  const Y* const res = static_cast<const Y*>(c.res) + row * c.ldr + col;
+  Y* const y = static_cast<Y*>(c.y) + row * c.ldy + col;
   float v[8], r[8];
   if (col + 8 <= c.cols) {
-    for (int64_t row = row0; row < c.rows; row += step) {
-      load_group<8>(v, x + row * c.ldx);
-      if (c.res) load_group<8>(r, res + row * c.ldr);
-      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
-      if (c.res) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += r[i];
-      }
-      store_group<8>(y + row * c.ldy, v);
-    }
-  } else if (col < c.cols) {
-    const int have = int(c.cols - col);
-    for (int64_t row = row0; row < c.rows; row += step) {
-      load_tail<8>(v, x + row * c.ldx, have);
-      load_tail<8>(r, res + row * c.ldr, c.res ? have : 0);
-      if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
+    load_group<8>(v, x);
+    if (c.res) load_group<8>(r, res);
+    if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), col);
+    if (c.res) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += r[i];
-      store_tail<8>(y + row * c.ldy, v, have);
     }
+    store_group<8>(y, v);
+  } else {
+    const int have = int(c.cols - col);
+    load_tail<8>(v, x, have);
+    load_tail<8>(r, res, c.res ? have : 0);
+    if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), col);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    store_tail<8>(y, v, have);
   }
 }
 
@@ -179,19 +179,22 @@ int log2_of(int v) {
 
 template <typename X>
 int launch_dropout_x(const DropCall& c, int32_t ye, hipStream_t st) {
-  const int tpr = threads_per_row(c.cols), lg = log2_of(tpr), rpb = kThreads / tpr;
-  // workgroups across a row (at most 2^19) times those down the rows, 2^22 or
-  // one pass over the rows at most
-  const int64_t across = (c.cols + int64_t(tpr) * 8 - 1) / (int64_t(tpr) * 8), blocks = (c.rows + rpb - 1) / rpb;
-  const int64_t most = (int64_t(1) << 22) / across > 0 ? (int64_t(1) << 22) / across : 1;
-  const dim3 grid(uint32_t(across * (blocks < most ? blocks : most)));
-  switch (ye) {
-    case kF32: dropout_kernel<X, float><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
-    case kF16: dropout_kernel<X, f16><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
-    case kBF16: dropout_kernel<X, bf16><<<grid, dim3(kThreads), 0, st>>>(c, lg, uint32_t(across)); break;
-    default: return int(hipErrorInvalidValue);
+  const int64_t groups = (c.cols + 7) / 8, most = (int64_t(1) << 31) / groups;  // groups <= 2^27
+  const FastDiv div = make_fastdiv(uint32_t(groups));
+  for (int64_t row0 = 0; row0 < c.rows; row0 += most) {
+    const int64_t rows = c.rows - row0 < most ? c.rows - row0 : most;
+    const uint32_t count = uint32_t(rows * groups);
+    const dim3 grid((count + kThreads - 1) / kThreads);
+    switch (ye) {
+      case kF32: dropout_kernel<X, float><<<grid, dim3(kThreads), 0, st>>>(c, div, row0, count); break;
+      case kF16: dropout_kernel<X, f16><<<grid, dim3(kThreads), 0, st>>>(c, div, row0, count); break;
+      case kBF16: dropout_kernel<X, bf16><<<grid, dim3(kThreads), 0, st>>>(c, div, row0, count); break;
+      default: return int(hipErrorInvalidValue);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return int(e);
   }
-  return int(hipGetLastError());
+  return int(hipSuccess);
 }
 
 template <typename Z>
