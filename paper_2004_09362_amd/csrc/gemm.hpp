@@ -344,24 +344,26 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
   n = in / h;
 }
 
+// LDS of a workgroup: five places, each for one operand of a tile.
+constexpr int ring_bytes(int tile) { return 5 * tile * kTileKBytes; }
+
+// Part `part` of tile `tile` of a product.
 template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC>
-__global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kernel(GemmArgs g) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint32_t part_of, char* lds) {
   constexpr int THREADS = WM * WN * 64, TM = WM * MT * 16, TN = WN * NT * 16;
   using OpA = Operand<T, AK, false, TM, THREADS>;
   using OpB = Operand<T, BK, true, TN, THREADS>;
-  // LDS: five places, each for one operand of a tile
   constexpr uint32_t kPlace = OpA::kBytes, kRing = 5 * kPlace;
   static_assert(OpB::kBytes == kPlace, "places of one size");
   constexpr int kInner = OpA::kInner;
   constexpr bool kPinned = MT * NT == 64;
-  __shared__ __attribute__((aligned(1024))) char lds[kRing];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
   uint32_t im, in;
-  tile_of(blockIdx.x, uint32_t(g.tiles_m), uint32_t(g.tiles_n), im, in);
+  tile_of(tile, uint32_t(g.tiles_m), uint32_t(g.tiles_n), im, in);
   const int32_t m0 = int32_t(im) * TM, n0 = int32_t(in) * TN;
-  const int32_t k0 = int32_t(blockIdx.y) * g.k_split;
+  const int32_t k0 = int32_t(part_of) * g.k_split;
   const int32_t klen = g.K - k0 < g.k_split ? g.K - k0 : g.k_split;
 
   OpA a;
@@ -570,7 +572,7 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   const bool swap = !BK && (lane & 16);
   const int32_t unit = lane % kUnits, n = n0 + wn * NT * 16 + 8 * unit;
   const int have = g.e.N - n;
-  float* part = g.part + int64_t(blockIdx.y) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
+  float* part = g.part + int64_t(part_of) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
   float bias[8];
   load_bias<T, 8>(bias, g.e, n);
   auto spread = [&](auto round) {
@@ -651,6 +653,28 @@ __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kerne
   }
 }
 
+template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC>
+__global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kernel(GemmArgs g) {
+  __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(WM * MT * 16)];
+  gemm_tile<T, AK, BK, MT, NT, WM, WN, ASYNC>(g, blockIdx.x, blockIdx.y, lds);
+}
+
+// The gradient's two products in one launch, x's first: for small ones, which
+// fill the chip together and have the latency of one.
+template <typename T, bool ASYNC>
+__global__ __launch_bounds__(256, 2) void gemm_pair_kernel(GemmArgs x, GemmArgs w) {
+  __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(128)];
+  const uint32_t tx = uint32_t(x.tiles_m) * uint32_t(x.tiles_n), tw = uint32_t(w.tiles_m) * uint32_t(w.tiles_n);
+  const uint32_t first = tx * uint32_t(x.splits);
+  if (blockIdx.x < first) {
+    const uint32_t part = blockIdx.x / tx;
+    gemm_tile<T, true, false, 4, 4, 2, 2, ASYNC>(x, blockIdx.x - part * tx, part, lds);
+  } else {
+    const uint32_t id = blockIdx.x - first, part = id / tw;
+    gemm_tile<T, false, false, 4, 4, 2, 2, ASYNC>(w, id - part * tw, part, lds);
+  }
+}
+
 template <typename T, bool AK, bool BK>
 int launch_layout(const GemmArgs& g, bool aligned, int32_t shape, hipStream_t st) {
   const dim3 grid(uint32_t(g.tiles_m) * uint32_t(g.tiles_n), uint32_t(g.splits));
@@ -671,6 +695,16 @@ int launch_gemm_of(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned
   if (a_kmajor) return b_kmajor ? launch_layout<T, true, true>(g, aligned, shape, st)
                                 : launch_layout<T, true, false>(g, aligned, shape, st);
   return b_kmajor ? int(hipErrorInvalidValue) : launch_layout<T, false, false>(g, aligned, shape, st);
+}
+
+template <typename T>
+int launch_pair_of(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const dim3 grid(uint32_t(x.tiles_m) * uint32_t(x.tiles_n) * uint32_t(x.splits) +
+                  uint32_t(w.tiles_m) * uint32_t(w.tiles_n) * uint32_t(w.splits));
+  if (aligned) gemm_pair_kernel<T, true><<<grid, dim3(256), 0, st>>>(x, w);
+  else gemm_pair_kernel<T, false><<<grid, dim3(256), 0, st>>>(x, w);
+  return int(hipGetLastError());
 }
 
 }  // namespace ar

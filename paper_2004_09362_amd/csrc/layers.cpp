@@ -24,6 +24,15 @@ int launch_gemm(const GemmArgs& g, int32_t elem, bool a_kmajor, bool b_kmajor, b
   return int(hipErrorInvalidValue);
 }
 
+int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, void* stream) {
+  switch (elem) {
+    case kF32: return launch_gemm_pair_f32(x, w, aligned, stream);
+    case kF16: return launch_gemm_pair_f16(x, w, aligned, stream);
+    case kBF16: return launch_gemm_pair_bf16(x, w, aligned, stream);
+  }
+  return int(hipErrorInvalidValue);
+}
+
 }  // namespace ar
 
 namespace {
@@ -261,8 +270,7 @@ Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Opera
 }
 int64_t part_bytes(const Product& p, int64_t M) { return p.splits > 1 ? p.splits * M * p.ldp * 4 : 0; }
 
-void run_product(const Product& p, int64_t K, ar_dtype type, const Operand& a, const Operand& b, const ar::Epilogue& e,
-                 void* part, hipStream_t stream, const char* what) {
+ar::GemmArgs gemm_args(const Product& p, int64_t K, const Operand& a, const Operand& b, const ar::Epilogue& e, void* part) {
   ar::GemmArgs g{};
   g.a = a.data;
   g.b = b.data;
@@ -276,12 +284,15 @@ void run_product(const Product& p, int64_t K, ar_dtype type, const Operand& a, c
   g.part = static_cast<float*>(part);
   g.ldp = p.ldp;
   g.e = e;
-  const int32_t elem = elem_of(type);
+  return g;
+}
+
+void run_product(const Product& p, const ar::GemmArgs& g, int32_t elem, bool a_kmajor, bool b_kmajor, hipStream_t stream,
+                 const char* what) {
   launched(p.kind == kFew      ? ar::launch_gemm_few(g, elem, stream)
            : p.kind == kStream ? ar::launch_gemm_stream(g, elem, stream)
-                               : ar::launch_gemm(g, elem, a.kmajor, b.kmajor, p.aligned, p.shape, stream),
+                               : ar::launch_gemm(g, elem, a_kmajor, b_kmajor, p.aligned, p.shape, stream),
            what);
-  if (p.splits > 1) launched(ar::launch_gemm_join(g, elem, stream), what);
 }
 
 Operand rows_of(const ar_matrix* m, int64_t rows) { return {m->data, m->ld, true, rows}; }
@@ -293,8 +304,9 @@ struct Backward {
   int32_t chunks = 1;
   int64_t rows_per = 0, sums_bytes = 0;
   Product px, pw;
-  int64_t part = 0;
-  int64_t total() const { return dz_bytes + sums_bytes + part; }
+  bool pair = false;        // both products in one launch
+  int64_t part_x = 0, part_w = 0;
+  int64_t total() const { return dz_bytes + sums_bytes + part_x + part_w; }
 };
 
 Backward plan_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, const ar_matrix* x, const ar_matrix* w,
@@ -315,12 +327,17 @@ Backward plan_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, con
   const Operand dz = {p.make_dz ? nullptr : dy->data, p.make_dz ? p.lddz : dy->ld, true, M};
   if (dx) {
     p.px = plan_product(M, K, N, type, dz, {w->data, w->ld, false, K});
-    p.part = std::max(p.part, part_bytes(p.px, M));
+    p.part_x = round_up(part_bytes(p.px, M), kWorkspaceAlign);
   }
   if (dw) {
     p.pw = plan_product(N, K, M, type, {dz.data, dz.ld, false, N}, {x->data, x->ld, false, K});
-    p.part = std::max(p.part, part_bytes(p.pw, N));
+    p.part_w = round_up(part_bytes(p.pw, N), kWorkspaceAlign);
   }
+  // Small products share a launch where both fit the chip at once: 200 x 1001 x
+  // 777 fp16 takes 18 us where the two in turn took 34.
+  auto workgroups = [](const Product& q) { return int64_t(q.tiles_m) * q.tiles_n * q.splits; };
+  p.pair = dx && dw && M > 0 && N > 0 && K > 0 && p.px.shape == ar::kTile128 && p.pw.shape == ar::kTile128 &&
+           p.px.aligned == p.pw.aligned && workgroups(p.px) + workgroups(p.pw) <= 2 * kCus;
   return p;
 }
 
@@ -445,7 +462,9 @@ ar_status ar_linear_forward(int64_t M, int64_t N, int64_t K, const ar_matrix* x,
       e.z = preact->data;
       e.ldz = preact->ld;
     }
-    run_product(p, K, x->dtype, a, b, e, workspace, stream, "linear kernel launch");
+    const ar::GemmArgs g = gemm_args(p, K, a, b, e, workspace);
+    run_product(p, g, elem_of(x->dtype), true, true, stream, "linear kernel launch");
+    if (p.splits > 1) launched(ar::launch_join(g, ar::GemmArgs{}, ar::SumsCall{}, elem_of(x->dtype), stream), "join kernel launch");
   });
 }
 
@@ -502,24 +521,31 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
       c.rows_per = p.rows_per;
       c.drop = drop_args(drop);
       launched(ar::launch_slope(c, elem_of(dy->dtype), elem_of(type), stream), "linear gradient kernel launch");
-      if (db)
-        launched(ar::launch_column_sums(sums, p.chunks, N, db->data, elem_of(db->dtype), accumulate != 0, stream),
-                 "column sum kernel launch");
+    }
+    ar::SumsCall s{};
+    if (db && N > 0) {
+      s.sums = sums;
+      s.db = db->data;
+      s.N = N;
+      s.chunks = p.chunks;
+      s.elem = elem_of(db->dtype);
+      s.accumulate = accumulate != 0;
     }
     const void* const gz = p.make_dz ? dz : dy->data;
     const int64_t ldg = p.make_dz ? p.lddz : dy->ld;
     ar::Epilogue e{};
     e.drop = drop_args(nullptr);
-    if (dx && M > 0 && K > 0) {
+    ar::GemmArgs gx{}, gw{};
+    const bool run_x = dx && M > 0 && K > 0, run_w = dw && N > 0 && K > 0;
+    if (run_x) {
       e.y = dx->data;
       e.ldy = dx->ld;
       e.M = int32_t(M);
       e.N = int32_t(K);
       e.y_f32 = dx->dtype == AR_FLOAT32;
-      run_product(p.px, N, type, {gz, ldg, true, M}, {w->data, w->ld, false, K}, e, part, stream,
-                  "input gradient kernel launch");
+      gx = gemm_args(p.px, N, {gz, ldg, true, M}, {w->data, w->ld, false, K}, e, part);
     }
-    if (dw && N > 0 && K > 0) {
+    if (run_w) {
       e.y = dw->data;
       e.ldy = dw->ld;
       e.M = int32_t(N);
@@ -529,9 +555,15 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
         e.res = dw->data;
         e.ldr = dw->ld;
       }
-      run_product(p.pw, M, type, {gz, ldg, false, N}, {x->data, x->ld, false, K}, e, part, stream,
-                  "weight gradient kernel launch");
+      gw = gemm_args(p.pw, M, {gz, ldg, false, N}, {x->data, x->ld, false, K}, e, static_cast<char*>(part) + p.part_x);
     }
+    if (run_x && run_w && p.pair) {
+      launched(ar::launch_gemm_pair(gx, gw, elem_of(type), p.px.aligned, stream), "gradient kernel launch");
+    } else {
+      if (run_x) run_product(p.px, gx, elem_of(type), true, false, stream, "input gradient kernel launch");
+      if (run_w) run_product(p.pw, gw, elem_of(type), false, false, stream, "weight gradient kernel launch");
+    }
+    launched(ar::launch_join(gx, gw, s, elem_of(type), stream), "join kernel launch");
   });
 }
 

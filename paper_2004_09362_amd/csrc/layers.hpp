@@ -64,15 +64,31 @@ int launch_gemm_f32(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligne
 int launch_gemm_f16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
 int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
 
+// The gradient's products with respect to x (a k-major, b not) and w (neither)
+// in one launch, on tiles of 128 x 128.
+int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, void* stream);
+int launch_gemm_pair_f32(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
+int launch_gemm_pair_f16(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
+int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
+
 // Products of few rows (both operands k-major): gemm_few.hip.
 constexpr int32_t kFewMaxRows = 64;
 int launch_gemm_few(const GemmArgs& g, int32_t elem, void* stream);
 // the same for operands that can be loaded asynchronously
 int launch_gemm_stream(const GemmArgs& g, int32_t elem, void* stream);
 
-// y of a product whose inner length was split: the parts summed in order,
-// then the epilogue (g.part, g.splits, g.ldp, g.e).
-int launch_gemm_join(const GemmArgs& g, int32_t elem, void* stream);
+// db[n] = (accumulate ? db[n] : 0) + sum over chunks of sums[chunk][n]
+struct SumsCall {
+  const float* sums;  // NULL: none
+  void* db;
+  int64_t N;
+  int32_t chunks, elem, accumulate;
+};
+
+// What the launches before left in parts, in one launch: y of up to two
+// products whose inner length was split (splits > 1; the others are passed
+// over), the parts summed in order and then the epilogue; and column sums.
+int launch_join(const GemmArgs& g, const GemmArgs& h, const SumsCall& s, int32_t elem, void* stream);
 
 // y = res + drop(x), element types xe (x) and ye (y, res).
 struct DropCall {
@@ -98,8 +114,5 @@ struct SlopeCall {
   DropArgs drop;
 };
 int launch_slope(const SlopeCall& c, int32_t dye, int32_t ze, void* stream);
-
-// db[n] = (accumulate ? db[n] : 0) + sum over chunks of sums[chunk][n]
-int launch_column_sums(const float* sums, int32_t chunks, int64_t N, void* db, int32_t dbe, bool accumulate, void* stream);
 
 }  // namespace ar

@@ -1,6 +1,6 @@
 // rowwise.hip -- the layer operators that read and write each element once:
 // dropout, the gradient through an activation and dropout with its column
-// sums, and the joins of split products and sums.
+// sums, and the joins of split products and of sums.
 //
 // All are bound by memory.  A thread takes 8 consecutive columns of a row (16
 // bytes of halves), at any alignment; 8 columns are two counters of the
@@ -13,14 +13,6 @@ namespace ar {
 namespace {
 
 constexpr int kThreads = 256;
-
-// Threads along a row: a power of two, as many as 8-column groups, at most a
-// workgroup's.
-int threads_per_row(int64_t cols) {
-  int t = 1;
-  while (t < kThreads && int64_t(t) * 8 < cols) t *= 2;
-  return t;
-}
 
 // A thread's group of 8 columns: groups are numbered through the rows, so that
 // no thread is left over at the end of a row of any length.  A launch takes
@@ -120,41 +112,39 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
 
 // 16 columns a workgroup, 16 threads to each column's chunks.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void column_sums_kernel(const float* sums, int32_t chunks, int64_t N, T* db,
-                                                               int accumulate) {
-  __shared__ float part[16][17];
+__device__ __forceinline__ void column_sums(const SumsCall& c, uint32_t block, float (&part)[16][17]) {
   const int ct = threadIdx.x & 15, rt = threadIdx.x >> 4;
-  const int64_t n = int64_t(blockIdx.x) * 16 + ct;
+  const int64_t n = int64_t(block) * 16 + ct;
   float s = 0.0f;
-  if (n < N) {
+  if (n < c.N) {
 #pragma unroll 8
-    for (int32_t c = rt; c < chunks; c += 16) s += sums[int64_t(c) * N + n];
+    for (int32_t k = rt; k < c.chunks; k += 16) s += c.sums[int64_t(k) * c.N + n];
   }
   part[rt][ct] = s;
   __syncthreads();
-  if (rt == 0 && n < N) {
-    float t = accumulate ? float(db[n]) : 0.0f;
+  if (rt == 0 && n < c.N) {
+    T* const db = static_cast<T*>(c.db);
+    float t = c.accumulate ? float(db[n]) : 0.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) t += part[r][ct];
     db[n] = T(t);
   }
 }
 
+// A thread joins 8 columns of a row; groups are numbered through the rows.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log_tpr) {
-  const int tpr = 1 << log_tpr, rpb = kThreads >> log_tpr;
-  const int64_t n = (int64_t(blockIdx.y) * tpr + (threadIdx.x & (tpr - 1))) * 8;
-  const int64_t m = int64_t(blockIdx.x) * rpb + (threadIdx.x >> log_tpr);
-  if (n >= g.e.N || m >= g.e.M) return;
-  const float* part = g.part + m * g.ldp + n;
+__device__ __forceinline__ void join(const GemmArgs& g, const FastDiv& groups, uint32_t id) {
+  const uint32_t m = fdiv(id, groups), n = (id - m * groups.d) * 8;
+  if (m >= uint32_t(g.e.M)) return;
+  const float* part = g.part + int64_t(m) * g.ldp + n;
   const int64_t step = int64_t(g.e.M) * g.ldp;
-  if (g.e.N - n < 8) {
+  if (uint32_t(g.e.N) - n < 8) {
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     for (int32_t s = 0; s < g.splits; ++s) {  // ldp is a multiple of 8: 8 columns lie there, not all written
 #pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] += n + i < g.e.N ? part[s * step + i] : 0.0f;
+      for (int i = 0; i < 7; ++i) v[i] += n + i < uint32_t(g.e.N) ? part[s * step + i] : 0.0f;
     }
-    emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), int(g.e.N - n));
+    emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), g.e.N - int32_t(n));
     return;
   }
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8];
@@ -171,10 +161,21 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, int log
   emit<T, 8>(v, bias, res[0], g.e, int32_t(m), int32_t(n));
 }
 
-int log2_of(int v) {
-  int l = 0;
-  while ((1 << l) < v) ++l;
-  return l;
+// Workgroups: those of g, of h, and of the column sums.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void gemm_join_kernel(GemmArgs g, GemmArgs h, FastDiv gdiv, FastDiv hdiv,
+                                                             uint32_t gblocks, uint32_t hblocks, SumsCall c) {
+  __shared__ float part[16][17];
+  if (blockIdx.x < gblocks) {
+    join<T>(g, gdiv, blockIdx.x * kThreads + threadIdx.x);
+  } else if (blockIdx.x < gblocks + hblocks) {
+    join<T>(h, hdiv, (blockIdx.x - gblocks) * kThreads + threadIdx.x);
+  } else {
+    const uint32_t block = blockIdx.x - gblocks - hblocks;
+    if (c.elem == kF32) column_sums<float>(c, block, part);
+    else if (c.elem == kF16) column_sums<f16>(c, block, part);
+    else column_sums<bf16>(c, block, part);
+  }
 }
 
 template <typename X>
@@ -228,26 +229,23 @@ int launch_slope(const SlopeCall& c, int32_t dye, int32_t ze, void* stream) {
   return int(hipErrorInvalidValue);
 }
 
-int launch_column_sums(const float* sums, int32_t chunks, int64_t N, void* db, int32_t dbe, bool accumulate, void* stream) {
+int launch_join(const GemmArgs& g, const GemmArgs& h, const SumsCall& c, int32_t elem, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid(uint32_t((N + 15) / 16));
-  switch (dbe) {
-    case kF32: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<float*>(db), accumulate); break;
-    case kF16: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<f16*>(db), accumulate); break;
-    case kBF16: column_sums_kernel<<<grid, dim3(kThreads), 0, st>>>(sums, chunks, N, static_cast<bf16*>(db), accumulate); break;
-    default: return int(hipErrorInvalidValue);
+  FastDiv div[2];
+  uint32_t blocks[2];
+  const GemmArgs* const both[2] = {&g, &h};
+  for (int i = 0; i < 2; ++i) {
+    const int64_t groups = (int64_t(both[i]->e.N) + 7) / 8, threads = both[i]->splits > 1 ? groups * both[i]->e.M : 0;
+    if (threads > (int64_t(1) << 31)) return int(hipErrorInvalidValue);  // products this large are not split
+    div[i] = make_fastdiv(uint32_t(groups > 0 ? groups : 1));
+    blocks[i] = uint32_t((threads + kThreads - 1) / kThreads);
   }
-  return int(hipGetLastError());
-}
-
-int launch_gemm_join(const GemmArgs& g, int32_t elem, void* stream) {
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  const int tpr = threads_per_row(g.e.N), lg = log2_of(tpr), rpb = kThreads / tpr;
-  const dim3 grid(uint32_t((int64_t(g.e.M) + rpb - 1) / rpb), uint32_t((g.e.N + int64_t(tpr) * 8 - 1) / (int64_t(tpr) * 8)));
+  const uint32_t all = blocks[0] + blocks[1] + (c.sums ? uint32_t((c.N + 15) / 16) : 0);
+  if (all == 0) return int(hipSuccess);
   switch (elem) {
-    case kF32: gemm_join_kernel<float><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
-    case kF16: gemm_join_kernel<f16><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
-    case kBF16: gemm_join_kernel<bf16><<<grid, dim3(kThreads), 0, st>>>(g, lg); break;
+    case kF32: gemm_join_kernel<float><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
+    case kF16: gemm_join_kernel<f16><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
+    case kBF16: gemm_join_kernel<bf16><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
     default: return int(hipErrorInvalidValue);
   }
   return int(hipGetLastError());
