@@ -84,11 +84,13 @@ __device__ __forceinline__ void mma_pinned(const i32x4v& rows_n, const i32x4v& r
   }
 }
 __device__ __forceinline__ void mma_ready() { asm volatile("s_nop 1"); }
-// last: the sums of the last products, those that may still be on their way.
-__device__ __forceinline__ void mma_done(f32x4v (&last)[8]) {
+// For the sums of the last three rows of products: those that may still be on
+// their way, and some more.
+__device__ __forceinline__ void mma_done(f32x4v (&a)[8], f32x4v (&b)[8], f32x4v (&c)[8]) {
   asm volatile("s_nop 15\n\ts_nop 15"
-               : "+a"(last[0]), "+a"(last[1]), "+a"(last[2]), "+a"(last[3]), "+a"(last[4]), "+a"(last[5]), "+a"(last[6]),
-                 "+a"(last[7])::"memory");
+               : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]), "+a"(a[4]), "+a"(a[5]), "+a"(a[6]), "+a"(a[7])::"memory");
+  asm volatile("" : "+a"(b[0]), "+a"(b[1]), "+a"(b[2]), "+a"(b[3]), "+a"(b[4]), "+a"(b[5]), "+a"(b[6]), "+a"(b[7]));
+  asm volatile("" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]), "+a"(c[4]), "+a"(c[5]), "+a"(c[6]), "+a"(c[7]));
 }
 
 // 16 bytes that start on any element.
@@ -473,7 +475,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
 #pragma unroll
       for (int x = 0; x < 2 * kProducts; ++x) product(x / kProducts, x % kProducts);
     }
-    if constexpr (kPinned) mma_done(acc[MT - 1]);
+    if constexpr (kPinned) mma_done(acc[MT - 1], acc[MT - 2], acc[MT - 3]);
   } else {
     // Tiles go through registers, two sets of them: while tile t is
     // multiplied, t + 2 is on its way and t + 1, which has arrived, is written
