@@ -573,10 +573,10 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
   char* share = lds + wave * kShare;
   const bool swap = !BK && (lane & 16);
   const int32_t unit = lane % kUnits, n = n0 + wn * NT * 16 + 8 * unit;
-  const int have = g.e.N - n;
+  const int have = g.e.N - n, back = have < 8 ? 8 - have : 0;
   float* part = g.part + int64_t(part_of) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
   float bias[8];
-  load_bias<T, 8>(bias, g.e, n);
+  load_bias<T, 8>(bias, g.e, n, have > 0 ? back : 0);
   auto spread = [&](auto round) {
     constexpr int first = decltype(round)::value * kTilesRound;
 #pragma unroll
@@ -601,11 +601,11 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     const int32_t mw = m0 + (wm * MT + round * kTilesRound) * 16 + lane / kUnits;
     auto unit_at = [&](int r) { return share + (r * kUnits + (unit ^ (r & (kUnits - 1)))) * 32; };
-    if (have >= 8) {
+    if (have > 0 && (g.e.N >= 8 || g.splits > 1)) {
       // the residual of half the passes is on its way while half are worked on
       Residual<8> res0[kAhead], res1[kAhead];
       auto fetch = [&](Residual<8> (&res)[kAhead], int pass) {
-        if (g.splits == 1) load_residuals<T, 8, kAhead>(res, g.e, mw + pass * kPassRows, kPassRows, n);
+        if (g.splits == 1) load_residuals<T, 8, kAhead>(res, g.e, mw + pass * kPassRows, kPassRows, n - back);
       };
       auto finish = [&](const Residual<8> (&res)[kAhead], int pass) {
 #pragma unroll
@@ -621,7 +621,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
             to[1] = y;
           } else {
             float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            emit<T, 8>(v, bias, res[q], g.e, m, n);
+            emit<T, 8>(v, bias, res[q], g.e, m, n, back);
           }
         }
       };
@@ -633,7 +633,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
         if (pass + 2 * kAhead < kPasses) fetch(res0, pass + 2 * kAhead);
         finish(res1, pass + kAhead);
       }
-    } else if (have > 0) {  // the lanes of a row's last, partial unit
+    } else if (have > 0) {  // rows shorter than a unit
 #pragma unroll 1
       for (int pass = 0; pass < kPasses; pass += kAhead) {
         const int32_t m = mw + pass * kPassRows;
@@ -641,15 +641,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
         auto sum = [&](int q, int i) {
           return reinterpret_cast<const float*>(unit_at((pass + q) * kPassRows + lane / kUnits))[i];
         };
-        if (g.splits > 1) {
-#pragma unroll
-          for (int q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (int i = 0; i < 7; ++i)
-              if (m + q * kPassRows < g.e.M && i < have) part[int64_t(m + q * kPassRows) * g.ldp + i] = sum(q, i);
-        } else {
-          emit_tail<T, 8, kAhead>(sum, g.e, m, kPassRows, n, have);
-        }
+        emit_tail<T, 8, kAhead>(sum, g.e, m, kPassRows, n, have);
       }
     }
   }

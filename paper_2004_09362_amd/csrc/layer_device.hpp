@@ -37,7 +37,42 @@ __device__ __forceinline__ void store_group(T* p, const float (&x)[V]) {
   for (int i = 0; i < V; ++i) u[i] = T(x[i]);
   *reinterpret_cast<U*>(p) = u;
 }
-// The first `have` < V of V elements, where a row ends; the rest 0.
+// Where a row of V elements at least ends within a group, its last V elements
+// are loaded, `back` before the group's own, and moved down to their places; 0
+// follows.  So a row of any length is loaded as wide as any other, and the one
+// group costs a few moves (element by element, the last group of 1001 columns
+// held up its workgroup for several times the latency of memory).
+template <int V>
+__device__ __forceinline__ void move_down(float (&x)[V], int back) {
+  if (back == 0) return;
+#pragma unroll
+  for (int step = V / 2; step > 0; step /= 2)
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = back & step ? (i + step < V ? x[i + step] : 0.0f) : x[i];
+}
+// The elements of a group that lie in the row, all but `back` < V.
+template <int V, typename T>
+__device__ __forceinline__ void store_most(T* p, const float (&x)[V], int back) {
+  if (back == 0) {
+    store_group<V>(p, x);
+  } else {
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) y[i] = x[i];
+#pragma unroll
+    for (int step = V / 2; step > 0; step /= 2) {
+      if ((V - back) & step) {
+        if (step == 4) store_group<4>(p, {y[0], y[1], y[2 % V], y[3 % V]});
+        if (step == 2) store_group<2>(p, {y[0], y[1]});
+        if (step == 1) store_group<1>(p, {y[0]});
+        p += step;
+#pragma unroll
+        for (int i = 0; i + step < V; ++i) y[i] = y[i + step];
+      }
+    }
+  }
+}
+// The first `have` < V of V elements, of rows shorter than V; the rest 0.
 template <int V, typename T>
 __device__ __forceinline__ void load_tail(float (&x)[V], const T* p, int have) {
 #pragma unroll
@@ -196,18 +231,18 @@ __device__ __forceinline__ void times_slope(float (&v)[V], const float (&z)[V], 
   }
 }
 
-// The bias of V columns from n on (zeros without one, or where the row ends
-// before the last).
+// The bias of V columns from n on, `back` of them behind the row's end (zeros
+// without one, or where the row is shorter than V or ends before n).
 template <typename T, int V>
-__device__ __forceinline__ void load_bias(float (&b)[V], const Epilogue& e, int32_t n) {
-  if (!e.bias || e.N - n < V) {
+__device__ __forceinline__ void load_bias(float (&b)[V], const Epilogue& e, int32_t n, int back = 0) {
+  if (!e.bias || e.N - n < V - back || e.N < V) {
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] = 0.0f;
-  } else if (e.bias_f32) {
-    load_group<V>(b, static_cast<const float*>(e.bias) + n);
-  } else {
-    load_group<V>(b, static_cast<const T*>(e.bias) + n);
+    return;
   }
+  if (e.bias_f32) load_group<V>(b, static_cast<const float*>(e.bias) + n - back);
+  else load_group<V>(b, static_cast<const T*>(e.bias) + n - back);
+  move_down<V>(b, back);
 }
 
 // V columns of a residual, as they lie in memory: 2 V bytes, and of 32-bit
@@ -239,45 +274,49 @@ __device__ __forceinline__ void load_residuals(Residual<V> (&r)[Q], const Epilog
   }
 }
 
-// v += the residual
+// v += the residual, which was loaded `back` columns early
 template <typename T, int V>
-__device__ __forceinline__ void add_residual(float (&v)[V], const Residual<V>& r, const Epilogue& e) {
+__device__ __forceinline__ void add_residual(float (&v)[V], const Residual<V>& r, const Epilogue& e, int back) {
   if (!e.res) return;
+  float x[V];
   if (sizeof(T) == 4 || e.y_f32) {
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
-      v[i] += __builtin_bit_cast(float, uint32_t(r.first[i]));
-      v[V / 2 + i] += __builtin_bit_cast(float, uint32_t(r.second[i]));
+      x[i] = __builtin_bit_cast(float, uint32_t(r.first[i]));
+      x[V / 2 + i] = __builtin_bit_cast(float, uint32_t(r.second[i]));
     }
   } else if constexpr (sizeof(T) == 2) {
     typedef T P __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < V / 2; ++i) {
       const P p = __builtin_bit_cast(P, uint32_t(r.first[i]));
-      v[2 * i] += float(p[0]);
-      v[2 * i + 1] += float(p[1]);
+      x[2 * i] = float(p[0]);
+      x[2 * i + 1] = float(p[1]);
     }
   }
+  move_down<V>(x, back);
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] += x[i];
 }
 
-// The epilogue of V (4 or 8) columns from n on (a multiple of V), all within
-// the row, of row m; v holds the product's sums.
+// The epilogue of V (4 or 8) columns from n on (a multiple of V) of row m, the
+// last `back` of them behind the row's end; v holds the product's sums.
 template <typename T, int V>
 __device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const Residual<V>& r, const Epilogue& e,
-                                     int32_t m, int32_t n) {
+                                     int32_t m, int32_t n, int back = 0) {
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] += b[i];
-  if (e.z) store_group<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v);
+  if (e.z) store_most<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, back);
   activate<V>(v, e.act);
   if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
-  add_residual<T, V>(v, r, e);
-  if (e.y_f32) store_group<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v);
-  else store_group<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v);
+  add_residual<T, V>(v, r, e, back);
+  if (e.y_f32) store_most<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, back);
+  else store_most<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, back);
 }
 
 // The same for the `have` < V columns of a row's end, of Q rows from m on `step`
-// apart, whose sums sum(q, i) gives; all loads of the Q rows go out before the
-// first is used.
+// apart, whose sums sum(q, i) gives, where the rows are shorter than V or only
+// few are left; all loads of the Q rows go out before the first is used.
 template <typename T, int V, int Q, typename F>
 __device__ __forceinline__ void emit_tail(F&& sum, const Epilogue& e, int32_t m, int32_t step, int32_t n, int have) {
   float b[V], r[Q][V];

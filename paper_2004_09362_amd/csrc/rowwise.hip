@@ -26,18 +26,21 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, FastDiv g
   const X* const x = static_cast<const X*>(c.x) + row * c.ldx + col;
   const Y* const res = static_cast<const Y*>(c.res) + row * c.ldr + col;
   Y* const y = static_cast<Y*>(c.y) + row * c.ldy + col;
+  const int have = c.cols - col < 8 ? int(c.cols - col) : 8;
   float v[8], r[8];
-  if (col + 8 <= c.cols) {
-    load_group<8>(v, x);
-    if (c.res) load_group<8>(r, res);
+  if (c.cols >= 8) {
+    const int back = 8 - have;
+    load_group<8>(v, x - back);
+    if (c.res) load_group<8>(r, res - back);
+    move_down<8>(v, back);
     if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), col);
     if (c.res) {
+      move_down<8>(r, back);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
-    store_group<8>(y, v);
+    store_most<8>(y, v, back);
   } else {
-    const int have = int(c.cols - col);
     load_tail<8>(v, x, have);
     load_tail<8>(r, res, c.res ? have : 0);
     if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), col);
@@ -63,26 +66,29 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
   const D* const dy = static_cast<const D*>(c.dy) + col;
   const Z* const z = static_cast<const Z*>(c.z) + col;
   Z* const dz = static_cast<Z*>(c.dz) + col;
-  if (have == 8) {
+  if (have > 0 && c.N >= 8) {
+    const int back = 8 - have;
     for (int64_t row0 = r0 + rt; row0 < r1; row0 += 8 * kRows) {
       float v[kRows][8], t[kRows][8];
 #pragma unroll
       for (int q = 0; q < kRows; ++q)  // of rows past the chunk's last, that one's
-        load_group<8>(v[q], dy + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.lddy);
+        load_group<8>(v[q], dy + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.lddy - back);
       if (c.z) {
 #pragma unroll
         for (int q = 0; q < kRows; ++q)
-          load_group<8>(t[q], z + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.ldz);
+          load_group<8>(t[q], z + (row0 + 8 * q < r1 ? row0 + 8 * q : r1 - 1) * c.ldz - back);
       }
 #pragma unroll
       for (int q = 0; q < kRows; ++q) {
         const int64_t row = row0 + 8 * q;
         if (row >= r1) break;
+        move_down<8>(v[q], back);
+        if (c.z) move_down<8>(t[q], back);
         if (c.drop.on) drop_some<8>(v[q], c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
         if (c.z) times_slope<8>(v[q], t[q], c.act);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += v[q][i];
-        if (c.dz) store_group<8>(dz + row * c.lddz, v[q]);
+        if (c.dz) store_group<8>(dz + row * c.lddz, v[q]);  // its rows have whole groups
       }
     }
   } else if (have > 0) {
@@ -138,19 +144,11 @@ __device__ __forceinline__ void join(const GemmArgs& g, const FastDiv& groups, u
   if (m >= uint32_t(g.e.M)) return;
   const float* part = g.part + int64_t(m) * g.ldp + n;
   const int64_t step = int64_t(g.e.M) * g.ldp;
-  if (uint32_t(g.e.N) - n < 8) {
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int32_t s = 0; s < g.splits; ++s) {  // ldp is a multiple of 8: 8 columns lie there, not all written
-#pragma unroll
-      for (int i = 0; i < 7; ++i) v[i] += n + i < uint32_t(g.e.N) ? part[s * step + i] : 0.0f;
-    }
-    emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), g.e.N - int32_t(n));
-    return;
-  }
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8];
   Residual<8> res[1];
-  load_bias<T, 8>(bias, g.e, int32_t(n));
-  load_residuals<T, 8, 1>(res, g.e, int32_t(m), 1, int32_t(n));
+  const int have = g.e.N - int32_t(n), back = have < 8 ? 8 - have : 0;
+  load_bias<T, 8>(bias, g.e, int32_t(n), back);
+  if (g.e.N >= 8) load_residuals<T, 8, 1>(res, g.e, int32_t(m), 1, int32_t(n) - back);
 #pragma unroll 4
   for (int32_t s = 0; s < g.splits; ++s) {
     const float4* p = reinterpret_cast<const float4*>(part + s * step);
@@ -158,7 +156,9 @@ __device__ __forceinline__ void join(const GemmArgs& g, const FastDiv& groups, u
     v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
     v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
-  emit<T, 8>(v, bias, res[0], g.e, int32_t(m), int32_t(n));
+  // ldp is a multiple of 8: whole groups lie there
+  if (g.e.N >= 8) emit<T, 8>(v, bias, res[0], g.e, int32_t(m), int32_t(n), back);
+  else emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), have);
 }
 
 // Workgroups: those of g, of h, and of the column sums.

@@ -411,3 +411,36 @@ def test_refusals_of_device_tensors():
             call()
     torch.cuda.synchronize()
     assert not x.any() and not w.any() and not wide.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("out32", [False, True], ids=["same", "f32"])
+def test_every_end_of_a_row(dtype, out32):
+    """Rows that end after each number of columns of the last group of 8, or are shorter than one, in place on the residual
+    and between columns that must stay as they are: whole and split products, the gradient, and dropout."""
+    out = torch.float32 if out32 else dtype
+    for N in (1, 3, 5, 7, 8, 9, 10, 11, 12, 13, 14, 15, 16, 21):
+        g = seeded(20, N)
+        for M, K in ((70, 40), (66, 2500)):
+            print("[gpu] row ends", dtype, out, M, N, K, flush=True)
+            x, w, bias = matrix(g, M, K, dtype), matrix(g, N, K, dtype, K ** -0.5), matrix(g, 1, N, dtype)[0]
+            wide = matrix(g, M, N + 5, out)
+            before, y = wide.clone(), wide[:, 2:N + 2]
+            d = (0.25, 5, 6, 7)
+            wy, wz, off, off_z = ref.forward(x, w, bias, before[:, 2:N + 2], "silu", d)
+            got, z = ar.ar_linear_forward(x, w, bias, y, activation="silu", dropout=ar.Dropout(*d), out=y, preact=True)
+            ref.close(got, wy, off, "y")
+            ref.close(z, wz, off_z, "z")
+            assert torch.equal(wide[:, :2], before[:, :2]) and torch.equal(wide[:, N + 2:], before[:, N + 2:])
+        M, K = 45, N + 2
+        dy, x, w, z = matrix(g, M, N, dtype, 0.1), matrix(g, M, K, dtype), matrix(g, N, K, dtype, 0.3), matrix(g, M, N, dtype)
+        want = ref.backward(dy, x, w, z, "gelu", d)
+        for name, t in zip(("dx", "dw", "db"), ar.ar_linear_backward(dy, x, w, preact=z, activation="gelu",
+                                                                     dropout=ar.Dropout(*d), dw_dtype=out)):
+            ref.close(t, want[name][0], want[name][1], name)
+        wide = matrix(g, 50, N + 3, dtype)
+        before, v = wide.clone(), wide[:, 1:N + 1]
+        ar.ar_dropout_backward(v, ar.Dropout(*d), out=v)
+        kept = ref.drop(before[:, 1:N + 1].double().cpu(), d)
+        ref.close(v, kept, 4 * ref.E32 * kept.abs(), "dropped")
+        assert torch.equal(wide[:, :1], before[:, :1]) and torch.equal(wide[:, N + 1:], before[:, N + 1:])
