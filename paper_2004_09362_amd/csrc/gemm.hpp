@@ -101,22 +101,31 @@ __device__ __forceinline__ i32x4v load_whole(const void* p) {
   return __builtin_bit_cast(i32x4v, W(*static_cast<const U*>(p)));
 }
 
-// 16 bytes of a row, elements past `have` zero (have may be negative: p lies
-// behind the row's end).  wide: the row has 16 bytes at least; then its last 16
-// bytes are loaded and shifted, without a branch, so that the loads of several
-// chunks go out together.
+// 16 bytes of a row that has 16 at least, elements past `have` zero (have may be
+// negative: p lies behind the row's end): the row's last 16 bytes are loaded
+// (load_end), without a branch, so that the loads of several chunks go out
+// together, and then shifted (end_chunk).
 template <typename T>
-__device__ __forceinline__ i32x4v load_chunk(const T* p, int64_t have, bool wide) {
+__device__ __forceinline__ i32x4v load_end(const T* p, int64_t have) {
+  constexpr int V = 16 / int(sizeof(T));
+  return load_whole<T>(p + ((have < V ? int(have) : V) - V));
+}
+template <typename T>
+__device__ __forceinline__ i32x4v end_chunk(const i32x4v& raw, int64_t have) {
   constexpr int V = 16 / int(sizeof(T));
   const int h = have < V ? int(have) : V;
-  if (wide) {
-    typedef uint64_t L __attribute__((ext_vector_type(2)));
-    const L x = __builtin_bit_cast(L, load_whole<T>(p + (h - V)));
-    const int bits = h > 0 ? (V - h) * 8 * int(sizeof(T)) : 128;  // to drop
-    const uint64_t lo = bits >= 64 ? x[1] >> (bits & 63) : bits ? x[0] >> bits | x[1] << (64 - bits) : x[0];
-    const L y = {bits >= 128 ? 0 : lo, bits >= 64 ? 0 : x[1] >> bits};
-    return __builtin_bit_cast(i32x4v, y);
-  }
+  typedef uint64_t L __attribute__((ext_vector_type(2)));
+  const L x = __builtin_bit_cast(L, raw);
+  const int bits = h > 0 ? (V - h) * 8 * int(sizeof(T)) : 128;  // to drop
+  const uint64_t lo = bits >= 64 ? x[1] >> (bits & 63) : bits ? x[0] >> bits | x[1] << (64 - bits) : x[0];
+  const L y = {bits >= 128 ? 0 : lo, bits >= 64 ? 0 : x[1] >> bits};
+  return __builtin_bit_cast(i32x4v, y);
+}
+// The same element by element, of a shorter row.
+template <typename T>
+__device__ __forceinline__ i32x4v short_chunk(const T* p, int64_t have) {
+  constexpr int V = 16 / int(sizeof(T));
+  const int h = have < V ? int(have) : V;
   typedef T W __attribute__((ext_vector_type(V)));
   W w;
 #pragma unroll
@@ -233,19 +242,6 @@ struct Operand {
   }
   __device__ __forceinline__ void issue(const char* p, int i) const { load_to_lds(p, voff[i]); }
 
-  // This thread's chunk i of tile t, of which k_have inner indices exist.
-  __device__ __forceinline__ i32x4v chunk(int i, int32_t t, int64_t k_have, int tid) const {
-    const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
-    if constexpr (KMAJOR) {  // rows past the last one: that one's, whose products are never stored
-      return load_chunk(reinterpret_cast<const T*>(at(t) + int64_t(r < rows ? r : rows - 1) * ld + c * 16),
-                        k_have - c * kElems, wide);
-    } else {  // inner indices past the last one: nothing of the tile's first
-      const bool there = r < k_have;
-      const i32x4v v = load_chunk(reinterpret_cast<const T*>(at(t) + (there ? int64_t(r) * ld : 0) + c * 16),
-                                  rows - c * kElems, wide);
-      return there ? v : i32x4v{0, 0, 0, 0};
-    }
-  }
   // A tile into registers.  One that is not the last (and whose offsets fit 32
   // bits) is loaded without a check, so that the loads go out together: what
   // it takes from behind a row's end are elements of the matrix' next row, or
@@ -255,9 +251,33 @@ struct Operand {
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) reg[i] = load_whole<T>(p + voff[i]);
   }
+  // Tile t, of which k_have inner indices exist.  Rows past the last one
+  // (k-major): that one's, whose products are never stored; inner indices past
+  // the last one (otherwise): zeros.
   __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
+    const T* p[kSlots];
+    int64_t have[kSlots];
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) reg[i] = chunk(i, t, k_have, tid);
+    for (int i = 0; i < kSlots; ++i) {
+      const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
+      const bool there = KMAJOR || r < k_have;
+      const int64_t row = KMAJOR ? (r < rows ? r : rows - 1) : (there ? r : 0);
+      p[i] = reinterpret_cast<const T*>(at(t) + row * ld + c * 16);
+      have[i] = KMAJOR ? k_have - c * kElems : rows - c * kElems;
+      if (!there && have[i] > 0) {  // a chunk of the tile's first row is loaded and dropped whole
+        p[i] += have[i];
+        have[i] = 0;
+      }
+    }
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) reg[i] = load_end(p[i], have[i]);
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) reg[i] = end_chunk<T>(reg[i], have[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) reg[i] = short_chunk(p[i], have[i]);
+    }
   }
   __device__ __forceinline__ void store(const i32x4v (&reg)[kSlots], char* lds, int tid) const {
 #pragma unroll
@@ -550,12 +570,26 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
         meet();
         multiply(0);
       }
-    } else {
-      for (; t < tiles; ++t) {
-        fetch(xa0, xb0, t);
-        place(xa0, xb0, t & 1);
+    } else {  // few tiles, or rows far apart: two tiles at a time, the next two on their way
+      auto get = [&](i32x4v (&xa)[OpA::kSlots], i32x4v (&xb)[OpB::kSlots], int32_t at) {
+        if (near && at + 1 < tiles) {
+          a.load(xa, at);
+          b.load(xb, at);
+        } else if (at < tiles) {
+          fetch(xa, xb, at);
+        }
+      };
+      get(xa0, xb0, 0);
+      get(xa1, xb1, 1);
+      for (; t < tiles; t += 2) {
+        if (t > 0) meet();
+        place(xa0, xb0, 0);
+        if (t + 1 < tiles) place(xa1, xb1, 1);
+        get(xa0, xb0, t + 2);
+        get(xa1, xb1, t + 3);
         meet();
-        multiply(t & 1);
+        multiply(0);
+        if (t + 1 < tiles) multiply(1);
       }
     }
   }

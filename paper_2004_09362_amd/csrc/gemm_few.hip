@@ -84,10 +84,22 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_few_kernel(GemmArgs g) {
 #pragma unroll 1
     for (int32_t k = kl + full * (kBatch * kStep); k - p * kElems < k0 + klen; k += kStep) {
       i32x4v w[NT], x[MT];
+      const int32_t have = k0 + klen - k;
+      if (K >= kElems) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) w[t] = load_chunk(wr[t] + k, k0 + klen - k, K >= kElems);
+        for (int t = 0; t < NT; ++t) w[t] = load_end(wr[t] + k, have);
 #pragma unroll
-      for (int t = 0; t < MT; ++t) x[t] = load_chunk(xr[t] + k, k0 + klen - k, K >= kElems);
+        for (int t = 0; t < MT; ++t) x[t] = load_end(xr[t] + k, have);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w[t] = end_chunk<T>(w[t], have);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) x[t] = end_chunk<T>(x[t], have);
+      } else {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) w[t] = short_chunk(wr[t] + k, have);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) x[t] = short_chunk(xr[t] + k, have);
+      }
 #pragma unroll
       for (int a = 0; a < MT; ++a)
 #pragma unroll
