@@ -32,6 +32,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 #include <utility>
 
 #include "layer_device.hpp"
@@ -91,6 +92,19 @@ __device__ __forceinline__ void mma_done(f32x4v (&a)[8], f32x4v (&b)[8], f32x4v 
                : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]), "+a"(a[4]), "+a"(a[5]), "+a"(a[6]), "+a"(a[7])::"memory");
   asm volatile("" : "+a"(b[0]), "+a"(b[1]), "+a"(b[2]), "+a"(b[3]), "+a"(b[4]), "+a"(b[5]), "+a"(b[6]), "+a"(b[7]));
   asm volatile("" : "+a"(c[0]), "+a"(c[1]), "+a"(c[2]), "+a"(c[3]), "+a"(c[4]), "+a"(c[5]), "+a"(c[6]), "+a"(c[7]));
+}
+
+// Pinned sums, moved to ordinary registers here and not before: the compiler
+// would move all 256 at the loop's end, most of them on to memory.
+__device__ __forceinline__ f32x4v unpinned(const f32x4v& a) {
+  f32x4v v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(a[e]));
+    v[e] = x;
+  }
+  return v;
 }
 
 // 16 bytes that start on any element.
@@ -366,11 +380,131 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, u
   n = in / h;
 }
 
+// The epilogue of a whole tile from a wave's registers: this lane's sums, the
+// first of which are those of row m, column n.  swap: the sums of tiles 2j and
+// 2j + 1 lie the other way round (SWAPS: in some lane).  BIAS: there may be one.
+template <typename T, int MT, int NT, bool BIAS, bool SWAPS>
+__device__ __forceinline__ void direct(const GemmArgs& g, f32x4v (&acc)[MT][NT], bool swap, int32_t m, int32_t n, uint32_t part_of) {
+  constexpr int kPairs = NT / 2, kUnits = MT * kPairs, kAhead = 4;
+  const Epilogue& e = g.e;
+  float b[kPairs][8];  // zeros without a bias, and where parts of a product are joined later
+  if constexpr (BIAS) {
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+      if (g.splits > 1) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) b[j][k] = 0.0f;
+      } else {
+        load_bias<T, 8>(b[j], e, n + 32 * j);
+      }
+    }
+  }
+  auto biased = [&](float (&v)[8], int j) {
+    if constexpr (BIAS) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] += b[j][k];
+    }
+  };
+  auto sum = [](const f32x4v& a) {
+    if constexpr (MT * NT == 64) return unpinned(a);
+    else return a;
+  };
+  // Of a lane whose sums lie the other way round what is read and written is
+  // exchanged, not the sums: the compiler would do that for all of them at once,
+  // beyond the registers.
+  typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+  auto swapped = [&](U4 w) { return SWAPS && swap ? U4{w[2], w[3], w[0], w[1]} : w; };
+  auto swap_halves = [&](U4& a, U4& b) {
+    const U4 c = a;
+    if (SWAPS) a = swap ? b : a;
+    if (SWAPS) b = swap ? c : b;
+  };
+  auto store = [&](auto* to, const float (&v)[8]) {
+    using Y = std::remove_pointer_t<decltype(to)>;
+    if constexpr (sizeof(Y) == 4) {
+      const int other = SWAPS && swap ? 4 : 0;
+      store_group<4>(to + other, {v[0], v[1], v[2], v[3]});
+      store_group<4>(to + (4 - other), {v[4], v[5], v[6], v[7]});
+    } else {
+      typedef Y H __attribute__((ext_vector_type(8)));
+      typedef U4 Any __attribute__((aligned(2)));
+      *reinterpret_cast<Any*>(to) = swapped(__builtin_bit_cast(U4, H{Y(v[0]), Y(v[1]), Y(v[2]), Y(v[3]), Y(v[4]), Y(v[5]), Y(v[6]), Y(v[7])}));
+    }
+  };
+  // f(row, pair, values) for each unit of 8 columns
+  auto units = [&](auto&& f) {
+    unrolled([&](auto index) {
+      constexpr int i = decltype(index)::value / kPairs, j = decltype(index)::value % kPairs;
+      const f32x4v x = sum(acc[i][2 * j]), y = sum(acc[i][2 * j + 1]);
+      float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+      f(i, j, v);
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, kUnits>{});
+  };
+  auto write = [&](auto* to, int64_t ld) {
+    to += int64_t(m) * ld + n;
+    units([&](int i, int j, float (&v)[8]) {
+      biased(v, j);
+      store(to + i * (16 * ld) + 32 * j, v);
+    });
+  };
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): the loads to LDS that nobody waits for
+  if (g.splits > 1) {
+    write(g.part + int64_t(part_of) * e.M * g.ldp, g.ldp);
+    return;
+  }
+  if (e.res) {
+    Residual<8> res[2][kAhead];  // of this group of units and of the next
+    auto fetch = [&](auto index) {
+      constexpr int x = decltype(index)::value;
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        Residual<8> r[1];
+        load_residuals<T, 8, 1>(r, e, m + (x * kAhead + q) / kPairs * 16, 0, n + (x * kAhead + q) % kPairs * 32);
+        res[x & 1][q] = r[0];
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    static_assert(kUnits % kAhead == 0, "whole groups");
+    fetch(std::integral_constant<int, 0>{});
+    auto finish = [&](auto* to) {
+      to += int64_t(m) * e.ldy + n;
+      unrolled([&](auto index) {
+        constexpr int x = decltype(index)::value;
+        if constexpr ((x + 1) * kAhead < kUnits) fetch(std::integral_constant<int, x + 1>{});
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const int i = (x * kAhead + q) / kPairs, j = (x * kAhead + q) % kPairs;
+          const f32x4v c = sum(acc[i][2 * j]), d = sum(acc[i][2 * j + 1]);
+          float v[1][8] = {{c[0], c[1], c[2], c[3], d[0], d[1], d[2], d[3]}};
+          biased(v[0], j);
+          Residual<8> r[1] = {res[x & 1][q]};
+          if (sizeof(*to) == 4) swap_halves(r[0].first, r[0].second);
+          else r[0].first = swapped(r[0].first);
+          add_residuals<T, 8, 1>(v, r, e, 0);
+          store(to + i * (16 * e.ldy) + 32 * j, v[0]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }, std::make_integer_sequence<int, kUnits / kAhead>{});
+    };
+    if (e.y_f32) finish(static_cast<float*>(e.y));
+    else finish(static_cast<T*>(e.y));
+  } else if (e.y_f32) {
+    write(static_cast<float*>(e.y), e.ldy);
+  } else {
+    write(static_cast<T*>(e.y), e.ldy);
+  }
+}
+
 // LDS of a workgroup: five places, each for one operand of a tile.
 constexpr int ring_bytes(int tile) { return 5 * tile * kTileKBytes; }
 
+// What a kernel's epilogue has, each with less code and fewer registers than the
+// next: kSums a residual, kBiased also a bias, kFull everything.
+enum Stages { kSums, kBiased, kFull };
+
 // Part `part` of tile `tile` of a product.
-template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC>
+template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC, Stages STAGES>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint32_t part_of, char* lds) {
   constexpr int THREADS = WM * WN * 64, TM = WM * MT * 16, TN = WN * NT * 16;
   using OpA = Operand<T, AK, false, TM, THREADS>;
@@ -594,7 +728,17 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
     }
   }
 
-  // The sums leave through LDS, each wave by itself in its share of the
+  // A whole tile's sums leave from the lanes that hold them: of tiles 2j, 2j + 1
+  // a lane has 8 columns (32 j + 8 p on) of a row, and four lanes have 64 bytes of
+  // halves together, whose line the next columns fill.  Each stage goes over all
+  // sums without a branch within.
+  const bool whole = m0 + TM <= g.e.M && n0 + TN <= g.e.N;
+  if (STAGES != kFull && whole) {
+    direct<T, MT, NT, STAGES == kBiased, !BK>(g, acc, !BK && (lane & 16), m0 + wm * MT * 16 + (lane & 15), n0 + wn * NT * 16 + 8 * (lane >> 4), part_of);
+    return;
+  }
+
+  // At the matrix' edges the sums leave through LDS, each wave by itself in its share of the
   // buffers: a lane of tiles 2j, 2j + 1 writes its 8 columns (32 j + 8 p on)
   // of a row as one 32-byte unit, at a place XORed with the row so that 16
   // rows fall on different banks, and then takes 8 columns of one row whose
@@ -610,18 +754,22 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
   const int have = g.e.N - n, back = have < 8 ? 8 - have : 0;
   float* part = g.part + int64_t(part_of) * g.e.M * g.ldp + n;  // ldp is a multiple of 8
   float bias[8];
-  load_bias<T, 8>(bias, g.e, n, have > 0 ? back : 0);
+  if constexpr (STAGES != kSums) load_bias<T, 8>(bias, g.e, n, have > 0 ? back : 0);
+  auto sum = [](const f32x4v& a) {
+    if constexpr (kPinned && STAGES != kFull) return unpinned(a);
+    else return a;
+  };
   auto spread = [&](auto round) {
     constexpr int first = decltype(round)::value * kTilesRound;
 #pragma unroll
     for (int i = 0; i < kTilesRound; ++i) {
 #pragma unroll
       for (int j = 0; j < NT / 2; ++j) {
-        const f32x4v x = acc[first + i][2 * j], y = acc[first + i][2 * j + 1];
+        const f32x4v x = sum(acc[first + i][2 * j]), y = sum(acc[first + i][2 * j + 1]);
         const int r = 16 * i + (lane & 15), u = (4 * j + (lane >> 4)) ^ (r & (kUnits - 1));
         f32x4v* q = reinterpret_cast<f32x4v*>(share + (r * kUnits + u) * 32);
-        q[0] = swap ? y : x;
-        q[1] = swap ? x : y;
+        q[swap ? 1 : 0] = x;
+        q[swap ? 0 : 1] = y;
       }
     }
   };
@@ -642,21 +790,24 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
         if (g.splits == 1) load_residuals<T, 8, kAhead>(res, g.e, mw + pass * kPassRows, kPassRows, n - back);
       };
       auto finish = [&](const Residual<8> (&res)[kAhead], int pass) {
+        float v[kAhead][8];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-          const int r = (pass + q) * kPassRows;
-          const int32_t m = mw + r;
-          if (m >= g.e.M) continue;
-          const f32x4v* w = reinterpret_cast<const f32x4v*>(unit_at(r + lane / kUnits));
+          const f32x4v* w = reinterpret_cast<const f32x4v*>(unit_at((pass + q) * kPassRows + lane / kUnits));
           const f32x4v x = w[0], y = w[1];
-          if (g.splits > 1) {
-            f32x4v* to = reinterpret_cast<f32x4v*>(part + int64_t(m) * g.ldp);
-            to[0] = x;
-            to[1] = y;
-          } else {
-            float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            emit<T, 8>(v, bias, res[q], g.e, m, n, back);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            v[q][i] = x[i];
+            v[q][4 + i] = y[i];
           }
+        }
+        const int32_t m = mw + pass * kPassRows;
+        if (g.splits > 1) {
+#pragma unroll
+          for (int q = 0; q < kAhead; ++q)
+            if (m + q * kPassRows < g.e.M) store_group<8>(part + int64_t(m + q * kPassRows) * g.ldp, v[q]);
+        } else {
+          emit<T, 8, kAhead, STAGES != kSums, STAGES == kFull>(v, bias, res, g.e, m, kPassRows, n, back);
         }
       };
       fetch(res0, 0);
@@ -681,57 +832,82 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
   }
 }
 
-template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC>
+template <typename T, bool AK, bool BK, int MT, int NT, int WM, int WN, bool ASYNC, Stages STAGES>
 __global__ __launch_bounds__(WM* WN * 64, MT * NT <= 16 ? 2 : 1) void gemm_kernel(GemmArgs g) {
   __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(WM * MT * 16)];
-  gemm_tile<T, AK, BK, MT, NT, WM, WN, ASYNC>(g, blockIdx.x, blockIdx.y, lds);
+  gemm_tile<T, AK, BK, MT, NT, WM, WN, ASYNC, STAGES>(g, blockIdx.x, blockIdx.y, lds);
 }
 
-// The gradient's two products in one launch, x's first: for small ones, which
-// fill the chip together and have the latency of one.
-template <typename T, bool ASYNC>
-__global__ __launch_bounds__(256, 2) void gemm_pair_kernel(GemmArgs x, GemmArgs w) {
-  __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(128)];
+// The gradient's two products in one launch: x's workgroups begin at x_from,
+// w's at w_from, one of which is 0; the other is a multiple of 8, so that both
+// orders of tiles (tile_of) go round the XCDs alike.
+template <typename T, int MT, int NT, bool ASYNC>
+__global__ __launch_bounds__(256, MT * NT <= 16 ? 2 : 1) void gemm_pair_kernel(GemmArgs x, GemmArgs w, uint32_t x_from,
+                                                                                uint32_t w_from) {
+  __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(2 * MT * 16)];
   const uint32_t tx = uint32_t(x.tiles_m) * uint32_t(x.tiles_n), tw = uint32_t(w.tiles_m) * uint32_t(w.tiles_n);
-  const uint32_t first = tx * uint32_t(x.splits);
-  if (blockIdx.x < first) {
-    const uint32_t part = blockIdx.x / tx;
-    gemm_tile<T, true, false, 4, 4, 2, 2, ASYNC>(x, blockIdx.x - part * tx, part, lds);
+  if (x_from > w_from ? blockIdx.x >= x_from : blockIdx.x < w_from) {
+    const uint32_t id = blockIdx.x - x_from, part = id / tx;
+    if (part < uint32_t(x.splits)) gemm_tile<T, true, false, MT, NT, 2, 2, ASYNC, kSums>(x, id - part * tx, part, lds);
   } else {
-    const uint32_t id = blockIdx.x - first, part = id / tw;
-    gemm_tile<T, false, false, 4, 4, 2, 2, ASYNC>(w, id - part * tw, part, lds);
+    const uint32_t id = blockIdx.x - w_from, part = id / tw;
+    if (part < uint32_t(w.splits)) gemm_tile<T, false, false, MT, NT, 2, 2, ASYNC, kSums>(w, id - part * tw, part, lds);
   }
 }
 
-template <typename T, bool AK, bool BK>
-int launch_layout(const GemmArgs& g, bool aligned, int32_t shape, hipStream_t st) {
+template <typename T, bool AK, bool BK, Stages STAGES>
+int launch_stages(const GemmArgs& g, bool aligned, int32_t shape, hipStream_t st) {
   const dim3 grid(uint32_t(g.tiles_m) * uint32_t(g.tiles_n), uint32_t(g.splits));
   if (shape == kTile256) {
-    if (!aligned) return int(hipErrorInvalidValue);
-    gemm_kernel<T, AK, BK, 8, 8, 2, 2, true><<<grid, dim3(256), 0, st>>>(g);
+    if constexpr (sizeof(T) == 2) {
+      if (!aligned) return int(hipErrorInvalidValue);
+      gemm_kernel<T, AK, BK, 8, 8, 2, 2, true, STAGES><<<grid, dim3(256), 0, st>>>(g);
+    } else {
+      return int(hipErrorInvalidValue);
+    }
   } else if (aligned) {
-    gemm_kernel<T, AK, BK, 4, 4, 2, 2, true><<<grid, dim3(256), 0, st>>>(g);
+    gemm_kernel<T, AK, BK, 4, 4, 2, 2, true, STAGES><<<grid, dim3(256), 0, st>>>(g);
   } else {
-    gemm_kernel<T, AK, BK, 4, 4, 2, 2, false><<<grid, dim3(256), 0, st>>>(g);
+    gemm_kernel<T, AK, BK, 4, 4, 2, 2, false, STAGES><<<grid, dim3(256), 0, st>>>(g);
   }
   return int(hipGetLastError());
 }
 
+// The gradient's products have a residual at most; parts are joined later with
+// the whole epilogue.
 template <typename T>
 int launch_gemm_of(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (a_kmajor) return b_kmajor ? launch_layout<T, true, true>(g, aligned, shape, st)
-                                : launch_layout<T, true, false>(g, aligned, shape, st);
-  return b_kmajor ? int(hipErrorInvalidValue) : launch_layout<T, false, false>(g, aligned, shape, st);
+  if (a_kmajor && b_kmajor) {
+    const bool full = g.splits == 1 && (g.e.z || g.e.act != kActNone || g.e.drop.on);
+    return full ? launch_stages<T, true, true, kFull>(g, aligned, shape, st) : launch_stages<T, true, true, kBiased>(g, aligned, shape, st);
+  }
+  if (b_kmajor || g.e.bias || g.e.z || g.e.act != kActNone || g.e.drop.on) return int(hipErrorInvalidValue);
+  return a_kmajor ? launch_stages<T, true, false, kSums>(g, aligned, shape, st)
+                  : launch_stages<T, false, false, kSums>(g, aligned, shape, st);
 }
 
+// The product with the longer parts first.
 template <typename T>
-int launch_pair_of(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream) {
+int launch_pair_of(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream) {
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const dim3 grid(uint32_t(x.tiles_m) * uint32_t(x.tiles_n) * uint32_t(x.splits) +
-                  uint32_t(w.tiles_m) * uint32_t(w.tiles_n) * uint32_t(w.splits));
-  if (aligned) gemm_pair_kernel<T, true><<<grid, dim3(256), 0, st>>>(x, w);
-  else gemm_pair_kernel<T, false><<<grid, dim3(256), 0, st>>>(x, w);
+  const uint32_t nx = uint32_t(x.tiles_m) * uint32_t(x.tiles_n) * uint32_t(x.splits);
+  const uint32_t nw = uint32_t(w.tiles_m) * uint32_t(w.tiles_n) * uint32_t(w.splits);
+  const bool x_first = x.k_split >= w.k_split;
+  const uint32_t x_from = x_first ? 0 : (nw + 7) / 8 * 8, w_from = x_first ? (nx + 7) / 8 * 8 : 0;
+  const dim3 grid(x_first ? w_from + nw : x_from + nx);
+  if (shape == kTile256) {
+    if constexpr (sizeof(T) == 2) {
+      if (!aligned) return int(hipErrorInvalidValue);
+      gemm_pair_kernel<T, 8, 8, true><<<grid, dim3(256), 0, st>>>(x, w, x_from, w_from);
+    } else {
+      return int(hipErrorInvalidValue);
+    }
+  } else if (aligned) {
+    gemm_pair_kernel<T, 4, 4, true><<<grid, dim3(256), 0, st>>>(x, w, x_from, w_from);
+  } else {
+    gemm_pair_kernel<T, 4, 4, false><<<grid, dim3(256), 0, st>>>(x, w, x_from, w_from);
+  }
   return int(hipGetLastError());
 }
 

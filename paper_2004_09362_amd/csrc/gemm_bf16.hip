@@ -7,8 +7,8 @@ int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool align
   return launch_gemm_of<bf16>(g, a_kmajor, b_kmajor, aligned, shape, stream);
 }
 
-int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream) {
-  return launch_pair_of<bf16>(x, w, aligned, stream);
+int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream) {
+  return launch_pair_of<bf16>(x, w, aligned, shape, stream);
 }
 
 }  // namespace ar

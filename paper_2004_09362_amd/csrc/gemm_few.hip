@@ -122,11 +122,11 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_few_kernel(GemmArgs g) {
     } else if (g.e.N - n < 4) {
       emit_tail<T, 4, 1>([&](int, int c) { return v[c]; }, g.e, m, 1, n, g.e.N - n);
     } else {
-      float x[4] = {v[0], v[1], v[2], v[3]}, bias[4];
+      float x[1][4] = {{v[0], v[1], v[2], v[3]}}, bias[4];
       Residual<4> res[1];
       load_bias<T, 4>(bias, g.e, n);
       load_residuals<T, 4, 1>(res, g.e, m, 1, n);
-      emit<T, 4>(x, bias, res[0], g.e, m, n);
+      emit<T, 4, 1>(x, bias, res, g.e, m, 1, n);
     }
   }
 }
@@ -226,10 +226,10 @@ __global__ __launch_bounds__(256) void gemm_stream_kernel(GemmArgs g) {
     } else if (g.e.N - n < 4) {
       emit_tail<T, 4, 1>([&](int, int c) { return acc[i][c]; }, g.e, m, 1, n, g.e.N - n);
     } else {
-      float x[4] = {acc[i][0], acc[i][1], acc[i][2], acc[i][3]};
+      float x[1][4] = {{acc[i][0], acc[i][1], acc[i][2], acc[i][3]}};
       Residual<4> res[1];
       load_residuals<T, 4, 1>(res, g.e, m, 1, n);
-      emit<T, 4>(x, bias, res[0], g.e, m, n);
+      emit<T, 4, 1>(x, bias, res, g.e, m, 1, n);
     }
   }
 }

@@ -183,26 +183,22 @@ __device__ __forceinline__ float slope_silu(float z) {
   return g * __builtin_fmaf(z, 1.0f - g, 1.0f);
 }
 
-// v[i] = act(v[i]): one branch for all.
-template <int V>
-__device__ __forceinline__ void activate(float (&v)[V], int act) {
+// v = act(v), of Q rows: one branch for all, so that the rows' long operations
+// overlap.
+template <int V, int Q, typename F>
+__device__ __forceinline__ void each(float (&v)[Q][V], F&& f) {
+#pragma unroll
+  for (int q = 0; q < Q; ++q)
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[q][i] = f(v[q][i]);
+}
+template <int V, int Q>
+__device__ __forceinline__ void activate(float (&v)[Q][V], int act) {
   switch (act) {
-    case kActRelu:
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = act_relu(v[i]);
-      break;
-    case kActGelu:
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = act_gelu(v[i]);
-      break;
-    case kActGeluTanh:
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = act_gelu_tanh(v[i]);
-      break;
-    case kActSilu:
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = act_silu(v[i]);
-      break;
+    case kActRelu: each(v, act_relu); break;
+    case kActGelu: each(v, act_gelu); break;
+    case kActGeluTanh: each(v, act_gelu_tanh); break;
+    case kActSilu: each(v, act_silu); break;
     default: break;
   }
 }
@@ -274,44 +270,63 @@ __device__ __forceinline__ void load_residuals(Residual<V> (&r)[Q], const Epilog
   }
 }
 
-// v += the residual, which was loaded `back` columns early
-template <typename T, int V>
-__device__ __forceinline__ void add_residual(float (&v)[V], const Residual<V>& r, const Epilogue& e, int back) {
+// v += the residuals, which were loaded `back` columns early
+template <typename T, int V, int Q>
+__device__ __forceinline__ void add_residuals(float (&v)[Q][V], const Residual<V> (&r)[Q], const Epilogue& e, int back) {
   if (!e.res) return;
-  float x[V];
-  if (sizeof(T) == 4 || e.y_f32) {
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-      x[i] = __builtin_bit_cast(float, uint32_t(r.first[i]));
-      x[V / 2 + i] = __builtin_bit_cast(float, uint32_t(r.second[i]));
-    }
-  } else if constexpr (sizeof(T) == 2) {
-    typedef T P __attribute__((ext_vector_type(2)));
+  for (int q = 0; q < Q; ++q) {
+    float x[V];
+    if (sizeof(T) == 4 || e.y_f32) {
 #pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-      const P p = __builtin_bit_cast(P, uint32_t(r.first[i]));
-      x[2 * i] = float(p[0]);
-      x[2 * i + 1] = float(p[1]);
+      for (int i = 0; i < V / 2; ++i) {
+        x[i] = __builtin_bit_cast(float, uint32_t(r[q].first[i]));
+        x[V / 2 + i] = __builtin_bit_cast(float, uint32_t(r[q].second[i]));
+      }
+    } else if constexpr (sizeof(T) == 2) {
+      typedef T P __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        const P p = __builtin_bit_cast(P, uint32_t(r[q].first[i]));
+        x[2 * i] = float(p[0]);
+        x[2 * i + 1] = float(p[1]);
+      }
     }
+    move_down<V>(x, back);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[q][i] += x[i];
   }
-  move_down<V>(x, back);
-#pragma unroll
-  for (int i = 0; i < V; ++i) v[i] += x[i];
 }
 
-// The epilogue of V (4 or 8) columns from n on (a multiple of V) of row m, the
-// last `back` of them behind the row's end; v holds the product's sums.
-template <typename T, int V>
-__device__ __forceinline__ void emit(float (&v)[V], const float (&b)[V], const Residual<V>& r, const Epilogue& e,
-                                     int32_t m, int32_t n, int back = 0) {
+// The epilogue of V (4 or 8) columns from n on (a multiple of V), the last
+// `back` of them behind the row's end, of Q rows from m on `step` apart; v holds
+// the product's sums.  Rows past the last one are worked on and not stored.
+// BIAS, STAGES: whether there may be a bias; a kept z, an activation, dropout.
+template <typename T, int V, int Q, bool BIAS = true, bool STAGES = true>
+__device__ __forceinline__ void emit(float (&v)[Q][V], const float (&b)[V], const Residual<V> (&r)[Q], const Epilogue& e,
+                                     int32_t m, int32_t step, int32_t n, int back = 0) {
+  auto store = [&](auto* to, int64_t ld) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) v[i] += b[i];
-  if (e.z) store_most<V>(static_cast<T*>(e.z) + int64_t(m) * e.ldz + n, v, back);
-  activate<V>(v, e.act);
-  if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(m), uint32_t(n));
-  add_residual<T, V>(v, r, e, back);
-  if (e.y_f32) store_most<V>(static_cast<float*>(e.y) + int64_t(m) * e.ldy + n, v, back);
-  else store_most<V>(static_cast<T*>(e.y) + int64_t(m) * e.ldy + n, v, back);
+    for (int q = 0; q < Q; ++q)
+      if (m + q * step < e.M) store_most<V>(to + int64_t(m + q * step) * ld + n, v[q], back);
+  };
+  if constexpr (BIAS) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[q][i] += b[i];
+  }
+  if constexpr (STAGES) {
+    if (e.z) store(static_cast<T*>(e.z), e.ldz);
+    activate(v, e.act);
+    if (e.drop.on) {
+#pragma unroll
+      for (int q = 0; q < Q; ++q) drop_some<V>(v[q], e.drop, e.drop.row0 + uint32_t(m + q * step), uint32_t(n));
+    }
+  }
+  add_residuals<T, V, Q>(v, r, e, back);
+  if (e.y_f32) store(static_cast<float*>(e.y), e.ldy);
+  else store(static_cast<T*>(e.y), e.ldy);
 }
 
 // The same for the `have` < V columns of a row's end, of Q rows from m on `step`
@@ -338,11 +353,12 @@ __device__ __forceinline__ void emit_tail(F&& sum, const Epilogue& e, int32_t m,
   for (int q = 0; q < Q; ++q) {
     const int32_t row = m + q * step;
     if (row >= e.M) break;
-    float v[V];
+    float w[1][V];
+    float(&v)[V] = w[0];
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = i < have ? sum(q, i) + b[i] : 0.0f;
     if (e.z) store_tail<V>(static_cast<T*>(e.z) + int64_t(row) * e.ldz + n, v, have);
-    activate<V>(v, e.act);
+    activate(w, e.act);
     if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(row), uint32_t(n));
     if (e.res) {
 #pragma unroll

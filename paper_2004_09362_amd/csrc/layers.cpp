@@ -8,6 +8,7 @@
 #include <cstdint>
 #include <exception>
 #include <string>
+#include <utility>
 
 #include "../../include/ar.h"
 #include "ar_internal.hpp"
@@ -24,11 +25,11 @@ int launch_gemm(const GemmArgs& g, int32_t elem, bool a_kmajor, bool b_kmajor, b
   return int(hipErrorInvalidValue);
 }
 
-int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, void* stream) {
+int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, int32_t shape, void* stream) {
   switch (elem) {
-    case kF32: return launch_gemm_pair_f32(x, w, aligned, stream);
-    case kF16: return launch_gemm_pair_f16(x, w, aligned, stream);
-    case kBF16: return launch_gemm_pair_bf16(x, w, aligned, stream);
+    case kF32: return launch_gemm_pair_f32(x, w, aligned, shape, stream);
+    case kF16: return launch_gemm_pair_f16(x, w, aligned, shape, stream);
+    case kBF16: return launch_gemm_pair_bf16(x, w, aligned, shape, stream);
   }
   return int(hipErrorInvalidValue);
 }
@@ -191,8 +192,19 @@ struct Product {
   Kind kind = kTiles;
   bool aligned = false;
   int32_t shape = ar::kTile128, splits = 1, k_split = 0, tiles_m = 0, tiles_n = 0;
-  int64_t ldp = 0;
+  int64_t ldp = 0, M = 0, N = 0, steps = 0, inner = 0;  // steps of `inner` make the inner length
+  double micros = 0.0;                                   // on tiles: what the model says, without the join's launch
 };
+
+// Shape and parts of a product, whose sizes are there.
+void set_parts(Product& p, int32_t shape, int64_t splits) {
+  const int64_t tile = ar::tile_rows(shape), per = ceil_div(p.steps, splits);
+  p.shape = shape;
+  p.tiles_m = int32_t(ceil_div(p.M, tile));
+  p.tiles_n = int32_t(ceil_div(p.N, tile));
+  p.k_split = int32_t(std::min(per * p.inner, kMaxLength));
+  p.splits = int32_t(ceil_div(p.steps, per));
+}
 
 // What a product on tiles takes, in microseconds, on this library's kernels at
 // the rates that they measured on MI355X: a tile of 128 x 128 costs `fixed` and
@@ -206,6 +218,13 @@ constexpr TileCost kCost256 = {10.0, 1.42, 1.42};
 constexpr TileCost kCost128[2][2] = {{{5.0, 0.90, 1.55}, {5.0, 0.68, 1.18}},   // halves: through registers, asynchronous
                                      {{5.0, 2.10, 4.00}, {5.0, 1.90, 3.60}}};  // floats
 constexpr double kJoinMicros = 4.0, kJoinBytesPerMicro = 5e6;
+const TileCost& tile_cost(const Product& p, int32_t shape, bool floats) {
+  return shape == ar::kTile256 ? kCost256 : kCost128[floats][p.aligned];
+}
+// What the parts of a product add.
+double parts_micros(const Product& p, int64_t splits) {
+  return splits > 1 ? double(splits) * double(p.M) * double(p.ldp) * 8.0 / kJoinBytesPerMicro : 0.0;
+}
 
 double tile_micros(const TileCost& c, int64_t workgroups, int64_t steps, bool shared) {
   const int64_t at_once = shared ? 2 * kCus : kCus, rounds = workgroups / at_once, rest = workgroups % at_once;
@@ -215,10 +234,13 @@ double tile_micros(const TileCost& c, int64_t workgroups, int64_t steps, bool sh
 
 Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Operand& a, const Operand& b) {
   Product p;
-  const int64_t eb = size_of(type), inner = ar::kTileKBytes / eb, steps = std::max<int64_t>(1, ceil_div(K, inner));
+  const int64_t eb = size_of(type);
+  p.M = M;
+  p.N = N;
+  p.inner = ar::kTileKBytes / eb;
+  p.steps = std::max<int64_t>(1, ceil_div(K, p.inner));
   p.ldp = round_up(N, 8);
   p.aligned = can_load_async(a, eb) && can_load_async(b, eb);
-  int64_t splits = 1;
   const bool rows = a.kmajor && b.kmajor && M <= ar::kFewMaxRows;
   // Few rows.  Aligned, both kernels read w at the rate of memory; the one
   // through LDS keeps it up with more rows and longer inner lengths, the other
@@ -231,42 +253,93 @@ Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Opera
   const int64_t row_tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   if (rows && p.aligned && (M <= 16 ? N >= 8192 || K * eb > 16384 : K * eb > 2048)) {
     p.kind = kStream;
-    splits = std::min(kCus / ceil_div(N, 64), steps / 8);
-  } else if (rows && (p.aligned || N * K * (1 + row_tiles) <= 20000000)) {
+    set_parts(p, ar::kTile128, std::max<int64_t>(1, std::min(kCus / ceil_div(N, 64), p.steps / 8)));
+    return p;
+  }
+  if (rows && (p.aligned || N * K * (1 + row_tiles) <= 20000000)) {
     p.kind = kFew;
-    splits = std::min(kCus / ceil_div(N, 16), steps / 64);
-  } else {
-    const int64_t small = ceil_div(M, 128) * ceil_div(N, 128), large = ceil_div(M, 256) * ceil_div(N, 256);
-    if (small >= (int64_t(1) << 31)) refuse(AR_ERR_UNSUPPORTED, "the product would need 2^31 or more tiles");
-    const TileCost& cost = kCost128[type == AR_FLOAT32][p.aligned];
-    double best = 0.0;
-    for (int64_t s = 1; s <= std::min<int64_t>(64, std::max<int64_t>(1, steps / 2)); ++s) {
-      if (s > 1 && s * std::min(small, large) > 8 * kCus) break;  // more parts than the chip takes at once
-      const int64_t per = ceil_div(steps, s);
-      const double join = s > 1 ? kJoinMicros + double(s) * double(M) * double(p.ldp) * 8.0 / kJoinBytesPerMicro : 0.0;
-      const double t128 = tile_micros(cost, s * small, per, true) + join;
-      if (s == 1 || t128 < best) {
-        best = t128;
-        p.shape = ar::kTile128;
-        splits = s;
-      }
-      if (!p.aligned || type == AR_FLOAT32) continue;
-      const double t256 = tile_micros(kCost256, s * large, per, false) + join;
-      if (t256 < best) {
-        best = t256;
-        p.shape = ar::kTile256;
-        splits = s;
+    set_parts(p, ar::kTile128, std::max<int64_t>(1, std::min<int64_t>({kCus / ceil_div(N, 16), p.steps / 64, 64})));
+    return p;
+  }
+  const int64_t small = ceil_div(M, 128) * ceil_div(N, 128), large = ceil_div(M, 256) * ceil_div(N, 256);
+  if (small >= (int64_t(1) << 31)) refuse(AR_ERR_UNSUPPORTED, "the product would need 2^31 or more tiles");
+  const bool floats = type == AR_FLOAT32;
+  int32_t shape = ar::kTile128;
+  int64_t splits = 1;
+  double best = 0.0;
+  for (int64_t s = 1; s <= std::min<int64_t>(64, std::max<int64_t>(1, p.steps / 2)); ++s) {
+    if (s > 1 && s * std::min(small, large) > 8 * kCus) break;  // more parts than the chip takes at once
+    for (int32_t sh : {ar::kTile128, ar::kTile256}) {
+      if (sh == ar::kTile256 && (!p.aligned || floats)) continue;
+      const double t = tile_micros(tile_cost(p, sh, floats), s * (sh == ar::kTile256 ? large : small), ceil_div(p.steps, s),
+                                   sh == ar::kTile128) + parts_micros(p, s) + (s > 1 ? kJoinMicros : 0.0);
+      if (best > 0.0 && t >= best) continue;
+      best = t;
+      shape = sh;
+      splits = s;
+    }
+  }
+  set_parts(p, shape, splits);
+  p.micros = best - (splits > 1 ? kJoinMicros : 0.0);
+  return p;
+}
+
+// Two products in one launch: workgroups of both kinds take the places that the
+// chip has, the longer ones first.
+double pair_micros(const TileCost& c, int64_t n1, int64_t steps1, int64_t n2, int64_t steps2, bool shared) {
+  const int64_t places = shared ? 2 * kCus : kCus;
+  const double one = n1 + n2 > kCus ? c.two : c.one;
+  double t1 = c.fixed + double(steps1) * one, t2 = c.fixed + double(steps2) * one;
+  if (t2 > t1) {
+    std::swap(t1, t2);
+    std::swap(n1, n2);
+  }
+  const int64_t late = n1 % places, early = places - late;  // places that are free a round later, and the others
+  double at0 = double(n1 / places) * t1, at1 = at0 + t1, end = late > 0 ? at1 : at0;
+  for (int64_t left = n2; left > 0;) {
+    const bool first = late == 0 || at0 <= at1;
+    left -= first ? early : late;
+    double& at = first ? at0 : at1;
+    at += t2;
+    end = std::max(end, at);
+  }
+  return end;
+}
+
+// Whether x and w, the gradient's two products, share a launch, and their parts
+// then: where the model says that it takes less time than one after the other.
+// One launch has one start and one end, and while some workgroups write their
+// results others multiply.
+bool plan_pair(Product& x, Product& w, ar_dtype type) {
+  constexpr double kLaunchMicros = 4.0;  // a launch's start and end, seen from the next one
+  constexpr int64_t kParts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  if (x.aligned != w.aligned) return false;
+  const bool floats = type == AR_FLOAT32;
+  double best = x.micros + w.micros + kLaunchMicros + (x.splits > 1 || w.splits > 1 ? kJoinMicros : 0.0);
+  int32_t shape = -1;
+  int64_t sx = 1, sw = 1;
+  for (int32_t sh : {ar::kTile128, ar::kTile256}) {
+    if (sh == ar::kTile256 && (!x.aligned || floats)) continue;
+    const int64_t tile = ar::tile_rows(sh), tx = ceil_div(x.M, tile) * ceil_div(x.N, tile), tw = ceil_div(w.M, tile) * ceil_div(w.N, tile);
+    if (tx + tw > 8 * kCus) continue;  // the ends of long launches weigh little
+    for (const int64_t i : kParts) {
+      if (i > 1 && (i > x.steps / 2 || i * tx > 4 * kCus)) break;
+      for (const int64_t j : kParts) {
+        if (j > 1 && (j > w.steps / 2 || j * tw > 4 * kCus)) break;
+        const double t = pair_micros(tile_cost(x, sh, floats), i * tx, ceil_div(x.steps, i), j * tw, ceil_div(w.steps, j), sh == ar::kTile128) +
+                         parts_micros(x, i) + parts_micros(w, j) + (i > 1 || j > 1 ? kJoinMicros : 0.0);
+        if (t >= best) continue;
+        best = t;
+        shape = sh;
+        sx = i;
+        sw = j;
       }
     }
-    const int64_t tile = ar::tile_rows(p.shape);
-    p.tiles_m = int32_t(ceil_div(M, tile));
-    p.tiles_n = int32_t(ceil_div(N, tile));
   }
-  splits = std::max<int64_t>(1, std::min<int64_t>(splits, 64));
-  const int64_t per = ceil_div(steps, splits);
-  p.k_split = int32_t(std::min(per * inner, kMaxLength));
-  p.splits = int32_t(ceil_div(steps, per));
-  return p;
+  if (shape < 0) return false;
+  set_parts(x, shape, sx);
+  set_parts(w, shape, sw);
+  return true;
 }
 int64_t part_bytes(const Product& p, int64_t M) { return p.splits > 1 ? p.splits * M * p.ldp * 4 : 0; }
 
@@ -325,19 +398,11 @@ Backward plan_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, con
   p.chunks = int32_t(std::max<int64_t>(1, ceil_div(M, p.rows_per)));
   if (db) p.sums_bytes = round_up(p.chunks * N * 4, kWorkspaceAlign);
   const Operand dz = {p.make_dz ? nullptr : dy->data, p.make_dz ? p.lddz : dy->ld, true, M};
-  if (dx) {
-    p.px = plan_product(M, K, N, type, dz, {w->data, w->ld, false, K});
-    p.part_x = round_up(part_bytes(p.px, M), kWorkspaceAlign);
-  }
-  if (dw) {
-    p.pw = plan_product(N, K, M, type, {dz.data, dz.ld, false, N}, {x->data, x->ld, false, K});
-    p.part_w = round_up(part_bytes(p.pw, N), kWorkspaceAlign);
-  }
-  // Small products share a launch where both fit the chip at once: 200 x 1001 x
-  // 777 fp16 takes 18 us where the two in turn took 34.
-  auto workgroups = [](const Product& q) { return int64_t(q.tiles_m) * q.tiles_n * q.splits; };
-  p.pair = dx && dw && M > 0 && N > 0 && K > 0 && p.px.shape == ar::kTile128 && p.pw.shape == ar::kTile128 &&
-           p.px.aligned == p.pw.aligned && workgroups(p.px) + workgroups(p.pw) <= 2 * kCus;
+  if (dx) p.px = plan_product(M, K, N, type, dz, {w->data, w->ld, false, K});
+  if (dw) p.pw = plan_product(N, K, M, type, {dz.data, dz.ld, false, N}, {x->data, x->ld, false, K});
+  p.pair = dx && dw && M > 0 && N > 0 && K > 0 && plan_pair(p.px, p.pw, type);
+  if (dx) p.part_x = round_up(part_bytes(p.px, M), kWorkspaceAlign);
+  if (dw) p.part_w = round_up(part_bytes(p.pw, N), kWorkspaceAlign);
   return p;
 }
 
@@ -558,7 +623,7 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
       gw = gemm_args(p.pw, M, {gz, ldg, false, N}, {x->data, x->ld, false, K}, e, static_cast<char*>(part) + p.part_x);
     }
     if (run_x && run_w && p.pair) {
-      launched(ar::launch_gemm_pair(gx, gw, elem_of(type), p.px.aligned, stream), "gradient kernel launch");
+      launched(ar::launch_gemm_pair(gx, gw, elem_of(type), p.px.aligned, p.px.shape, stream), "gradient kernel launch");
     } else {
       if (run_x) run_product(p.px, gx, elem_of(type), true, false, stream, "input gradient kernel launch");
       if (run_w) run_product(p.pw, gw, elem_of(type), false, false, stream, "weight gradient kernel launch");

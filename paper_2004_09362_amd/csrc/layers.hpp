@@ -66,10 +66,10 @@ int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool align
 
 // The gradient's products with respect to x (a k-major, b not) and w (neither)
 // in one launch, on tiles of 128 x 128.
-int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, void* stream);
-int launch_gemm_pair_f32(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
-int launch_gemm_pair_f16(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
-int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, void* stream);
+int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, int32_t shape, void* stream);
+int launch_gemm_pair_f32(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream);
+int launch_gemm_pair_f16(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream);
+int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream);
 
 // Products of few rows (both operands k-major): gemm_few.hip.
 constexpr int32_t kFewMaxRows = 64;

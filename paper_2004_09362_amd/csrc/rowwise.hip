@@ -144,7 +144,8 @@ __device__ __forceinline__ void join(const GemmArgs& g, const FastDiv& groups, u
   if (m >= uint32_t(g.e.M)) return;
   const float* part = g.part + int64_t(m) * g.ldp + n;
   const int64_t step = int64_t(g.e.M) * g.ldp;
-  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0}, bias[8];
+  float w[1][8] = {{0, 0, 0, 0, 0, 0, 0, 0}}, bias[8];
+  float(&v)[8] = w[0];
   Residual<8> res[1];
   const int have = g.e.N - int32_t(n), back = have < 8 ? 8 - have : 0;
   load_bias<T, 8>(bias, g.e, int32_t(n), back);
@@ -157,7 +158,7 @@ __device__ __forceinline__ void join(const GemmArgs& g, const FastDiv& groups, u
     v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
   }
   // ldp is a multiple of 8: whole groups lie there
-  if (g.e.N >= 8) emit<T, 8>(v, bias, res[0], g.e, int32_t(m), int32_t(n), back);
+  if (g.e.N >= 8) emit<T, 8, 1>(w, bias, res, g.e, int32_t(m), 1, int32_t(n), back);
   else emit_tail<T, 8, 1>([&](int, int i) { return v[i]; }, g.e, int32_t(m), 1, int32_t(n), have);
 }
 
