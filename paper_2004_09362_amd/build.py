@@ -35,8 +35,9 @@ GENDIR = os.path.join(OBJDIR, "gen")
 # kernel of fused_free.hpp -- in COL_UNITS
 # generated units that share the P values round-robin, so that they compile
 # in parallel.  Fifteen of them (about 90 s each) and fused_group.hip (about
-# 60 s), started first, keep eight cores busy to the end: about 180 s in all,
-# where eight column units (160 s) followed by fused_group.hip took 216 s.
+# 60 s), started first, keep eight cores busy to the end: about 180 s, where
+# eight column units (160 s) followed by fused_group.hip took 216 s, and 230 s
+# with the layer operators' units.
 COL_UNITS = 15
 COL_KINDS = ("bo", "mid", "rot")
 
@@ -185,7 +186,7 @@ def kernel_families(kernel: str) -> list[str]:
                             ("fused_small_kernel", "small"), ("fused_wide_kernel", "col"),
                             ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast"),
                             ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer"),
-                            ("column_sums_kernel", "layer")):
+                            ("layer")):
             if part.startswith(prefix):
                 out.append(fam)
                 break

