@@ -14,9 +14,8 @@
 // 8192 x 16384 x 4096 785 us (1400 TFLOP/s), its input gradient 755 us, 4096^3
 // 93 us; a step of one tile 0.96 us, 0.43 us of it the products' own at full
 // clock, and up to 1.4 us where the chip lowers its clock for its power.
-// Around a tile's steps lie 4000 cycles until its first loads are there and
-// 8000 to 23000 of the epilogue, which nothing hides: one tile takes a compute
-// unit's LDS.  Smaller products take 128 x 128 tiles, two to a unit, which hide
+// Around a tile's steps lie 4000 cycles until its first loads are there, and
+// the epilogue, which nothing hides: one tile takes a compute unit's LDS.  Smaller products take 128 x 128 tiles, two to a unit, which hide
 // each other's but read LDS twice as much for each product.  fp32: 2048 x 4096
 // x 1024 124 us (138 TFLOP/s; the unit's rate is 157).
 //

@@ -444,3 +444,34 @@ def test_every_end_of_a_row(dtype, out32):
         kept = ref.drop(before[:, 1:N + 1].double().cpu(), d)
         ref.close(v, kept, 4 * ref.E32 * kept.abs(), "dropped")
         assert torch.equal(wide[:, :1], before[:, :1]) and torch.equal(wide[:, N + 1:], before[:, N + 1:])
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=IDS[:2])
+def test_forward_large_tiles_to_float32(dtype):
+    """256 x 256 tiles with a residual and results of 32 bits, in place, with every stage and with the residual alone."""
+    M, N, K = 256 * 15 + 8, 256 * 13 + 40, 136
+    g = seeded(21, M, N)
+    x, w, bias, r = matrix(g, M, K, dtype), matrix(g, N, K, dtype, K ** -0.5), matrix(g, 1, N, dtype)[0], matrix(g, M, N, torch.float32)
+    d = (0.1, 9, 8, 1 << 40)
+    for act, drop in (("silu", d), ("none", None)):
+        wy, wz, off, _ = ref.forward(x, w, bias, r, act, drop)
+        y = r.clone()
+        ar.ar_linear_forward(x, w, bias, y, activation=act, dropout=drop and ar.Dropout(*drop), out=y)
+        ref.close(y, wy, off, act)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_backward_products_together(dtype):
+    """Gradients of medium size, whose products share a launch, one of them split, added to what is there."""
+    for M, N, K in ((6100, 1000, 1032), (2048, 1280, 768), (700, 2050, 515)):
+        print("[gpu] products together", dtype, M, N, K, flush=True)
+        g = seeded(22, M)
+        dy, x, w = matrix(g, M, N, dtype, 0.1), matrix(g, M, K, dtype), matrix(g, N, K, dtype, K ** -0.5)
+        want = ref.backward(dy, x, w)
+        dw, db = matrix(g, N, K, torch.float32), matrix(g, 1, N, torch.float32)[0]
+        before = {"dw": dw.clone().double().cpu(), "db": db.clone().double().cpu()}
+        dx, _, _ = ar.ar_linear_backward(dy, x, w, dw=dw, db=db, accumulate=True)
+        ref.close(dx, want["dx"][0], want["dx"][1], "dx")
+        for name, t in (("dw", dw), ("db", db)):
+            sum_ = before[name] + want[name][0]
+            ref.close(t, sum_, want[name][1] + 4 * ref.E32 * (before[name].abs() + want[name][0].abs()), name)
