@@ -131,9 +131,13 @@ __device__ __forceinline__ i32x4v load_whole(const void* p) {
 // (load_end), without a branch, so that the loads of several chunks go out
 // together, and then shifted (end_chunk).
 template <typename T>
-__device__ __forceinline__ i32x4v load_end(const T* p, int64_t have) {
+__host__ __device__ __forceinline__ const T* end_at(const T* p, int64_t have) {
   constexpr int V = 16 / int(sizeof(T));
-  return load_whole<T>(p + ((have < V ? int(have) : V) - V));
+  return p + ((have < V ? int(have) : V) - V);
+}
+template <typename T>
+__device__ __forceinline__ i32x4v load_end(const T* p, int64_t have) {
+  return load_whole<T>(end_at(p, have));
 }
 template <typename T>
 __device__ __forceinline__ i32x4v end_chunk(const i32x4v& raw, int64_t have) {
@@ -223,7 +227,7 @@ struct Operand {
   static_assert(kSlots * THREADS == kChunks && kSlotRows * kRowChunks == THREADS, "whole slots");
 
   // Chunk c of tile row r lies at position c ^ swz(r).
-  __device__ static __forceinline__ int swz(int r) {
+  __host__ __device__ static __forceinline__ int swz(int r) {
     if constexpr (KMAJOR) return FIRST ? (r & 3) | ((r >> 1) & 4) : r & 7;
     else if constexpr (sizeof(T) == 2) return FIRST ? ((r & 1) << 2) | ((r >> 1) & 1) : (r & 3) << 1;
     else return FIRST ? ((r >> 2) & 1) | (r & 8) : (r & 12);
@@ -232,16 +236,21 @@ struct Operand {
   const char* base;   // element (first row, first inner index of the split)
   int64_t ld;         // bytes between rows of the matrix
   int32_t rows;       // rows of the output left from the tile's first one
-  bool near, wide;    // whether a tile's offsets fit 32 bits; whether the matrix' rows have 16 bytes
+  bool open, wide;    // whether every tile but the last may be loaded without a check; whether the matrix' rows have 16 bytes
   uint32_t voff[kSlots];
 
   // Byte offsets of this thread's chunks from the tile's first element.  A
   // chunk of rows past the last is read from the last (k-major) or the first
   // (otherwise): its products land in sums that are never stored.
-  __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int64_t inner, int tid) {
+  __host__ __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int64_t inner, int tid) {
     ld = ld_elems * int64_t(sizeof(T));
     rows = int32_t(nrows - row0 < R ? nrows - row0 : R);
-    near = ld <= kMaxTileLd;
+    open = ld <= kMaxTileLd;
+    if constexpr (!KMAJOR) {
+      // the last chunk of the row before the last tile ends within the rows of that one
+      const int64_t last_rows = inner - (inner - 1) / kInner * kInner, last_chunk = (nrows - 1) / kElems * kElems;
+      open = open && last_chunk + kElems <= last_rows * ld_elems + nrows;
+    }
     wide = (KMAJOR ? inner : nrows) >= kElems;
     base = reinterpret_cast<const char*>(p) +
            (KMAJOR ? row0 * ld + k0 * int64_t(sizeof(T)) : k0 * ld + row0 * int64_t(sizeof(T)));
@@ -254,9 +263,9 @@ struct Operand {
   }
 
   // Bytes from an inner tile to the next.
-  __device__ __forceinline__ int64_t step() const { return KMAJOR ? int64_t(kTileKBytes) : kInner * ld; }
+  __host__ __device__ __forceinline__ int64_t step() const { return KMAJOR ? int64_t(kTileKBytes) : kInner * ld; }
   // The start of inner tile t.
-  __device__ __forceinline__ const char* at(int32_t t) const {
+  __host__ __device__ __forceinline__ const char* at(int32_t t) const {
     return base + t * step();
   }
 
@@ -267,33 +276,41 @@ struct Operand {
   }
   __device__ __forceinline__ void issue(const char* p, int i) const { load_to_lds(p, voff[i]); }
 
-  // A tile into registers.  One that is not the last (and whose offsets fit 32
-  // bits) is loaded without a check, so that the loads go out together: what
-  // it takes from behind a row's end are elements of the matrix' next row, or
-  // lie between the two, and land in sums that are never stored.
+  // A tile into registers.  One that is not the last, of an operand that is
+  // open, is loaded without a check, so that the loads go out together: what it
+  // takes from behind a row's end are elements of the matrix' next rows, or lie
+  // between rows, and land in sums that are never stored.  Open are those whose
+  // offsets within a tile fit 32 bits, but for one that is not k-major and has
+  // rows so much shorter than 16 bytes that a chunk of the last row before the
+  // last tile reaches past that tile's few rows, the end of the matrix (1 column
+  // of halves whose inner length is 64 t + 1 to 6, 2 with 1 or 2, 3 with 1; of
+  // floats 1 column, 32 t + 1 or 2): its tiles are all checked, two at a time.
   __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t) const {
     const char* p = at(t);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) reg[i] = load_whole<T>(p + voff[i]);
   }
-  // Tile t, of which k_have inner indices exist.  Rows past the last one
-  // (k-major): that one's, whose products are never stored; inner indices past
-  // the last one (otherwise): zeros.
+  // This thread's chunk i of tile t, of which k_have inner indices exist: where
+  // it starts, and how many of its elements are there (negative: it lies that far
+  // behind the row's end).  Rows past the last one (k-major): that one's, whose
+  // products are never stored; inner indices past the last one (otherwise): none.
+  __host__ __device__ __forceinline__ const T* chunk(int32_t t, int64_t k_have, int i, int tid, int64_t& have) const {
+    const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
+    const bool there = KMAJOR || r < k_have;
+    const int64_t row = KMAJOR ? (r < rows ? r : rows - 1) : (there ? r : 0);
+    const T* p = reinterpret_cast<const T*>(at(t) + row * ld + c * 16);
+    have = KMAJOR ? k_have - c * kElems : rows - c * kElems;
+    if (!there && have > 0) {  // a chunk of the tile's first row is loaded and dropped whole
+      p += have;
+      have = 0;
+    }
+    return p;
+  }
   __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
     const T* p[kSlots];
     int64_t have[kSlots];
 #pragma unroll
-    for (int i = 0; i < kSlots; ++i) {
-      const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
-      const bool there = KMAJOR || r < k_have;
-      const int64_t row = KMAJOR ? (r < rows ? r : rows - 1) : (there ? r : 0);
-      p[i] = reinterpret_cast<const T*>(at(t) + row * ld + c * 16);
-      have[i] = KMAJOR ? k_have - c * kElems : rows - c * kElems;
-      if (!there && have[i] > 0) {  // a chunk of the tile's first row is loaded and dropped whole
-        p[i] += have[i];
-        have[i] = 0;
-      }
-    }
+    for (int i = 0; i < kSlots; ++i) p[i] = chunk(t, k_have, i, tid, have[i]);
     if (wide) {
 #pragma unroll
       for (int i = 0; i < kSlots; ++i) reg[i] = load_end(p[i], have[i]);
@@ -737,9 +754,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
           for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
       }
     };
-    const bool near = a.near && b.near;
+    const bool open = a.open && b.open;
     int32_t t = 0;
-    if (near && tiles > 4) {
+    if (open && tiles > 4) {
       a.load(xa0, 0);
       b.load(xb0, 0);
       a.load(xa1, 1);
@@ -785,7 +802,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
       }
     } else {  // few tiles, or rows far apart: two tiles at a time, the next two on their way
       auto get = [&](i32x4v (&xa)[OpA::kSlots], i32x4v (&xb)[OpB::kSlots], int32_t at) {
-        if (near && at + 1 < tiles) {
+        if (open && at + 1 < tiles) {
           a.load(xa, at);
           b.load(xb, at);
         } else if (at < tiles) {
