@@ -159,8 +159,9 @@ __device__ __forceinline__ float normal_tail(float z, float& gauss) {
 __device__ __forceinline__ float act_relu(float z) { return z > 0.0f ? z : (z != z ? z : 0.0f); }
 __device__ __forceinline__ float act_gelu(float z) {
   float gauss;
-  const float q = z * normal_tail(z, gauss);
-  return z > 0.0f ? z - q : q;
+  const float q = normal_tail(z, gauss);
+  // far out the tail is 0, which an infinite z would make NaN
+  return z > 0.0f ? z - __builtin_fminf(z, 64.0f) * q : z * q;
 }
 // (1 + tanh(u)) / 2 is the logistic function of 2 u.
 __device__ __forceinline__ float act_gelu_tanh(float z) {

@@ -33,3 +33,55 @@ def test_gradients_of_narrow_layers(dtype):
                 want = ref.backward(dy, x, w)
                 for name, t in zip(("dx", "dw", "db"), ar.ar_linear_backward(dy, x, w, dw_dtype=torch.float32)):
                     ref.close(t, want[name][0], want[name][1], name)
+
+
+def extremes(dtype):
+    big = [6e4, 65504.0] if dtype == torch.float16 else [1e4, 1.8e19, 2e19, 1e20, 1e30, 3e38]
+    return torch.tensor([0.0, 1.0, -1.0, 30.0, -30.0, 300.0, -300.0] + big + [-v for v in big] + [math.inf, -math.inf, math.nan])
+
+
+def act_far_out(z, act):
+    """The activations in 64 bits, in forms that stay finite for finite z; at -inf they are -inf * 0."""
+    if act == "relu":
+        return torch.where(z > 0, z, 0.0 * z.nan_to_num(posinf=0, neginf=0, nan=math.nan))
+    if act == "gelu":
+        return z * torch.special.ndtr(z)
+    u = z if act == "silu" else 2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)
+    return z * torch.sigmoid(u)
+
+
+def agree(got, want, where):
+    """NaN and infinities in the same places; elsewhere the size of the rounding, and of the activation's evaluation."""
+    g, w = got.double().cpu(), want
+    u = ref.U[got.dtype]
+    w = torch.where(w.abs() > torch.finfo(got.dtype).max, w.sign() * math.inf, w)
+    assert torch.equal(g.isnan(), w.isnan()), (where, g, w)
+    assert torch.equal(g.isinf(), w.isinf()) and torch.equal(g.sign()[g.isinf()], w.sign()[w.isinf()]), (where, g, w)
+    ok = w.isfinite()
+    assert bool(((g - w).abs()[ok] <= (u + 2.0 ** -22) * w.abs()[ok] + 2.0 ** -20).all()), (where, g, w)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_activations_at_infinities_and_far_out(dtype, act):
+    """Every kernel that applies an activation: of few rows, of tiles (at a matrix' edge, whole ones, through 16-byte
+    boundaries and not), and the join of a split product."""
+    v = extremes(dtype)
+    z1 = v.to(dtype)
+    for M, N, K, pad in ((len(v), 1, 1, 0), (1, len(v), 1, 0), (len(v), 70, 1, 3), (200, 130, 1, 0), (200, 136, 8, 0), (len(v), 24, 9000, 0),
+                         (256 * 15 + 40, 256 * 13 - 24, 200, 0)):
+        print("[gpu] far out", dtype, act, M, N, K, flush=True)
+        x = torch.zeros(M, K + pad, dtype=dtype)[:, :K]
+        w = torch.zeros(N, K + pad, dtype=dtype)[:, :K]
+        if M == 1:  # a row of values
+            x[:, 0] = 1
+            w[:, 0] = z1
+        else:
+            x[:, 0] = z1[torch.arange(M) % len(v)]
+            w[:, 0] = 1
+        x, w = x.to(DEV), w.to(DEV)
+        y, z = ar.ar_linear_forward(x, w, activation=act, preact=True)
+        want = z1.double() if M == 1 else z1.double()[torch.arange(M) % len(v)][:, None].expand(M, N)
+        if K > 1:  # the zeros of w make an infinity's row NaN only where they meet it, which is nowhere
+            assert torch.equal(z.cpu().isnan(), want.reshape(M, N).isnan())
+        agree(y, act_far_out(want.reshape(M, N), act), (M, N, K))
