@@ -514,7 +514,9 @@ ar_status ar_linear_forward_workspace(int64_t M, int64_t N, int64_t K, const ar_
  * several calls; a gradient buffer that is a rank buffer of a plan).  db sums
  * dz in 32 bits.  The two products take dz in x's type, since the matrix
  * instructions do: where act or drop is there, or dy is wider than x, dz is
- * rounded to it, once.  x is not read without dw, nor w without dx.
+ * rounded to it, once (who needs more bits there passes x and w in float32).
+ * At an infinite pre-activation the slopes of the last three activations are
+ * inf * 0, NaN; relu's is 0 at NaN.  x is not read without dw, nor w without dx.
  * Workspace and errors as above. */
 ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* dy, const ar_matrix* x,
                              const ar_matrix* w, const ar_matrix* preact, ar_activation act, const ar_dropout* drop,

@@ -175,7 +175,8 @@ __device__ __forceinline__ float slope_gelu(float z) {
   return __builtin_fmaf(z * kInvSqrt2Pi, gauss, z > 0.0f ? 1.0f - q : q);
 }
 __device__ __forceinline__ float slope_gelu_tanh(float z) {
-  const float t = z * z;
+  // far out g or 1 - g is 0, which must not meet an infinite square
+  const float t = __builtin_fminf(z * z, 1e8f);
   const float g = logistic2(z * __builtin_fmaf(-kLog2e * kGeluTanh2 * kGeluCubic, t, -kLog2e * kGeluTanh2));
   return __builtin_fmaf(z * g * (1.0f - g), __builtin_fmaf(3.0f * kGeluCubic * kGeluTanh2, t, kGeluTanh2), g);
 }

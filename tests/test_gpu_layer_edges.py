@@ -50,6 +50,18 @@ def act_far_out(z, act):
     return z * torch.sigmoid(u)
 
 
+def slope_far_out(z, act):
+    """Their slopes: at infinities inf * 0, but for relu's, which is 0 at NaN too."""
+    if act == "relu":
+        return (z > 0).double()
+    if act == "gelu":
+        return torch.special.ndtr(z) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    u, du = (z, torch.ones_like(z)) if act == "silu" else (2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3),
+                                                         2 * math.sqrt(2 / math.pi) * (1 + 0.134145 * z ** 2))
+    s = torch.sigmoid(u)
+    return s + z * s * (1 - s) * du
+
+
 def agree(got, want, where):
     """NaN and infinities in the same places; elsewhere the size of the rounding, and of the activation's evaluation."""
     g, w = got.double().cpu(), want
@@ -85,3 +97,26 @@ def test_activations_at_infinities_and_far_out(dtype, act):
         if K > 1:  # the zeros of w make an infinity's row NaN only where they meet it, which is nowhere
             assert torch.equal(z.cpu().isnan(), want.reshape(M, N).isnan())
         agree(y, act_far_out(want.reshape(M, N), act), (M, N, K))
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+def test_slopes_at_infinities_and_far_out(dtype, act):
+    """db of one row is the slope in 32 bits; dx of one column is it in the operands' type; rows of 8 columns and shorter ones."""
+    v = extremes(dtype)
+    z1 = v.to(dtype)
+    want = slope_far_out(z1.double(), act)
+    row = z1[None].to(DEV)
+    _, _, db = ar.ar_linear_backward(torch.ones_like(row), torch.ones(1, 1, dtype=dtype, device=DEV),
+                                     torch.ones(len(v), 1, dtype=dtype, device=DEV), preact=row, activation=act, dx=False, dw=False,
+                                     dw_dtype=torch.float32)
+    agree(db, want, "db")
+    for i in range(0, len(v), 5):  # rows shorter than 8
+        _, _, db = ar.ar_linear_backward(torch.ones(1, 5, dtype=dtype, device=DEV)[:, :len(v) - i], torch.ones(1, 1, dtype=dtype, device=DEV),
+                                         torch.ones(min(5, len(v) - i), 1, dtype=dtype, device=DEV), preact=row[:, i:i + 5], activation=act,
+                                         dx=False, dw=False, dw_dtype=torch.float32)
+        agree(db, want[i:i + 5], "db of short rows")
+    column = z1[:, None].to(DEV)
+    dx, _, _ = ar.ar_linear_backward(torch.ones_like(column), column, torch.ones(1, 1, dtype=dtype, device=DEV), preact=column,
+                                     activation=act, dw=False, db=False)
+    agree(dx[:, 0], want, "dx")
