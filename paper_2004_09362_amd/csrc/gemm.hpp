@@ -236,7 +236,7 @@ struct Operand {
   const char* base;   // element (first row, first inner index of the split)
   int64_t ld;         // bytes between rows of the matrix
   int32_t rows;       // rows of the output left from the tile's first one
-  bool open, wide;    // whether every tile but the last may be loaded without a check; whether the matrix' rows have 16 bytes
+  bool wide;          // whether the matrix' rows have 16 bytes
   uint32_t voff[kSlots];
 
   // Byte offsets of this thread's chunks from the tile's first element.  A
@@ -245,12 +245,6 @@ struct Operand {
   __host__ __device__ __forceinline__ void init(const T* p, int64_t ld_elems, int64_t row0, int64_t k0, int64_t nrows, int64_t inner, int tid) {
     ld = ld_elems * int64_t(sizeof(T));
     rows = int32_t(nrows - row0 < R ? nrows - row0 : R);
-    open = ld <= kMaxTileLd;
-    if constexpr (!KMAJOR) {
-      // the last chunk of the row before the last tile ends within the rows of that one
-      const int64_t last_rows = inner - (inner - 1) / kInner * kInner, last_chunk = (nrows - 1) / kElems * kElems;
-      open = open && last_chunk + kElems <= last_rows * ld_elems + nrows;
-    }
     wide = (KMAJOR ? inner : nrows) >= kElems;
     base = reinterpret_cast<const char*>(p) +
            (KMAJOR ? row0 * ld + k0 * int64_t(sizeof(T)) : k0 * ld + row0 * int64_t(sizeof(T)));
@@ -277,40 +271,37 @@ struct Operand {
   __device__ __forceinline__ void issue(const char* p, int i) const { load_to_lds(p, voff[i]); }
 
   // A tile into registers.  One that is not the last, of an operand that is
-  // open, is loaded without a check, so that the loads go out together: what it
-  // takes from behind a row's end are elements of the matrix' next rows, or lie
-  // between rows, and land in sums that are never stored.  Open are those whose
-  // offsets within a tile fit 32 bits, but for one that is not k-major and has
-  // rows so much shorter than 16 bytes that a chunk of the last row before the
-  // last tile reaches past that tile's few rows, the end of the matrix (1 column
-  // of halves whose inner length is 64 t + 1 to 6, 2 with 1 or 2, 3 with 1; of
-  // floats 1 column, 32 t + 1 or 2): its tiles are all checked, two at a time.
+  // open (tiles_open in layers.hpp), is loaded without a check, so that the loads
+  // go out together: what it takes from behind a row's end are elements of the
+  // matrix' next rows, or lie between rows, and land in sums that are never stored.
   __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t) const {
     const char* p = at(t);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) reg[i] = load_whole<T>(p + voff[i]);
   }
-  // This thread's chunk i of tile t, of which k_have inner indices exist: where
-  // it starts, and how many of its elements are there (negative: it lies that far
-  // behind the row's end).  Rows past the last one (k-major): that one's, whose
-  // products are never stored; inner indices past the last one (otherwise): none.
-  __host__ __device__ __forceinline__ const T* chunk(int32_t t, int64_t k_have, int i, int tid, int64_t& have) const {
-    const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
-    const bool there = KMAJOR || r < k_have;
-    const int64_t row = KMAJOR ? (r < rows ? r : rows - 1) : (there ? r : 0);
-    const T* p = reinterpret_cast<const T*>(at(t) + row * ld + c * 16);
-    have = KMAJOR ? k_have - c * kElems : rows - c * kElems;
-    if (!there && have > 0) {  // a chunk of the tile's first row is loaded and dropped whole
-      p += have;
-      have = 0;
+  // This thread's chunks of tile t, of which k_have inner indices exist: where
+  // they start, and how many of their elements are there (negative: it lies that
+  // far behind the row's end).  Rows past the last one (k-major): that one's,
+  // whose products are never stored; inner indices past the last one
+  // (otherwise): none.
+  __host__ __device__ __forceinline__ void chunks(const T* (&p)[kSlots], int64_t (&have)[kSlots], int32_t t, int64_t k_have, int tid) const {
+#pragma unroll
+    for (int i = 0; i < kSlots; ++i) {
+      const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
+      const bool there = KMAJOR || r < k_have;
+      const int64_t row = KMAJOR ? (r < rows ? r : rows - 1) : (there ? r : 0);
+      p[i] = reinterpret_cast<const T*>(at(t) + row * ld + c * 16);
+      have[i] = KMAJOR ? k_have - c * kElems : rows - c * kElems;
+      if (!there && have[i] > 0) {  // a chunk of the tile's first row is loaded and dropped whole
+        p[i] += have[i];
+        have[i] = 0;
+      }
     }
-    return p;
   }
   __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
     const T* p[kSlots];
     int64_t have[kSlots];
-#pragma unroll
-    for (int i = 0; i < kSlots; ++i) p[i] = chunk(t, k_have, i, tid, have[i]);
+    chunks(p, have, t, k_have, tid);
     if (wide) {
 #pragma unroll
       for (int i = 0; i < kSlots; ++i) reg[i] = load_end(p[i], have[i]);
@@ -754,7 +745,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
           for (int j = 0; j < NT; ++j) acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
       }
     };
-    const bool open = a.open && b.open;
+    const bool open = g.open;
     int32_t t = 0;
     if (open && tiles > 4) {
       a.load(xa0, 0);

@@ -345,13 +345,15 @@ bool plan_pair(Product& x, Product& w, ar_dtype type) {
 }
 int64_t part_bytes(const Product& p, int64_t M) { return p.splits > 1 ? p.splits * M * p.ldp * 4 : 0; }
 
-ar::GemmArgs gemm_args(const Product& p, int64_t K, const Operand& a, const Operand& b, const ar::Epilogue& e, void* part) {
+ar::GemmArgs gemm_args(const Product& p, int64_t K, ar_dtype type, const Operand& a, const Operand& b, const ar::Epilogue& e,
+                       void* part) {
   ar::GemmArgs g{};
   g.a = a.data;
   g.b = b.data;
   g.lda = a.ld;
   g.ldb = b.ld;
   g.K = int32_t(K);
+  g.open = ar::tiles_open(a.kmajor, a.rows, K, a.ld, size_of(type)) && ar::tiles_open(b.kmajor, b.rows, K, b.ld, size_of(type));
   g.tiles_m = p.tiles_m;
   g.tiles_n = p.tiles_n;
   g.splits = p.splits;
@@ -529,7 +531,7 @@ ar_status ar_linear_forward(int64_t M, int64_t N, int64_t K, const ar_matrix* x,
       e.z = preact->data;
       e.ldz = preact->ld;
     }
-    const ar::GemmArgs g = gemm_args(p, K, a, b, e, workspace);
+    const ar::GemmArgs g = gemm_args(p, K, x->dtype, a, b, e, workspace);
     run_product(p, g, elem_of(x->dtype), true, true, stream, "linear kernel launch");
     if (p.splits > 1) launched(ar::launch_join(g, ar::GemmArgs{}, ar::SumsCall{}, elem_of(x->dtype), stream), "join kernel launch");
   });
@@ -610,7 +612,7 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
       e.M = int32_t(M);
       e.N = int32_t(K);
       e.y_f32 = dx->dtype == AR_FLOAT32;
-      gx = gemm_args(p.px, N, {gz, ldg, true, M}, {w->data, w->ld, false, K}, e, part);
+      gx = gemm_args(p.px, N, type, {gz, ldg, true, M}, {w->data, w->ld, false, K}, e, part);
     }
     if (run_w) {
       e.y = dw->data;
@@ -622,7 +624,7 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
         e.res = dw->data;
         e.ldr = dw->ld;
       }
-      gw = gemm_args(p.pw, M, {gz, ldg, false, N}, {x->data, x->ld, false, K}, e, static_cast<char*>(part) + p.part_x);
+      gw = gemm_args(p.pw, M, type, {gz, ldg, false, N}, {x->data, x->ld, false, K}, e, static_cast<char*>(part) + p.part_x);
     }
     if (run_x && run_w && p.pair) {
       launched(ar::launch_gemm_pair(gx, gw, elem_of(type), p.px.aligned, p.px.shape, stream), "gradient kernel launch");

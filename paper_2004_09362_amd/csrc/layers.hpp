@@ -39,7 +39,7 @@ struct GemmArgs {
   const void* a;
   const void* b;
   int64_t lda, ldb;
-  int32_t K;
+  int32_t K, open;  // open: tiles_open of both operands
   int32_t tiles_m, tiles_n;
   int32_t splits, k_split;  // inner length dealt out: split s takes [s * k_split, min(K, (s + 1) * k_split))
   float* part;              // splits > 1: partial sums [splits][M][ldp]
@@ -56,6 +56,21 @@ constexpr int32_t tile_rows(int32_t shape) { return shape == kTile256 ? 256 : 12
 
 // The largest distance of two rows in bytes at which a tile's offsets fit 32 bits.
 constexpr int64_t kMaxTileLd = int64_t(1) << 23;
+
+// Whether every tile but the last of an operand (rows along the output, inner
+// indices, ld in elements) may be loaded through registers without a check:
+// offsets within a tile fit 32 bits, and where the operand is not k-major, the
+// last 16 bytes of the last row before the last tile end within that tile's rows.
+// They do not where rows are much shorter than 16 bytes and few are left: 1
+// column of halves whose inner length is 64 t + 1 to 6, 2 with 1 or 2, 3 with 1; of
+// floats 1 column, 32 t + 1 or 2.  All tiles of such an operand are checked.
+constexpr bool tiles_open(bool kmajor, int64_t rows, int64_t inner, int64_t ld, int64_t elem_bytes) {
+  if (inner < 1 || rows < 1) return true;  // nothing is loaded
+  const int64_t per = 16 / elem_bytes, tile = kTileKBytes / elem_bytes, last_rows = (inner - 1) % tile + 1;
+  if (kmajor) return rows == 1 || ld * elem_bytes <= kMaxTileLd;
+  if (inner <= tile) return true;  // the last tile is the only one
+  return ld * elem_bytes <= kMaxTileLd && (rows - 1) / per * per + per <= last_rows * ld + rows;
+}
 
 // elem: Elem; a_kmajor / b_kmajor as above (a k-major b with a not is not
 // provided); aligned: whether the asynchronous loads apply (see gemm.hpp).

@@ -46,6 +46,7 @@ struct Replay {
     bytes = ((height - 1) * ld + width) * int64_t(sizeof(T));
     first = reinterpret_cast<const char*>(uintptr_t(1) << 40);
     // what the host asks of operands that are loaded asynchronously
+    const bool open = tiles_open(KMAJOR, rows, inner, ld, sizeof(T));
     const bool async = ld % Op::kElems == 0 && (KMAJOR || rows % Op::kElems == 0);
     for (int64_t row0 = 0; row0 < rows; row0 += R) {
       for (int64_t k0 = 0; k0 < inner; k0 += part * Op::kInner) {
@@ -55,12 +56,15 @@ struct Replay {
           Op op;
           op.init(reinterpret_cast<const T*>(first), ld, row0, k0, rows, inner, tid);
           for (int t = 0; t < tiles; ++t) {
+            const T* chunk[Op::kSlots];
+            int64_t there[Op::kSlots];
+            op.chunks(chunk, there, t, klen - int64_t(t) * Op::kInner, tid);
             for (int i = 0; i < Op::kSlots; ++i) {
               const char* const plain = op.at(t) + op.voff[i];
-              if (op.open && t + 1 < tiles && !inside(plain, 16, "unchecked chunk", row0, k0, t)) return false;
+              if (open && t + 1 < tiles && !inside(plain, 16, "unchecked chunk", row0, k0, t)) return false;
               if (async && t < whole && !inside(plain, 16, "asynchronous chunk", row0, k0, t)) return false;
-              int64_t have;
-              const T* const p = op.chunk(t, klen - int64_t(t) * Op::kInner, i, tid, have);
+              const int64_t have = there[i];
+              const T* const p = chunk[i];
               if (op.wide) {
                 if (!inside(end_at(p, have), 16, "checked chunk", row0, k0, t)) return false;
               } else if (have > 0) {
