@@ -87,12 +87,9 @@ template <typename T>
 __device__ __forceinline__ void mma_pinned(const i32x4v& rows_n, const i32x4v& rows_m, f32x4v& acc) {
   if constexpr (elem_of<T>() == kBF16) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
-  } else if constexpr (elem_of<T>() == kF16) {
-    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
   } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      asm volatile("v_mfma_f32_16x16x4_f32 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n[e]), "v"(rows_m[e]));
+    static_assert(elem_of<T>() == kF16, "floats take tiles whose sums are not pinned");
+    asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(acc) : "v"(rows_n), "v"(rows_m));
   }
 }
 __device__ __forceinline__ void mma_ready() { asm volatile("s_nop 1"); }
@@ -920,7 +917,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
         auto sum = [&](int q, int i) {
           return reinterpret_cast<const float*>(unit_at((pass + q) * kPassRows + lane / kUnits))[i];
         };
-        emit_tail<T, 8, kAhead>(sum, g.e, m, kPassRows, n, have);
+        emit_tail<T, 8, kAhead, STAGES != kSums, STAGES == kFull>(sum, g.e, m, kPassRows, n, have);
       }
     }
   }

@@ -334,12 +334,12 @@ __device__ __forceinline__ void emit(float (&v)[Q][V], const float (&b)[V], cons
 // The same for the `have` < V columns of a row's end, of Q rows from m on `step`
 // apart, whose sums sum(q, i) gives, where the rows are shorter than V or only
 // few are left; all loads of the Q rows go out before the first is used.
-template <typename T, int V, int Q, typename F>
+template <typename T, int V, int Q, bool BIAS = true, bool STAGES = true, typename F>
 __device__ __forceinline__ void emit_tail(F&& sum, const Epilogue& e, int32_t m, int32_t step, int32_t n, int have) {
   float b[V], r[Q][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) b[i] = 0.0f;
-  if (e.bias) {
+  if (BIAS && e.bias) {
     if (e.bias_f32) load_tail<V>(b, static_cast<const float*>(e.bias) + n, have);
     else load_tail<V>(b, static_cast<const T*>(e.bias) + n, have);
   }
@@ -359,9 +359,11 @@ __device__ __forceinline__ void emit_tail(F&& sum, const Epilogue& e, int32_t m,
     float(&v)[V] = w[0];
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = i < have ? sum(q, i) + b[i] : 0.0f;
-    if (e.z) store_tail<V>(static_cast<T*>(e.z) + int64_t(row) * e.ldz + n, v, have);
-    activate(w, e.act);
-    if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(row), uint32_t(n));
+    if constexpr (STAGES) {
+      if (e.z) store_tail<V>(static_cast<T*>(e.z) + int64_t(row) * e.ldz + n, v, have);
+      activate(w, e.act);
+      if (e.drop.on) drop_some<V>(v, e.drop, e.drop.row0 + uint32_t(row), uint32_t(n));
+    }
     if (e.res) {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[i] += r[q][i];
