@@ -271,17 +271,17 @@ struct Operand {
   // open (tiles_open in layers.hpp), is loaded without a check, so that the loads
   // go out together: what it takes from behind a row's end are elements of the
   // matrix' next rows, or lie between rows, and land in sums that are never stored.
-  __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t) const {
+  __host__ __device__ __forceinline__ void load(i32x4v (&reg)[kSlots], int32_t t) const {
     const char* p = at(t);
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) reg[i] = load_whole<T>(p + voff[i]);
   }
-  // This thread's chunks of tile t, of which k_have inner indices exist: where
-  // they start, and how many of their elements are there (negative: it lies that
-  // far behind the row's end).  Rows past the last one (k-major): that one's,
-  // whose products are never stored; inner indices past the last one
-  // (otherwise): none.
-  __host__ __device__ __forceinline__ void chunks(const T* (&p)[kSlots], int64_t (&have)[kSlots], int32_t t, int64_t k_have, int tid) const {
+  // Tile t, of which k_have inner indices exist.  Rows past the last one
+  // (k-major): that one's, whose products are never stored; inner indices past
+  // the last one (otherwise): zeros.
+  __host__ __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
+    const T* p[kSlots];
+    int64_t have[kSlots];
 #pragma unroll
     for (int i = 0; i < kSlots; ++i) {
       const int s = i * THREADS + tid, r = s / kRowChunks, c = (s % kRowChunks) ^ swz(r);
@@ -294,11 +294,6 @@ struct Operand {
         have[i] = 0;
       }
     }
-  }
-  __device__ __forceinline__ void load_checked(i32x4v (&reg)[kSlots], int32_t t, int64_t k_have, int tid) const {
-    const T* p[kSlots];
-    int64_t have[kSlots];
-    chunks(p, have, t, k_have, tid);
     if (wide) {
 #pragma unroll
       for (int i = 0; i < kSlots; ++i) reg[i] = load_end(p[i], have[i]);

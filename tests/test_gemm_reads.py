@@ -1,8 +1,9 @@
 """Where the tiled products read, without a GPU.
 
-The address arithmetic of csrc/gemm.hpp is compiled for the host and run for
-every thread, slot and tile of a workgroup: whatever a tile's loads take lies
-between the first element of the operand's matrix and its last one."""
+The operands' loads of csrc/gemm.hpp are compiled for the host, with reads that
+say where they are, and run for every thread and tile of a workgroup: whatever
+they take lies between the first element of the operand's matrix and its last
+one."""
 import os
 import subprocess
 
@@ -14,26 +15,63 @@ PROGRAM = r"""
 #include <cstdio>
 #include <initializer_list>
 
+#include <hip/hip_runtime.h>
+
+// The loads as the host sees them: they say where they read.
+namespace ar {
+typedef int32_t i32x4v __attribute__((ext_vector_type(4)));
+void reads(const void* p, int64_t bytes);
+template <typename T> __host__ i32x4v load_whole(const void* p) {
+  reads(p, 16);
+  return i32x4v{};
+}
+template <typename T> __host__ i32x4v load_end(const T* p, int64_t have);
+template <typename T> __host__ i32x4v end_chunk(const i32x4v& raw, int64_t) { return raw; }
+template <typename T> __host__ i32x4v short_chunk(const T* p, int64_t have) {
+  const int64_t per = 16 / sizeof(T);
+  if (have > 0) reads(p, (have < per ? have : per) * int64_t(sizeof(T)));
+  return i32x4v{};
+}
+}  // namespace ar
+
 #include "gemm.hpp"
+
+namespace ar {
+template <typename T> __host__ i32x4v load_end(const T* p, int64_t have) {
+  reads(end_at(p, have), 16);
+  return i32x4v{};
+}
+}  // namespace ar
 
 using namespace ar;
 
+// The matrix at hand, and what is read of it.
+const char* first;
+int64_t bytes;  // to the end of its last row
 long checked = 0;
+bool outside = false;
+int64_t outside_from, outside_to;
+
+void ar::reads(const void* p, int64_t n) {
+  const int64_t from = static_cast<const char*>(p) - first;
+  ++checked;
+  if (from >= 0 && from + n <= bytes) return;
+  outside = true;
+  outside_from = from;
+  outside_to = from + n;
+}
 
 template <typename T, bool KMAJOR, bool FIRST, int R>
 struct Replay {
   using Op = Operand<T, KMAJOR, FIRST, R, 256>;
-  const char* first;
-  int64_t bytes;  // of the matrix: to the end of its last row
   int64_t rows, inner, ld;
 
-  bool inside(const void* p, int64_t n, const char* what, int64_t row0, int64_t k0, int t) {
-    const int64_t from = static_cast<const char*>(p) - first;
-    ++checked;
-    if (from >= 0 && from + n <= bytes) return true;
+  bool inside(const char* what, int64_t row0, int64_t k0, int t) {
+    if (!outside) return true;
     std::printf("%s of %d-byte elements, kmajor %d, tile of %d rows: rows %ld, inner length %ld, ld %ld, from row %ld and inner index %ld, "
                 "tile %d: bytes %ld to %ld of %ld\n", what, int(sizeof(T)), int(KMAJOR), R, long(rows), long(inner), long(ld), long(row0),
-                long(k0), t, long(from), long(from + n), long(bytes));
+                long(k0), t, long(outside_from), long(outside_to), long(bytes));
+    outside = false;
     return false;
   }
 
@@ -56,22 +94,14 @@ struct Replay {
           Op op;
           op.init(reinterpret_cast<const T*>(first), ld, row0, k0, rows, inner, tid);
           for (int t = 0; t < tiles; ++t) {
-            const T* chunk[Op::kSlots];
-            int64_t there[Op::kSlots];
-            op.chunks(chunk, there, t, klen - int64_t(t) * Op::kInner, tid);
-            for (int i = 0; i < Op::kSlots; ++i) {
-              const char* const plain = op.at(t) + op.voff[i];
-              if (open && t + 1 < tiles && !inside(plain, 16, "unchecked chunk", row0, k0, t)) return false;
-              if (async && t < whole && !inside(plain, 16, "asynchronous chunk", row0, k0, t)) return false;
-              const int64_t have = there[i];
-              const T* const p = chunk[i];
-              if (op.wide) {
-                if (!inside(end_at(p, have), 16, "checked chunk", row0, k0, t)) return false;
-              } else if (have > 0) {
-                const int64_t n = have < Op::kElems ? have : Op::kElems;
-                if (!inside(p, n * int64_t(sizeof(T)), "short chunk", row0, k0, t)) return false;
-              }
-            }
+            i32x4v reg[Op::kSlots];
+            if (open && t + 1 < tiles) op.load(reg, t);
+            if (!inside("unchecked tile", row0, k0, t)) return false;
+            op.load_checked(reg, t, klen - int64_t(t) * Op::kInner, tid);
+            if (!inside("checked tile", row0, k0, t)) return false;
+            if (async && t < whole)
+              for (int i = 0; i < Op::kSlots; ++i) reads(op.at(t) + op.voff[i], 16);
+            if (!inside("asynchronous tile", row0, k0, t)) return false;
           }
         }
       }
