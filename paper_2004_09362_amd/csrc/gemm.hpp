@@ -564,7 +564,7 @@ __device__ __forceinline__ void direct_full(const GemmArgs& g, const f32x4v (&ac
       if (i + 1 < MT) fetch(row + 16);
     }
     if (e.z) store(static_cast<T*>(e.z), e.ldz);
-    activate(v, e.act);
+    activate<T>(v, e.act);
     if (e.drop.on) {
 #pragma unroll
       for (int j = 0; j < kPairs; ++j) drop_some<8>(v[j], e.drop, e.drop.row0 + uint32_t(row), uint32_t(n + 32 * j));

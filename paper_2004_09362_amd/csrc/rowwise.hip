@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
         move_down<8>(v[q], back);
         if (c.z) move_down<8>(t[q], back);
         if (c.drop.on) drop_some<8>(v[q], c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
-        if (c.z) times_slope<8>(v[q], t[q], c.act);
+        if (c.z) times_slope<Z, 8>(v[q], t[q], c.act);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] += v[q][i];
         if (c.dz) store_group<8>(dz + row * c.lddz, v[q]);  // its rows have whole groups
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
       load_tail<8>(v, dy + row * c.lddy, have);
       load_tail<8>(t, z + row * c.ldz, c.z ? have : 0);
       if (c.drop.on) drop_some<8>(v, c.drop, c.drop.row0 + uint64_t(row), uint32_t(col));
-      if (c.z) times_slope<8>(v, t, c.act);
+      if (c.z) times_slope<Z, 8>(v, t, c.act);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += i < have ? v[i] : 0.0f;
       if (c.dz) store_tail<8>(dz + row * c.lddz, v, have);

@@ -120,3 +120,39 @@ def test_slopes_at_infinities_and_far_out(dtype, act):
     dx, _, _ = ar.ar_linear_backward(torch.ones_like(column), column, torch.ones(1, 1, dtype=dtype, device=DEV), preact=column,
                                      activation=act, dw=False, db=False)
     agree(dx[:, 0], want, "dx")
+
+
+def test_gelu_in_float32_is_good_to_its_value():
+    """gelu's negative side is a tail of the normal distribution times z, and its results are small: the error is bounded
+    by the result, not by 1.  The tail is a polynomial fitted to 1 unit of 2^-24, with its coefficients' roundings and eight
+    multiply-adds of partly alternating terms (3), a reciprocal of 2 that enters 1.5-fold (3), an exponential of 2 with a
+    corrected exponent (1) and three products (1.5): 12 units, and 16 = 2^-20 allowed.  The slope adds z times the density,
+    within 1.13 in all: 2^-20 of 1."""
+    n = 1 << 18
+    z = torch.linspace(-12.0, 12.0, n, device=DEV)
+    y = ar.ar_linear_forward(z[:, None], torch.ones(1, 1, device=DEV), activation="gelu")[:, 0]
+    zz = z.double()
+    tail = torch.special.erfc(-zz / math.sqrt(2)) / 2
+    worst = ((y.double() - zz * tail).abs() / (zz * tail).abs()).max()
+    assert float(worst) <= 2.0 ** -20, float(worst) * 2 ** 24
+    few = ar.ar_linear_forward(z[:64, None], torch.ones(1, 1, device=DEV), activation="gelu")[:, 0]
+    assert torch.equal(few, y[:64])
+    _, _, db = ar.ar_linear_backward(torch.ones(1, n, device=DEV), torch.ones(1, 1, device=DEV), torch.ones(n, 1, device=DEV),
+                                     preact=z[None], activation="gelu", dx=False, dw=False)
+    want = tail + zz * torch.exp(-zz * zz / 2) / math.sqrt(2 * math.pi)
+    assert float((db.double() - want).abs().max()) <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("dtype", TYPES[:2], ids=IDS[:2])
+def test_gelu_of_16_bits_is_good_to_its_value(dtype):
+    """From operands of 16 bits the tail is good to 6e-5 of itself and 60 units of 2^-24 (its exponent's rounding at z = -9),
+    7e-5 together, and the result is rounded once; below 16 bits' normal numbers by half their smallest step."""
+    z = torch.linspace(-9.0, 9.0, 1 << 16, device=DEV).to(dtype)
+    zz = z.double()
+    want = zz * torch.special.erfc(-zz / math.sqrt(2)) / 2
+    one = torch.ones(1, 1, dtype=dtype, device=DEV)
+    y = ar.ar_linear_forward(z[:, None], one, activation="gelu")[:, 0].double()
+    step = 2.0 ** -25 if dtype == torch.float16 else 2.0 ** -134
+    assert bool(((y - want).abs() <= (ref.U[dtype] * (1 + 7e-5) + 7e-5) * want.abs() + step).all())
+    y = ar.ar_linear_forward(z[:, None], one, activation="gelu", out_dtype=torch.float32)[:, 0].double()
+    assert bool(((y - want).abs() <= 7e-5 * want.abs()).all())
