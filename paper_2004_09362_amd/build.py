@@ -185,8 +185,7 @@ def kernel_families(kernel: str) -> list[str]:
                             ("fused_ring_kernel", "group"), ("fused_free_kernel", "free"),
                             ("fused_small_kernel", "small"), ("fused_wide_kernel", "col"),
                             ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast"),
-                            ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer"),
-                            ("layer")):
+                            ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer")):
             if part.startswith(prefix):
                 out.append(fam)
                 break

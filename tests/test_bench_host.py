@@ -115,6 +115,14 @@ def test_kernel_families_cover_every_source():
     assert b.source_hash(["col", "bcast"]) != b.source_hash("col")
 
 
+def test_an_unknown_kernel_is_named():
+    from paper_2004_09362_amd import build as b
+
+    for name in ("gamm_kernel<P=8>", "", "fused_bo_kernel<P=127>+braodcast", "layer"):
+        with pytest.raises(ValueError, match="unknown kernel"):
+            b.kernel_families(name)
+
+
 def test_cpu_baseline_runs_the_oracle_on_a_sample():
     import torch
 
