@@ -449,7 +449,8 @@ const char* ar_last_error(void);
  * operands on 16-byte boundaries, with an ld of whole 16 bytes, take
  * asynchronous loads.  Rows, columns and inner lengths go from 0 to 2^30 (a
  * matrix without elements may have NULL data; an inner length of 0 is a sum
- * of nothing).  Products are summed in 32 bits, everything up to the store is
+ * of nothing); a result of 2^24 tiles of 128 x 128 or more is
+ * AR_ERR_UNSUPPORTED.  Products are summed in 32 bits, everything up to the store is
  * computed in 32 bits, and a result is rounded once (to nearest, ties to
  * even) to its matrix' type.  Results do not depend on timing: no sum's order
  * does.  NaN and infinities go through as the formulas say. */

@@ -251,18 +251,18 @@ Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Opera
   // boundaries the registers' kernel (4096 x 4096: 27 at M = 16, 63 at 64)
   // leaves large ones to the tiles (20 and 22; 2047 x 1023: 6.5 against 15).
   const int64_t row_tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-  if (rows && p.aligned && (M <= 16 ? N >= 8192 || K * eb > 16384 : K * eb > 2048)) {
+  if (rows && p.aligned && N <= ar::kStreamMaxCols && (M <= 16 ? N >= 8192 || K * eb > 16384 : K * eb > 2048)) {
     p.kind = kStream;
     set_parts(p, ar::kTile128, std::max<int64_t>(1, std::min(kCus / ceil_div(N, 64), p.steps / 8)));
     return p;
   }
-  if (rows && (p.aligned || N * K * (1 + row_tiles) <= 20000000)) {
+  if (rows && N <= ar::kFewMaxCols && (p.aligned || N * K * (1 + row_tiles) <= 20000000)) {
     p.kind = kFew;
     set_parts(p, ar::kTile128, std::max<int64_t>(1, std::min<int64_t>({kCus / ceil_div(N, 16), p.steps / 64, 64})));
     return p;
   }
   const int64_t small = ceil_div(M, 128) * ceil_div(N, 128), large = ceil_div(M, 256) * ceil_div(N, 256);
-  if (small >= (int64_t(1) << 31)) refuse(AR_ERR_UNSUPPORTED, "the product would need 2^31 or more tiles");
+  if (small >= ar::kMaxTiles) refuse(AR_ERR_UNSUPPORTED, "the product would need 2^24 or more tiles of 128 x 128");
   const bool floats = type == AR_FLOAT32;
   int32_t shape = ar::kTile128;
   int64_t splits = 1;
@@ -595,7 +595,7 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
     if (db && N > 0) {
       s.sums = sums;
       s.db = db->data;
-      s.N = N;
+      s.N = s.ld = N;
       s.chunks = p.chunks;
       s.elem = elem_of(db->dtype);
       s.accumulate = accumulate != 0;

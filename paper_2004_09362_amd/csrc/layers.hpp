@@ -53,6 +53,8 @@ enum GemmShape : int32_t { kTile256 = 0, kTile128 = 1 };
 // and the bytes of inner length it takes at a time.
 constexpr int32_t kTileKBytes = 128;
 constexpr int32_t tile_rows(int32_t shape) { return shape == kTile256 ? 256 : 128; }
+// Tiles of a product are below this: 256 threads each, fewer than 2^32 in a launch.
+constexpr int64_t kMaxTiles = int64_t(1) << 24;
 
 // The largest distance of two rows in bytes at which a tile's offsets fit 32 bits.
 constexpr int64_t kMaxTileLd = int64_t(1) << 23;
@@ -88,15 +90,17 @@ int launch_gemm_pair_bf16(const GemmArgs& x, const GemmArgs& w, bool aligned, in
 
 // Products of few rows (both operands k-major): gemm_few.hip.
 constexpr int32_t kFewMaxRows = 64;
+// The widest w of each (a launch has fewer than 2^32 threads: 1024 for 64 columns, and 256).
+constexpr int64_t kFewMaxCols = (int64_t(1) << 28) - 64, kStreamMaxCols = (int64_t(1) << 30) - 64;
 int launch_gemm_few(const GemmArgs& g, int32_t elem, void* stream);
 // the same for operands that can be loaded asynchronously
 int launch_gemm_stream(const GemmArgs& g, int32_t elem, void* stream);
 
-// db[n] = (accumulate ? db[n] : 0) + sum over chunks of sums[chunk][n]
+// db[n] = (accumulate ? db[n] : 0) + sum over chunks of sums[chunk * ld + n]
 struct SumsCall {
   const float* sums;  // NULL: none
   void* db;
-  int64_t N;
+  int64_t N, ld;
   int32_t chunks, elem, accumulate;
 };
 

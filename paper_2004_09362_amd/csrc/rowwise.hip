@@ -126,7 +126,7 @@ __device__ __forceinline__ void column_sums(const SumsCall& c, uint32_t block, f
   float s = 0.0f;
   if (n < c.N) {
 #pragma unroll 8
-    for (int32_t k = rt; k < c.chunks; k += 16) s += c.sums[int64_t(k) * c.N + n];
+    for (int32_t k = rt; k < c.chunks; k += 16) s += c.sums[int64_t(k) * c.ld + n];
   }
   part[rt][ct] = s;
   __syncthreads();
@@ -241,19 +241,33 @@ int launch_join(const GemmArgs& g, const GemmArgs& h, const SumsCall& c, int32_t
   const GemmArgs* const both[2] = {&g, &h};
   for (int i = 0; i < 2; ++i) {
     const int64_t groups = (int64_t(both[i]->e.N) + 7) / 8, threads = both[i]->splits > 1 ? groups * both[i]->e.M : 0;
-    if (threads > (int64_t(1) << 31)) return int(hipErrorInvalidValue);  // products this large are not split
+    if (threads > (int64_t(1) << 30)) return int(hipErrorInvalidValue);  // products this large are not split
     div[i] = make_fastdiv(uint32_t(groups > 0 ? groups : 1));
     blocks[i] = uint32_t((threads + kThreads - 1) / kThreads);
   }
-  const uint32_t all = blocks[0] + blocks[1] + (c.sums ? uint32_t((c.N + 15) / 16) : 0);
-  if (all == 0) return int(hipSuccess);
-  switch (elem) {
-    case kF32: gemm_join_kernel<float><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
-    case kF16: gemm_join_kernel<f16><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
-    case kBF16: gemm_join_kernel<bf16><<<dim3(all), dim3(kThreads), 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], c); break;
-    default: return int(hipErrorInvalidValue);
+  // a launch takes so many columns that it has fewer than 2^32 threads
+  constexpr int64_t kMost = int64_t(1) << 26;
+  const int64_t size = c.elem == kF32 ? 4 : 2;
+  SumsCall s = c;
+  for (int64_t n0 = 0; n0 == 0 || n0 < c.N; n0 += kMost, blocks[0] = blocks[1] = 0) {
+    if (c.sums) {
+      s.sums = c.sums + n0;
+      s.db = static_cast<char*>(c.db) + n0 * size;
+      s.N = c.N - n0 < kMost ? c.N - n0 : kMost;
+    }
+    const uint32_t all = blocks[0] + blocks[1] + (c.sums ? uint32_t((s.N + 15) / 16) : 0);
+    if (all == 0) return int(hipSuccess);
+    const dim3 grid(all), block(kThreads);
+    switch (elem) {
+      case kF32: gemm_join_kernel<float><<<grid, block, 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], s); break;
+      case kF16: gemm_join_kernel<f16><<<grid, block, 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], s); break;
+      case kBF16: gemm_join_kernel<bf16><<<grid, block, 0, st>>>(g, h, div[0], div[1], blocks[0], blocks[1], s); break;
+      default: return int(hipErrorInvalidValue);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return int(e);
   }
-  return int(hipGetLastError());
+  return int(hipSuccess);
 }
 
 }  // namespace ar

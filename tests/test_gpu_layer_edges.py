@@ -156,3 +156,33 @@ def test_gelu_of_16_bits_is_good_to_its_value(dtype):
     assert bool(((y - want).abs() <= (ref.U[dtype] * (1 + 7e-5) + 7e-5) * want.abs() + step).all())
     y = ar.ar_linear_forward(z[:, None], one, activation="gelu", out_dtype=torch.float32)[:, 0].double()
     assert bool(((y - want).abs() <= 7e-5 * want.abs()).all())
+
+
+def test_the_widest_matrices():
+    """Column counts at which a launch with a thread for each piece of a row would pass 2^32 threads: the bias' gradient, the
+    two kernels of few rows and, beyond their widths, tiles."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 30 GB")
+    n = (1 << 28) + 21
+    dy = torch.empty(1, n, dtype=torch.bfloat16, device=DEV).normal_()
+    one = torch.ones(1, 1, dtype=torch.bfloat16, device=DEV)
+    w = torch.empty(n, 1, dtype=torch.bfloat16, device=DEV)
+    print("[gpu] db", n, flush=True)
+    _, _, db = ar.ar_linear_backward(dy, one, w, dx=False, dw=False)
+    assert torch.equal(db, dy[0])
+    got = torch.ones(n, dtype=torch.float32, device=DEV)
+    ar.ar_linear_backward(dy, one, w, dx=False, dw=False, db=got, accumulate=True)
+    assert torch.equal(got[:10000], 1 + dy[0, :10000].float()) and torch.equal(got[-10000:], 1 + dy[0, -10000:].float())
+    del dy, w, db, got
+    torch.cuda.empty_cache()
+    for M, N in ((17, (1 << 28) - 64), (17, (1 << 28) + 40), (2, (1 << 30) - 64), (2, 1 << 30)):
+        print("[gpu] forward", M, N, flush=True)
+        w = torch.empty(N, 8, dtype=torch.bfloat16, device=DEV).normal_()
+        x = torch.empty(M, 8, dtype=torch.bfloat16, device=DEV).normal_()
+        y = ar.ar_linear_forward(x, w)
+        at = torch.cat([torch.arange(200), torch.randint(0, N, (2000,), generator=torch.Generator().manual_seed(1)),
+                        torch.arange(N - 200, N)]).to(DEV)
+        want = ref.forward(x, w[at])
+        ref.close(y[:, at], want[0], want[2], "y")
+        del w, y
+        torch.cuda.empty_cache()

@@ -104,6 +104,16 @@ def test_forward_workspace():
     assert ask(big, big, 8, mat(A, 8), mat(A, 8), ctypes.byref(need)) == UNSUPPORTED and "tiles" in ar.ar_last_error_message()
 
 
+def test_products_of_too_many_tiles_are_refused():
+    """A launch of 256 threads for each tile of 128 x 128 holds fewer than 2^24 of them."""
+    need = ctypes.c_int64()
+    ask = lambda M, N: ar.lib.ar_linear_forward_workspace(M, N, 8, mat(A, 8), mat(A, 8), ctypes.byref(need))  # noqa: E731
+    assert ask(1 << 19, 1 << 19) == UNSUPPORTED and "tiles" in ar.ar_last_error_message()
+    assert ask((1 << 19) - 127, 1 << 19) == UNSUPPORTED
+    assert ask((1 << 19) - 128, 1 << 19) == ar.AR_OK
+    assert ask(1 << 30, 128) == ar.AR_OK and ask(1, 1 << 30) == ar.AR_OK and ask(64, 1 << 30) == ar.AR_OK
+
+
 def backward(M=4, N=6, K=8, dy=None, x=None, w=None, z=None, act=0, d=None, dx=None, dw=None, db=None, acc=0, ws=None, n=0):
     dy, x, w = dy or mat(A, 6), x or mat(A + 0x100000, 8), w or mat(A + 0x200000, 8)
     return ar.lib.ar_linear_backward(M, N, K, dy, x, w, z, act, d, dx, dw, db, acc, ws, n, None)
