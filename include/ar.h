@@ -450,10 +450,10 @@ const char* ar_last_error(void);
  * asynchronous loads.  Rows, columns and inner lengths go from 0 to 2^30 (a
  * matrix without elements may have NULL data; an inner length of 0 is a sum
  * of nothing); a result of 2^24 tiles of 128 x 128 or more is
- * AR_ERR_UNSUPPORTED.  Products are summed in 32 bits, everything up to the store is
- * computed in 32 bits, and a result is rounded once (to nearest, ties to
- * even) to its matrix' type.  Results do not depend on timing: no sum's order
- * does.  NaN and infinities go through as the formulas say. */
+ * AR_ERR_UNSUPPORTED.  Products are summed in 32 bits, everything up to the
+ * store is computed in 32 bits, and a result is rounded once (to nearest, ties
+ * to even) to its matrix' type.  Results do not depend on timing: no sum's
+ * order does.  NaN and infinities go through as the formulas say. */
 typedef struct {
   void* data;
   int64_t ld;     /* elements from one row to the next; of a vector, unused */
@@ -494,9 +494,10 @@ typedef struct {
  *
  * workspace: device memory of at least as many bytes as
  * ar_linear_forward_workspace says for the same arguments (often 0, where it
- * may be NULL), on a 16-byte boundary; it is free again when the call's work
- * is done.  Errors: AR_ERR_INVALID_ARG (sizes, ld, pointers, p, workspace),
- * AR_ERR_UNSUPPORTED (types), AR_ERR_ALIAS, AR_ERR_NO_DEVICE, AR_ERR_HIP. */
+ * may be NULL), on a 16-byte boundary, apart from the matrices (AR_ERR_ALIAS);
+ * it is free again when the call's work is done.  Errors: AR_ERR_INVALID_ARG
+ * (sizes, ld, pointers, p, workspace), AR_ERR_UNSUPPORTED (types), AR_ERR_ALIAS,
+ * AR_ERR_NO_DEVICE, AR_ERR_HIP. */
 ar_status ar_linear_forward(int64_t M, int64_t N, int64_t K, const ar_matrix* x, const ar_matrix* w,
                             const ar_matrix* bias, const ar_matrix* residual, ar_activation act,
                             const ar_dropout* drop, const ar_matrix* y, const ar_matrix* preact, void* workspace,

@@ -162,10 +162,16 @@ void check_device() {
   }
 }
 
-void check_workspace(void* w, int64_t have, int64_t need) {
-  if (need == 0) return;
+// The part of the workspace that a call uses.
+Extent check_workspace(void* w, int64_t have, int64_t need) {
+  Extent e;
+  if (need == 0) return e;
   if (!w || have < need) refuse(AR_ERR_INVALID_ARG, "the workspace must hold " + std::to_string(need) + " bytes");
   if (reinterpret_cast<uintptr_t>(w) % 16 != 0) refuse(AR_ERR_INVALID_ARG, "the workspace must lie on a 16-byte boundary");
+  e.at = reinterpret_cast<uintptr_t>(w);
+  e.row = e.pitch = need;
+  e.rows = 1;
+  return e;
 }
 
 // An operand of a product: `rows` of the output along it.
@@ -511,7 +517,10 @@ ar_status ar_linear_forward(int64_t M, int64_t N, int64_t K, const ar_matrix* x,
     if (residual && !same_place(residual, y, M)) check_apart("y", ey, "residual", er);
     const Operand a = rows_of(x, M), b = rows_of(w, N);
     const Product p = plan_product(M, N, K, x->dtype, a, b);
-    check_workspace(workspace, workspace_bytes, part_bytes(p, M));
+    const Extent ews = check_workspace(workspace, workspace_bytes, part_bytes(p, M));
+    const Extent* const all[] = {&ex, &ew, &eb, &er, &ey, &ez};
+    const char* const names[] = {"x", "w", "bias", "residual", "y", "preact"};
+    for (int i = 0; i < 6; ++i) check_apart("the workspace", ews, names[i], *all[i]);
     check_device();
     e.y = y->data;
     e.ldy = y->ld;
@@ -565,7 +574,9 @@ ar_status ar_linear_backward(int64_t M, int64_t N, int64_t K, const ar_matrix* d
       for (int i = 0; i < o; ++i) check_apart(out_names[o], outs[o], out_names[i], outs[i]);
     }
     const Backward p = plan_backward(M, N, K, dy, x, w, act, drop, dx, dw, db);
-    check_workspace(workspace, workspace_bytes, p.total());
+    const Extent ews = check_workspace(workspace, workspace_bytes, p.total());
+    for (int i = 0; i < 4; ++i) check_apart("the workspace", ews, in_names[i], ins[i]);
+    for (int o = 0; o < 3; ++o) check_apart("the workspace", ews, out_names[o], outs[o]);
     const ar_dtype type = dw ? x->dtype : dx ? w->dtype : act != AR_ACT_NONE ? preact->dtype : dy->dtype;
     const bool any = (dx && M > 0 && K > 0) || (dw && N > 0 && K > 0) || (db && N > 0);
     if (!any) return;

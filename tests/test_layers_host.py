@@ -104,6 +104,26 @@ def test_forward_workspace():
     assert ask(big, big, 8, mat(A, 8), mat(A, 8), ctypes.byref(need)) == UNSUPPORTED and "tiles" in ar.ar_last_error_message()
 
 
+def test_a_workspace_within_an_operand_is_refused():
+    """The workspace is written while operands are read and results stored."""
+    M, N, K, need = 100, 64, 8192, ctypes.c_int64()
+    x, w, y = A, A + 0x1000000, A + 0x2000000
+    kw = dict(M=M, N=N, K=K, x=mat(x, K), w=mat(w, K), y=mat(y, N), preact=mat(A + 0x3000000, N), residual=mat(A + 0x4000000, N),
+              bias=mat(A + 0x5000000, 0))
+    assert ar.lib.ar_linear_forward_workspace(M, N, K, kw["x"], kw["w"], ctypes.byref(need)) == ar.AR_OK and need.value > 0
+    for at, name in ((x + 16, "x"), (w - need.value + 16, "w"), (y, "y"), (A + 0x3000000 + M * N * 2 - 16, "preact"),
+                     (A + 0x4000000, "residual"), (A + 0x5000000 - need.value + 16, "bias")):
+        assert forward(ws=at, ws_bytes=need.value, **kw) == ALIAS, name
+        assert "the workspace overlaps " + name in ar.ar_last_error_message()
+    if not torch.cuda.is_available():  # beside them it is taken: what is left to miss is the GPU
+        assert forward(ws=A + 0x6000000, ws_bytes=1 << 40, **kw) == ar.AR_ERR_NO_DEVICE
+    kw = dict(M=500, N=64, K=8, dy=mat(A, 64), x=mat(A + 0x100000, 8), w=mat(A + 0x200000, 8), z=mat(A + 0x300000, 64), act=2,
+              dx=mat(A + 0x400000, 8), dw=mat(A + 0x500000, 8), db=mat(A + 0x600000, 0))
+    for i, name in enumerate(("dy", "x", "w", "preact", "dx", "dw", "db")):
+        assert backward(ws=A + i * 0x100000, n=1 << 40, **kw) == ALIAS, name
+        assert "the workspace overlaps " + name in ar.ar_last_error_message()
+
+
 def test_products_of_too_many_tiles_are_refused():
     """A launch of 256 threads for each tile of 128 x 128 holds fewer than 2^24 of them."""
     need = ctypes.c_int64()
