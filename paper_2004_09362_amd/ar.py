@@ -540,6 +540,10 @@ class Plan:
 
 
 # ---- layer operators (include/ar.h, "Layer operators") ----
+#
+# torch records no gradient of these calls.  The forward ones refuse a tensor
+# that requires one while torch records (call them under torch.no_grad(), as in
+# the forward of a torch.autograd.Function whose backward is the _backward call).
 
 _ACTIVATIONS = {"none": AR_ACT_NONE, "relu": AR_ACT_RELU, "gelu": AR_ACT_GELU, "gelu_tanh": AR_ACT_GELU_TANH,
                 "silu": AR_ACT_SILU}
@@ -590,7 +594,8 @@ def ar_linear_forward(x, w, bias=None, residual=None, *, activation: str = "none
     sums.  With ``preact`` (a tensor, or True for a new one) the
     pre-activation x w^T + bias is kept for :func:`ar_linear_backward` and
     (y, preact) is returned.  Rows may have any distance; their elements are
-    consecutive."""
+    consecutive.  torch records no gradient of the call: while it records, a
+    tensor that requires one is refused."""
     return _layer_call("ar_linear_forward", _bind.linear_forward,
                        (x, w, bias, residual, out, preact, _activation_code(activation),
                         _float_code(out_dtype, "out_dtype"), dropout), stream)
@@ -615,11 +620,11 @@ def ar_dropout_forward(x, dropout: Dropout, residual=None, *, out=None, out_dtyp
     """y = residual + drop(x), y of ``out_dtype`` (default x's type; the
     residual has y's) or written to ``out``, which may be x or residual."""
     return _layer_call("ar_dropout_forward", _bind.dropout,
-                       (x, residual, out, _float_code(out_dtype, "out_dtype"), dropout), stream)
+                       (x, residual, out, _float_code(out_dtype, "out_dtype"), dropout, False), stream)
 
 
 def ar_dropout_backward(dy, dropout: Dropout, *, out=None, out_dtype=None, stream=None):
     """dx = drop(dy), the gradient of :func:`ar_dropout_forward` with the
     same dropout (dy is the residual's gradient as well)."""
     return _layer_call("ar_dropout_backward", _bind.dropout,
-                       (dy, None, out, _float_code(out_dtype, "out_dtype"), dropout), stream)
+                       (dy, None, out, _float_code(out_dtype, "out_dtype"), dropout, True), stream)

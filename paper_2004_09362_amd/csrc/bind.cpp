@@ -8,6 +8,7 @@
 // call to the next).  Whatever fails one, or is no plain torch tensor in a
 // list or tuple -- raw addresses, subclasses, other sequences -- is answered
 // with None, and the caller takes the Python path, which names the fault.
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -161,6 +162,21 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   return THPVariable_Unpack(o);
 }
 
+// The same of a forward call, which torch would not know to have happened: a
+// gradient that it is to record is not lost silently.
+const at::Tensor& unrecorded(PyObject* o, const char* name) {
+  const at::Tensor& t = tensor(o, name);
+  if (at::GradMode::is_enabled() && t.requires_grad())
+    throw Fault{std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() (the "
+                "_backward calls compute the gradient)"};
+  return t;
+}
+
+// A given tensor was written: torch's check of what a backward pass still needs.
+void written(PyObject* given, const at::Tensor& t) {
+  if (THPVariable_Check(given) && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A tensor of `dims` dimensions (2, or 1: a vector) with consecutive elements
 // in a row, on the call's device; rows and cols < 0 are not checked.
 ar_matrix view(const at::Tensor& t, const char* name, int dims, int64_t rows, int64_t cols, const Place& at_) {
@@ -234,23 +250,23 @@ PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return answer([&]() -> PyObject* {
     if (nargs != 11 || !g_linear_forward) throw Fault{"linear_forward takes 11 arguments"};
     const Place at_{number(args[9], "device"), number(args[10], "stream")};
-    const at::Tensor& x = tensor(args[0], "x");
-    const at::Tensor& w = tensor(args[1], "w");
+    const at::Tensor& x = unrecorded(args[0], "x");
+    const at::Tensor& w = unrecorded(args[1], "w");
     const ar_matrix mx = view(x, "x", 2, -1, -1, at_);
     const int64_t M = x.size(0), K = x.size(1);
     const ar_matrix mw = view(w, "w", 2, -1, K, at_);
     const int64_t N = w.size(0);
     ar_matrix mb, mr, mz;
-    if (args[2] != Py_None) mb = view(tensor(args[2], "bias"), "bias", 1, 1, N, at_);
-    if (args[3] != Py_None) mr = view(tensor(args[3], "residual"), "residual", 2, M, N, at_);
+    if (args[2] != Py_None) mb = view(unrecorded(args[2], "bias"), "bias", 1, 1, N, at_);
+    if (args[3] != Py_None) mr = view(unrecorded(args[3], "residual"), "residual", 2, M, N, at_);
     const int64_t act = number(args[6], "activation"), code = number(args[7], "out dtype");
     ar_dropout d;
     const ar_dropout* drop = dropout_of(args[8], &d);
     at::Tensor y, z;
-    if (args[4] != Py_None) y = tensor(args[4], "out");
+    if (args[4] != Py_None) y = unrecorded(args[4], "out");
     else y = at::empty({M, N}, x.options().dtype(scalar_of(code, x.scalar_type())));
     if (args[5] == Py_True) z = at::empty({M, N}, x.options());
-    else if (args[5] != Py_None && args[5] != Py_False) z = tensor(args[5], "preact");
+    else if (args[5] != Py_None && args[5] != Py_False) z = unrecorded(args[5], "preact");
     const ar_matrix my = view(y, "out", 2, M, N, at_);
     if (z.defined()) mz = view(z, "preact", 2, M, N, at_);
     int64_t bytes = 0;
@@ -263,6 +279,8 @@ PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       Py_END_ALLOW_THREADS
     }
     if (st != AR_OK) return PyLong_FromLong(long(st));
+    written(args[4], y);
+    if (z.defined()) written(args[5], z);
     PyObject* py = THPVariable_Wrap(y);
     if (!z.defined() || !py) return py;
     PyObject* pz = THPVariable_Wrap(z);
@@ -330,8 +348,12 @@ PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const at::Tensor* const parts[] = {&dx, &dw, &db};
     for (int i = 0; got && i < 3; ++i) {
       PyObject* o = Py_None;
-      if (parts[i]->defined()) o = THPVariable_Wrap(*parts[i]);
-      else Py_INCREF(o);
+      if (parts[i]->defined()) {
+        written(args[6 + i], *parts[i]);
+        o = THPVariable_Wrap(*parts[i]);
+      } else {
+        Py_INCREF(o);
+      }
       if (!o) {
         Py_DECREF(got);
         return nullptr;
@@ -342,19 +364,20 @@ PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
-// dropout(x, residual, out, out dtype, dropout, device, stream) -> y, a status, or a text.
+// dropout(x, residual, out, out dtype, dropout, backward, device, stream) -> y, a status, or a text.
 PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   return answer([&]() -> PyObject* {
-    if (nargs != 7 || !g_dropout_forward) throw Fault{"dropout takes 7 arguments"};
-    const Place at_{number(args[5], "device"), number(args[6], "stream")};
-    const at::Tensor& x = tensor(args[0], "x");
+    if (nargs != 8 || !g_dropout_forward) throw Fault{"dropout takes 8 arguments"};
+    const Place at_{number(args[6], "device"), number(args[7], "stream")};
+    auto* const operand = args[5] == Py_True ? tensor : unrecorded;
+    const at::Tensor& x = operand(args[0], "x");
     const ar_matrix mx = view(x, "x", 2, -1, -1, at_);
     const int64_t rows = x.size(0), cols = x.size(1);
     ar_matrix mr;
-    if (args[1] != Py_None) mr = view(tensor(args[1], "residual"), "residual", 2, rows, cols, at_);
+    if (args[1] != Py_None) mr = view(operand(args[1], "residual"), "residual", 2, rows, cols, at_);
     const int64_t code = number(args[3], "out dtype");
     at::Tensor y;
-    if (args[2] != Py_None) y = tensor(args[2], "out");
+    if (args[2] != Py_None) y = operand(args[2], "out");
     else y = at::empty({rows, cols}, x.options().dtype(scalar_of(code, x.scalar_type())));
     const ar_matrix my = view(y, "out", 2, rows, cols, at_);
     ar_dropout d;
@@ -363,7 +386,9 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     Py_BEGIN_ALLOW_THREADS
     st = g_dropout_forward(rows, cols, &mx, args[1] != Py_None ? &mr : nullptr, drop, &my, at_.hip());
     Py_END_ALLOW_THREADS
-    return st == AR_OK ? THPVariable_Wrap(y) : PyLong_FromLong(long(st));
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    written(args[2], y);
+    return THPVariable_Wrap(y);
   });
 }
 

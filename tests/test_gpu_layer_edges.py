@@ -186,3 +186,52 @@ def test_the_widest_matrices():
         ref.close(y[:, at], want[0], want[2], "y")
         del w, y
         torch.cuda.empty_cache()
+
+
+def test_tensors_that_torch_records():
+    """A forward call on a tensor that requires a gradient is refused while torch records and runs where it does not; a custom
+    function of the two calls differentiates; what is written in place counts as written."""
+    g = torch.Generator().manual_seed(30)
+    x, w, b, r = (matrix(g, *s, torch.float32) for s in ((40, 24), (16, 24), (1, 16), (40, 16)))
+    b = b[0]
+    want = ar.ar_linear_forward(x, w, b, r)
+    for i, name in enumerate(("x", "w", "bias", "residual")):
+        args = [t.clone().requires_grad_(j == i) for j, t in enumerate((x, w, b, r))]
+        with pytest.raises(ar.ArError, match=name + " requires a gradient"):
+            ar.ar_linear_forward(*args)
+        with torch.no_grad():
+            assert torch.equal(ar.ar_linear_forward(*args), want)
+    with pytest.raises(ar.ArError, match="out requires a gradient"):
+        ar.ar_linear_forward(x, w, b, r, out=torch.zeros(40, 16, device=DEV, requires_grad=True))
+
+    class Linear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, b):
+            y, z = ar.ar_linear_forward(x, w, b, activation="silu", preact=True)
+            ctx.save_for_backward(x, w, z)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w, z = ctx.saved_tensors
+            return ar.ar_linear_backward(dy, x, w, preact=z, activation="silu")
+
+    leaves = [t.clone().requires_grad_(True) for t in (x, w, b)]
+    c = matrix(g, 40, 16, torch.float32)
+    (Linear.apply(*leaves) * c).sum().backward()
+    with torch.no_grad():
+        z = ar.ar_linear_forward(x, w, b)
+        grads = ar.ar_linear_backward(c, *leaves[:2], preact=z, activation="silu")
+    for leaf, grad in zip(leaves, grads):
+        assert torch.equal(leaf.grad, grad)
+
+    y, z, dx, dw, db, v = (torch.zeros(s, device=DEV) for s in ((40, 16), (40, 16), (40, 24), (16, 24), (16,), (40, 16)))
+    before = [t._version for t in (y, z, dx, dw, db, v)]
+    ar.ar_linear_forward(x, w, b, out=y, preact=z)
+    ar.ar_linear_backward(c, x, w, dx=dx, dw=dw, db=db)
+    ar.ar_dropout_forward(c, ar.Dropout(0.5, 1), out=v)
+    assert [t._version for t in (y, z, dx, dw, db, v)] == [n + 1 for n in before]
+    with torch.inference_mode():
+        t = torch.zeros(40, 16, device=DEV)
+    ar.ar_linear_forward(x, w, b, r, out=t)
+    assert torch.equal(t, want)

@@ -204,6 +204,25 @@ def test_binding_refusals_without_a_gpu():
             call()
 
 
+def test_tensors_that_require_a_gradient():
+    """The forward calls refuse them while torch records, and go on to the next check where it does not; the gradients' calls
+    take them."""
+    x, w, b, r = (torch.zeros(s, requires_grad=True) for s in ((4, 8), (6, 8), (6,), (4, 6)))
+    d = ar.Dropout(0.5, 1)
+    plain = x.detach()
+    for call, name in ((lambda: ar.ar_linear_forward(x, w), "x"), (lambda: ar.ar_linear_forward(plain, w), "w"),
+                       (lambda: ar.ar_dropout_forward(x, d), "x")):
+        with pytest.raises(ar.ArError, match=name + " requires a gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ar.ArError, match="not on a GPU"):
+            call()
+        with torch.inference_mode(), pytest.raises(ar.ArError, match="not on a GPU"):
+            call()
+    for call in (lambda: ar.ar_linear_backward(r, x, w), lambda: ar.ar_dropout_backward(x, d)):
+        with pytest.raises(ar.ArError, match="not on a GPU"):
+            call()
+
+
 def test_plans_take_rank_buffer_types_only():
     h = ctypes.c_void_p()
     for code in (F16, BF16):
