@@ -182,6 +182,7 @@ void written(PyObject* given, const at::Tensor& t) {
 ar_matrix view(const at::Tensor& t, const char* name, int dims, int64_t rows, int64_t cols, const Place& at_) {
   const std::string n(name);
   if (t.layout() != at::kStrided) throw Fault{n + " must be a dense tensor"};
+  if (t.is_neg()) throw Fault{n + " is a negated view, whose memory holds other values"};
   if (!t.is_cuda()) throw Fault{n + " is not on a GPU"};
   if (t.get_device() != at_.device)
     throw Fault{n + " is on cuda:" + std::to_string(t.get_device()) + ", the current device is cuda:" +

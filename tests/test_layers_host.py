@@ -223,6 +223,16 @@ def test_tensors_that_require_a_gradient():
             call()
 
 
+def test_negated_views_are_refused():
+    """The imaginary part of a conjugate is a view of the number's memory, to be read with its sign turned."""
+    t = torch.imag(torch.ones(4, 1, dtype=torch.complex64).conj())
+    assert t.is_neg() and t.dtype == torch.float32
+    for call in (lambda: ar.ar_linear_forward(t, torch.zeros(6, 1)), lambda: ar.ar_dropout_forward(t, ar.Dropout(0.5, 1)),
+                 lambda: ar.ar_linear_backward(t, torch.zeros(4, 2), torch.zeros(1, 2))):
+        with pytest.raises(ar.ArError, match="negated view"):
+            call()
+
+
 def test_plans_take_rank_buffer_types_only():
     h = ctypes.c_void_p()
     for code in (F16, BF16):
