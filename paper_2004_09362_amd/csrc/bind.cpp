@@ -10,6 +10,7 @@
 // with None, and the caller takes the Python path, which names the fault.
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -239,8 +240,8 @@ PyObject* answer(F&& body) {
     return PyUnicode_FromString(f.text.c_str());
   } catch (const std::bad_alloc&) {
     return PyErr_NoMemory();
-  } catch (const std::exception& e) {  // torch's own, of an allocation
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (...) {  // torch's own, of an allocation: as the error that torch raises for it
+    torch::translate_exception_to_python(std::current_exception());
     return nullptr;
   }
 }

@@ -235,3 +235,11 @@ def test_tensors_that_torch_records():
         t = torch.zeros(40, 16, device=DEV)
     ar.ar_linear_forward(x, w, b, r, out=t)
     assert torch.equal(t, want)
+
+
+def test_no_memory_for_a_result():
+    """torch's own error, which programs catch to go on with less."""
+    x = torch.ones(1 << 21, 1, dtype=torch.bfloat16, device=DEV)  # 8 TB of results
+    with pytest.raises(torch.OutOfMemoryError):
+        ar.ar_linear_forward(x, x)
+    assert ar.ar_linear_forward(x[:2], x[:3]).shape == (2, 3)
