@@ -445,7 +445,8 @@ const char* ar_last_error(void);
  *
  * Matrices lie in rows: element (i, j) of a matrix is at data + i * ld + j (in
  * elements, ld at least the columns), in 32-bit, 16-bit (IEEE) or bfloat
- * floats.  Any address and ld that are multiples of the element are taken;
+ * floats.  What lies between rows may be read, is not used, and is not written.
+ * Any address and ld that are multiples of the element are taken;
  * operands on 16-byte boundaries, with an ld of whole 16 bytes, take
  * asynchronous loads.  Rows, columns and inner lengths go from 0 to 2^30 (a
  * matrix without elements may have NULL data; an inner length of 0 is a sum

@@ -11,13 +11,14 @@
 // Bound by the matrix units on large products: a 256 x 256 tile (a wave: 128 x
 // 128, whose 256 sums a lane fill half of the register file) reads 64 KB of LDS'
 // 128 bytes a cycle for 1024 cycles of products each step.  Measured, bf16:
-// 8192 x 16384 x 4096 785 us (1400 TFLOP/s), its input gradient 755 us, 4096^3
-// 93 us; a step of one tile 0.96 us, 0.43 us of it the products' own at full
+// 8192 x 16384 x 4096 785 us (1400 TFLOP/s), its input gradient 751 us, 4096^3
+// 94 us; a step of one tile 0.96 us, 0.43 us of it the products' own at full
 // clock, and up to 1.4 us where the chip lowers its clock for its power.
 // Around a tile's steps lie 4000 cycles until its first loads are there, and
-// the epilogue, which nothing hides: one tile takes a compute unit's LDS.  Smaller products take 128 x 128 tiles, two to a unit, which hide
-// each other's but read LDS twice as much for each product.  fp32: 2048 x 4096
-// x 1024 124 us (138 TFLOP/s; the unit's rate is 157).
+// the epilogue, which nothing hides: one tile takes a compute unit's LDS.
+// Smaller products take 128 x 128 tiles, two to a unit, which hide each other's
+// but read LDS twice as much for each product.  fp32: 2048 x 4096 x 1024 124 us
+// (138 TFLOP/s; the unit's rate is 157).
 //
 // Inner lengths of 128 bytes at a time (a tile: 64 halves or 32 floats) are
 // staged in LDS, every operand in the order that it has in memory:
@@ -29,8 +30,8 @@
 //             4-byte reads.
 // Both orders give lane group g = lane / 16 the same inner indices (8 g to
 // 8 g + 7, or 4 g to 4 g + 3, of a 64-byte slice), so they can be mixed.
-// Chunks lie at a position XORed with a function of their row (swz_a, swz_b
-// below), which spreads a fragment read's lanes over all banks.
+// Chunks lie at a position XORed with a function of their row (Operand::swz),
+// which spreads a fragment read's lanes over all banks.
 //
 // Columns of the wave are dealt to instructions so that tiles 2j and 2j + 1
 // together give a lane 8 consecutive ones: row 4 p + r of tile t is column
@@ -322,7 +323,8 @@ struct Fragments {
   static constexpr int kRowBytes = KMAJOR ? kTileKBytes : R * int(sizeof(T));
   uint32_t off[4];
 
-  // w0: the wave's first row in the tile (a multiple of 64).
+  // w0: the wave's first row in the tile, a multiple of 16 where the operand is
+  // k-major and of 64 otherwise (its chunks' places repeat after 64 rows).
   __device__ __forceinline__ void init(int w0, int lane) {
     const int i = lane & 15, g = lane >> 4;
     using Op = Operand<T, KMAJOR, FIRST, R, R>;
@@ -511,8 +513,8 @@ __device__ __forceinline__ void direct(const GemmArgs& g, f32x4v (&acc)[MT][NT],
 // instructions' tiles, whose sums a chain of branches fetches from their
 // registers, so that the code of the stages is there once (for every sum, it
 // would not fit the instruction cache).  What the stages add to 8192 x 4096 x
-// 4096 bf16, 189 us: relu 3, the tanh form of gelu 6, with a bias and z kept 15,
-// dropout, bias and residual 22 (through LDS 20, 19, 30 and 37).
+// 4096 bf16, 182 us: relu or silu 8, the tanh form of gelu 10 and with a bias and
+// z kept 16, gelu 19 and 23, dropout, bias and residual 27.
 template <typename T, int MT, int NT>
 __device__ __forceinline__ void direct_full(const GemmArgs& g, const f32x4v (&acc)[MT][NT], int32_t m, int32_t n) {
   constexpr int kPairs = NT / 2;
@@ -605,6 +607,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
   OpB b;
   a.init(static_cast<const T*>(g.a), g.lda, m0, k0, g.e.M, g.K, tid);
   b.init(static_cast<const T*>(g.b), g.ldb, n0, k0, g.e.N, g.K, tid);
+  static_assert(MT % 4 == 0 && NT % 4 == 0, "the waves' first rows are multiples of 64");
   Fragments<T, AK, false, TM> ra;
   Fragments<T, BK, true, TN> rb;
   ra.init(wm * MT * 16, lane);
@@ -809,7 +812,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
 
   // A whole tile's sums leave from the lanes that hold them: of tiles 2j, 2j + 1 a lane has 8 columns
   // (32 j + 8 p on) of a row, and four lanes have 64 bytes of halves together,
-  // whose line the next columns fill.  16384 x 1024 x 1024 bf16 32 us, through LDS
+  // whose line the next columns fill.  16384 x 1024 x 1024 bf16 30 us, through LDS
   // 40 (the passes below wait for each step by themselves).
   const bool whole = m0 + TM <= g.e.M && n0 + TN <= g.e.N;
   if (STAGES != kFull && whole) {

@@ -240,11 +240,20 @@ namespace {
 
 template <typename T, int MT>
 int launch_few(const GemmArgs& g, hipStream_t st) {
+  // One, two or four tiles of 16 columns a workgroup, so that two rounds of
+  // workgroups become one.  w of 4096 / 6144 / 8192 / 12288 / 16384 / 32768 rows of 1024
+  // halves, M = 24, us in a graph: one 5.6 / 9.7 / 9.9 / 14.2 / 18.5 / 35.1, two 7.6 / 7.8 /
+  // 7.9 / 14.0 / 14.9 / 27.7, four 12.1 / 12.5 / 12.3 / 12.6 / 13.4 / 24.9; of 512 floats 5.9 /
+  // 10.1 / 10.5 / 15.1 / 19.2 / 35.9, 8.0 / 8.2 / 8.5 / 15.0 / 15.6 / 28.9 and 12.7 / 12.9 / 13.1 /
+  // 13.2 / 13.4 / 25.3; at 4096 inner indices (6144 columns) one and two are even.
   const int32_t tiles = (g.e.N + 15) / 16, nw = tiles >= 4 * 256 ? 4 : tiles >= 2 * 256 ? 2 : 1;
   const dim3 grid(uint32_t((tiles + nw - 1) / nw), uint32_t(g.splits));
   if constexpr (MT == 1) {
-    // up to 8 KB of a row: eight waves that each ask for all of theirs at once
-    // (4096 x 4096 bf16 8.0 us, sixteen 8.7; at 32 KB 36.8 and 30.7)
+    // up to 8 KB of a row: eight waves that each ask for all of theirs at once.
+    // w of 4096 rows of 2 / 4 / 8 / 12 / 16 KB, M = 1, us in a graph: bf16 4.3 / 6.3 /
+    // 9.1 / 12.4 / 16.7 and with sixteen 4.6 / 6.3 / 9.8 / 12.5 / 17.1; fp32 4.6 / 6.6 /
+    // 10.7 / 13.2 / 17.7 and 4.7 / 6.7 / 10.2 / 12.7 / 17.8; M = 16 within 2%, at 16 KB
+    // 21.7 and 22.8.  At 32 KB of bf16 36.8 and 30.7.
     if (nw == 1 && int64_t(g.K) * int64_t(sizeof(T)) <= 8192) {
       gemm_few_kernel<T, 1, 1, 8><<<grid, dim3(512), 0, st>>>(g);
       return int(hipGetLastError());

@@ -146,7 +146,8 @@ __device__ __forceinline__ float logistic2(float u) {
 
 // exp(-z^2 / 2), and the normal distribution's tail beyond |z|: t P(t) exp(-z^2 / 2)
 // with t = 1 / (1 + c |z|) and polynomials P fitted to erfcx for the least relative
-// error: small where the tail is, unlike 1 + erf.  From 64 on, and for NaN, both are 0.
+// error: small where the tail is, unlike 1 + erf.  x is |z|, 64 at most; from there
+// on, and for NaN, both are 0.
 //   FINE, for operands of 32 bits: degree 8, 7e-8, and the exponent's rounding, which
 //   would grow with z^2 to 1e-5 of the tail, is carried along (lost).  With an exp2
 //   and a reciprocal of one unit in the last place the tail is off by 12 * 2^-24

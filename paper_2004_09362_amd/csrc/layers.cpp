@@ -250,12 +250,23 @@ Product plan_product(int64_t M, int64_t N, int64_t K, ar_dtype type, const Opera
   const bool rows = a.kmajor && b.kmajor && M <= ar::kFewMaxRows;
   // Few rows.  Aligned, both kernels read w at the rate of memory; the one
   // through LDS keeps it up with more rows and longer inner lengths, the other
-  // starts sooner.  w of 4096 x 4096 bf16, M = 1 / 16 / 24 / 64, us: registers
-  // 9.0 / 10.8 / 12.7 / 21, LDS 11.4 / 11.9 / 11.9 / 13.4; of 16384 x 4096 28 /
-  // 34 / 41 / 75 and 28 / 27 / 27 / 29; of 4096 x 16384 29 / 36 / 43 / 78 and
-  // 27 / 27 / 28 / 31; K = 1024 and less 5.5-7 and 5.5-8.  Off the 16-byte
-  // boundaries the registers' kernel (4096 x 4096: 27 at M = 16, 63 at 64)
-  // leaves large ones to the tiles (20 and 22; 2047 x 1023: 6.5 against 15).
+  // starts sooner.  M = 1 / 16 / 24 / 64, us in a graph, w beyond the caches:
+  //   w               registers, bf16     LDS, bf16          registers, fp32  LDS, fp32
+  //   4096 x 4096     8.4/10.5/13.1/23  12.4/12.7/13.0/14.3    17/21/25/46    24/23/23/31
+  //   16384 x 4096     32/38/42/76        30/30/29/31          72/81/96/167   60/61/61/96
+  //   4096 x 16384     30/37/44/79        29/29/30/33          57/70/91/170   63/63/64/100
+  //   8192 x 2048     9.6/10.7/12.6/22  12.3/12.7/12.9/14.2    17/19/25/46    22/23/23/32
+  //   16384 x 1024    8.4/10.4/12.6/21   9.1/9.2/9.5/11.2      17/19/24/45    18/19/19/28
+  //   4096 x 1024     4.3/4.8/5.5/7.7    7.9/8.3/8.5/10.5     6.3/7.1/8.5/14  11/12/12/16
+  //   1024 x 512      3.1/3.6/4.0/5.2    4.2/4.4/4.6/6.2      3.8/4.4/5.3/7.7  8/9/9/12
+  // Where these bounds give time away: 3 to 5 us at 8192 x 2048 with up to 16 rows,
+  // 6 at 4096 x 16384 fp32 with one, 3 to 10 at 16384 x 1024 bf16 and 4 at 4096 x
+  // 1024 fp32 with more than 16.
+  // Off the 16-byte boundaries, bf16, the registers' kernel takes 18.6 / 29 / 36 /
+  // 64 for 4096 x 4095 and 7.6 / 10.5 / 11.7 / 18.7 for 2047 x 1023, tiles 33 / 36 /
+  // 20 / 21 and 14 / 15 / 16 / 17; fp32 at 4096 x 4095 18 / 24 / 29 / 51 and 50 / 49 / 49 /
+  // 48.  The bound sends all four of 4096 x 4095 to the tiles: right for 16 bits
+  // from 17 rows on, 7 to 15 us late with fewer, and 20 to 32 in fp32 below 64.
   const int64_t row_tiles = M <= 16 ? 1 : M <= 32 ? 2 : 4;
   if (rows && p.aligned && N <= ar::kStreamMaxCols && (M <= 16 ? N >= 8192 || K * eb > 16384 : K * eb > 2048)) {
     p.kind = kStream;

@@ -82,7 +82,7 @@ int launch_gemm_f16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligne
 int launch_gemm_bf16(const GemmArgs& g, bool a_kmajor, bool b_kmajor, bool aligned, int32_t shape, void* stream);
 
 // The gradient's products with respect to x (a k-major, b not) and w (neither)
-// in one launch, on tiles of 128 x 128.
+// in one launch, both on tiles of that shape.
 int launch_gemm_pair(const GemmArgs& x, const GemmArgs& w, int32_t elem, bool aligned, int32_t shape, void* stream);
 int launch_gemm_pair_f32(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream);
 int launch_gemm_pair_f16(const GemmArgs& x, const GemmArgs& w, bool aligned, int32_t shape, void* stream);

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropCall c, FastDiv g
 // A workgroup takes 256 columns (32 threads of 8) of one chunk of rows, 8
 // rows at a time, four of these together so that enough loads are in flight;
 // the sums of its 8 row threads meet in LDS in their order.  8192 x 16384 bf16
-// through an activation 144 us (5.6 TB/s).
+// through an activation 146 us (5.5 TB/s).
 template <typename D, typename Z>
 __global__ __launch_bounds__(kThreads) void slope_kernel(SlopeCall c) {
   constexpr int kRows = 4;
