@@ -542,6 +542,38 @@ ar_status ar_dropout_forward(int64_t rows, int64_t cols, const ar_matrix* x, con
 ar_status ar_dropout_backward(int64_t rows, int64_t cols, const ar_matrix* dy, const ar_dropout* drop,
                               const ar_matrix* dx, hipStream_t stream);
 
+/* Layer norm of each row of x [rows, cols], of any of the three types:
+ *   mean = sum_j x_ij / cols, rstd = 1 / sqrt(sum_j (x_ij - mean)^2 / cols + eps)
+ *   y = (x - mean) rstd weight + bias      [rows, cols], of any of the types
+ * weight and bias [cols], of any of the types each (NULL: ones, zeros).  stats
+ * [rows, 2] float32 receives (mean, rstd) of each row for the gradient (NULL:
+ * not kept; cols = 0 has none: AR_ERR_INVALID_ARG).  Sums are in 32 bits, the
+ * variance's about the mean.  y may be x where data, ld and type are the same.
+ * eps: finite, at least 0 (AR_ERR_INVALID_ARG; a row of equal values with
+ * eps = 0 gives NaN, as the formula says). */
+ar_status ar_layer_norm_forward(int64_t rows, int64_t cols, const ar_matrix* x, const ar_matrix* weight,
+                                const ar_matrix* bias, double eps, const ar_matrix* y, const ar_matrix* stats,
+                                hipStream_t stream);
+
+/* The gradient of ar_layer_norm_forward for dy [rows, cols], the gradient of y
+ * (of any of the types), with the same x and weight, and the stats that it kept;
+ * h = (x - mean) rstd, g = dy weight:
+ *   dx = residual + rstd (g - mean_j(g) - h mean_j(g h))   [rows, cols]
+ *   dw = sum_i dy_ij h_ij, db = sum_i dy_ij                [cols]
+ * dx and residual (a gradient that reaches x past the norm; NULL: none) have x's
+ * type, dw and db any of the types each.  dx, dw or db NULL: not computed.  dx
+ * may be dy or residual where data, ld and type are the same.  With
+ * accumulate != 0 dw and db are added to what is there.  Workspace and errors
+ * as of ar_linear_forward. */
+ar_status ar_layer_norm_backward(int64_t rows, int64_t cols, const ar_matrix* dy, const ar_matrix* x,
+                                 const ar_matrix* stats, const ar_matrix* weight, const ar_matrix* residual,
+                                 const ar_matrix* dx, const ar_matrix* dw, const ar_matrix* db, int32_t accumulate,
+                                 void* workspace, int64_t workspace_bytes, hipStream_t stream);
+ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_matrix* dy, const ar_matrix* x,
+                                           const ar_matrix* stats, const ar_matrix* weight, const ar_matrix* residual,
+                                           const ar_matrix* dx, const ar_matrix* dw, const ar_matrix* db,
+                                           int64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

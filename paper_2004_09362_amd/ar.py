@@ -44,6 +44,7 @@ EXPORTS = [
     "ar_execute_noalloc",
     "ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward", "ar_linear_backward_workspace",
     "ar_dropout_forward", "ar_dropout_backward",
+    "ar_layer_norm_forward", "ar_layer_norm_backward", "ar_layer_norm_backward_workspace",
 ]
 
 
@@ -159,8 +160,12 @@ def _load():
                                                ctypes.POINTER(i64)]
     L.ar_dropout_forward.argtypes = [i64, i64, mp, mp, dp, mp, vp]
     L.ar_dropout_backward.argtypes = [i64, i64, mp, dp, mp, vp]
+    L.ar_layer_norm_forward.argtypes = [i64, i64, mp, mp, mp, dbl, mp, mp, vp]
+    L.ar_layer_norm_backward.argtypes = [i64, i64, mp, mp, mp, mp, mp, mp, mp, mp, i32, vp, i64, vp]
+    L.ar_layer_norm_backward_workspace.argtypes = [i64, i64, mp, mp, mp, mp, mp, mp, mp, mp, ctypes.POINTER(i64)]
     for name in ("ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward",
-                 "ar_linear_backward_workspace", "ar_dropout_forward", "ar_dropout_backward"):
+                 "ar_linear_backward_workspace", "ar_dropout_forward", "ar_dropout_backward",
+                 "ar_layer_norm_forward", "ar_layer_norm_backward", "ar_layer_norm_backward_workspace"):
         getattr(L, name).restype = ctypes.c_int
     for name in ("ar_plan_create", "ar_plan_create_ex", "ar_plan_set_path", "ar_execute", "ar_execute_batched", "ar_plan_stats",
                  "ar_plan_num_launches", "ar_plan_launch", "ar_model_time", "ar_model_best_k", "ar_plan_model_time",
@@ -182,7 +187,8 @@ def _load_bind():
     mod.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.ar_execute_batched, lib.ar_execute_noalloc)))
     mod.bind_layers(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.ar_linear_forward, lib.ar_linear_forward_workspace, lib.ar_linear_backward,
-        lib.ar_linear_backward_workspace, lib.ar_dropout_forward)))
+        lib.ar_linear_backward_workspace, lib.ar_dropout_forward, lib.ar_layer_norm_forward,
+        lib.ar_layer_norm_backward, lib.ar_layer_norm_backward_workspace)))
     return mod
 
 
@@ -628,3 +634,34 @@ def ar_dropout_backward(dy, dropout: Dropout, *, out=None, out_dtype=None, strea
     same dropout (dy is the residual's gradient as well)."""
     return _layer_call("ar_dropout_backward", _bind.dropout,
                        (dy, None, out, _float_code(out_dtype, "out_dtype"), dropout, True), stream)
+
+
+def ar_layer_norm_forward(x, weight=None, bias=None, *, eps: float = 1e-5, out=None, out_dtype=None, stats=None,
+                          stream=None):
+    """y = (x - mean) rstd weight + bias over each row of x [rows, cols], with
+    rstd = 1 / sqrt(variance + eps).
+
+    y is ``out`` (which may be x) or a new tensor of ``out_dtype`` (default
+    x's type).  With ``stats`` (a float32 tensor [rows, 2], or True for a new
+    one) each row's (mean, rstd) is kept for :func:`ar_layer_norm_backward`
+    and (y, stats) is returned.  weight and bias [cols] have any of the types.
+    torch records no gradient of the call: while it records, a tensor that
+    requires one is refused."""
+    return _layer_call("ar_layer_norm_forward", _bind.norm_forward,
+                       (x, weight, bias, eps, out, _float_code(out_dtype, "out_dtype"), stats), stream)
+
+
+def ar_layer_norm_backward(dy, x, stats, weight=None, *, residual=None, dx=True, dw=True, db=True,
+                           accumulate: bool = False, dw_dtype=None, stream=None):
+    """The gradient of :func:`ar_layer_norm_forward`: (dx, dw, db) for the same
+    x and weight, and the stats that it kept.
+
+    dx = residual + the norm's part, of x's type: ``residual`` is a gradient
+    that reaches x past the norm.  Each of ``dx`` (which may be dy or
+    residual), ``dw`` and ``db`` is a tensor to write, True for a new one, or
+    False (None in the result).  New dw and db have x's type or ``dw_dtype``:
+    float32, as for rank buffers of a :class:`Plan`.  ``accumulate`` adds to
+    the dw and db given."""
+    return _layer_call("ar_layer_norm_backward", _bind.norm_backward,
+                       (dy, x, stats, weight, residual, dx, dw, db, _float_code(dw_dtype, "dw_dtype"), bool(accumulate)),
+                       stream)

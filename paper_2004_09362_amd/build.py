@@ -19,10 +19,12 @@ LIB = os.path.join(HERE, "libar.so")
 SOURCES = [os.path.join(CSRC, f) for f in ["plan.cpp", "capi.cpp", "kernels.hip", "fused_lo.hip", "fused_group.hip",
                                            "fused_free.hip", "fused_small.hip",
                                            "broadcast.hip", "noalloc.hip", "layers.cpp", "gemm_bf16.hip",
-                                           "gemm_f16.hip", "gemm_f32.hip", "gemm_few.hip", "rowwise.hip"]]
+                                           "gemm_f16.hip", "gemm_f32.hip", "gemm_few.hip", "rowwise.hip",
+                                           "training.cpp", "norm.hip"]]
 HEADERS = [os.path.join(CSRC, f) for f in ("ar_internal.hpp", "device_common.hpp", "fused_col.hpp",
                                                "fused_free.hpp", "free_shape.hpp", "layers.hpp",
-                                               "layer_device.hpp", "gemm.hpp")] + [
+                                               "layer_device.hpp", "layer_checks.hpp", "gemm.hpp",
+                                               "training.hpp")] + [
     os.path.join(ROOT, "include", "ar.h")]
 # The native part of the Python binding: host code only, against torch's and Python's headers.
 BIND_SOURCE = os.path.join(CSRC, "bind.cpp")
@@ -170,8 +172,9 @@ FAMILIES = {
     "free": ["fused_free.hip", "fused_free.hpp", "free_shape.hpp"],
     "small": ["fused_small.hip"],
     "bcast": ["broadcast.hip"],
-    "layer": ["layers.cpp", "layers.hpp", "layer_device.hpp", "gemm.hpp", "gemm_bf16.hip", "gemm_f16.hip",
+    "layer": ["layers.cpp", "layers.hpp", "layer_checks.hpp", "layer_device.hpp", "gemm.hpp", "gemm_bf16.hip", "gemm_f16.hip",
               "gemm_f32.hip", "gemm_few.hip", "rowwise.hip"],
+    "training": ["training.cpp", "training.hpp", "norm.hip"],
 }
 
 
@@ -185,7 +188,8 @@ def kernel_families(kernel: str) -> list[str]:
                             ("fused_ring_kernel", "group"), ("fused_free_kernel", "free"),
                             ("fused_small_kernel", "small"), ("fused_wide_kernel", "col"),
                             ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast"),
-                            ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer")):
+                            ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer"),
+                            ("norm_", "training")):
             if part.startswith(prefix):
                 out.append(fam)
                 break

@@ -124,6 +124,15 @@ ar_status (*g_linear_backward_workspace)(int64_t, int64_t, int64_t, const ar_mat
 ar_status (*g_dropout_forward)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_dropout*,
                                const ar_matrix*, hipStream_t) = nullptr;
 
+ar_status (*g_norm_forward)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*, double,
+                            const ar_matrix*, const ar_matrix*, hipStream_t) = nullptr;
+ar_status (*g_norm_backward)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*, const ar_matrix*,
+                             const ar_matrix*, const ar_matrix*, const ar_matrix*, const ar_matrix*, int32_t, void*,
+                             int64_t, hipStream_t) = nullptr;
+ar_status (*g_norm_backward_workspace)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*,
+                                       const ar_matrix*, const ar_matrix*, const ar_matrix*, const ar_matrix*,
+                                       const ar_matrix*, int64_t*) = nullptr;
+
 struct Fault {
   std::string text;
 };
@@ -246,6 +255,17 @@ PyObject* answer(F&& body) {
   }
 }
 
+// a, or (a, b) where b is kept.
+PyObject* with_kept(const at::Tensor& a, const at::Tensor& b) {
+  PyObject* pa = THPVariable_Wrap(a);
+  if (!b.defined() || !pa) return pa;
+  PyObject* pb = THPVariable_Wrap(b);
+  PyObject* both = pb ? PyTuple_Pack(2, pa, pb) : nullptr;
+  Py_DECREF(pa);
+  Py_XDECREF(pb);
+  return both;
+}
+
 // linear_forward(x, w, bias, residual, out, preact, activation, out dtype, dropout, device, stream)
 // -> y, (y, z) where preact is a tensor or True, a status, or a text.
 PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
@@ -283,13 +303,7 @@ PyObject* linear_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (st != AR_OK) return PyLong_FromLong(long(st));
     written(args[4], y);
     if (z.defined()) written(args[5], z);
-    PyObject* py = THPVariable_Wrap(y);
-    if (!z.defined() || !py) return py;
-    PyObject* pz = THPVariable_Wrap(z);
-    PyObject* both = pz ? PyTuple_Pack(2, py, pz) : nullptr;
-    Py_DECREF(py);
-    Py_XDECREF(pz);
-    return both;
+    return with_kept(y, z);
   });
 }
 
@@ -298,6 +312,27 @@ at::Tensor wanted(PyObject* o, const char* name, at::IntArrayRef shape, const at
   if (o == Py_None || o == Py_False) return at::Tensor();
   if (o == Py_True) return at::empty(shape, options);
   return tensor(o, name);
+}
+
+// The tuple (dx, dw, db) of what was written, None for what was not wanted.
+PyObject* gradients(PyObject* const* given, const at::Tensor& dx, const at::Tensor& dw, const at::Tensor& db) {
+  PyObject* got = PyTuple_New(3);
+  const at::Tensor* const parts[] = {&dx, &dw, &db};
+  for (int i = 0; got && i < 3; ++i) {
+    PyObject* o = Py_None;
+    if (parts[i]->defined()) {
+      written(given[i], *parts[i]);
+      o = THPVariable_Wrap(*parts[i]);
+    } else {
+      Py_INCREF(o);
+    }
+    if (!o) {
+      Py_DECREF(got);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(got, i, o);
+  }
+  return got;
 }
 
 // linear_backward(dy, x, w, preact, activation, dropout, dx, dw, db, dx dtype, dw dtype, accumulate, device, stream)
@@ -346,23 +381,7 @@ PyObject* linear_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
       Py_END_ALLOW_THREADS
     }
     if (st != AR_OK) return PyLong_FromLong(long(st));
-    PyObject* got = PyTuple_New(3);
-    const at::Tensor* const parts[] = {&dx, &dw, &db};
-    for (int i = 0; got && i < 3; ++i) {
-      PyObject* o = Py_None;
-      if (parts[i]->defined()) {
-        written(args[6 + i], *parts[i]);
-        o = THPVariable_Wrap(*parts[i]);
-      } else {
-        Py_INCREF(o);
-      }
-      if (!o) {
-        Py_DECREF(got);
-        return nullptr;
-      }
-      PyTuple_SET_ITEM(got, i, o);
-    }
-    return got;
+    return gradients(args + 6, dx, dw, db);
   });
 }
 
@@ -394,12 +413,97 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
-// bind_layers(addresses of the five functions above, in their order)
+double real(PyObject* o, const char* name) {
+  const double v = PyFloat_AsDouble(o);
+  const bool bad = PyErr_Occurred() != nullptr;
+  PyErr_Clear();
+  if (bad) throw Fault{std::string(name) + " must be a number"};
+  return v;
+}
+
+// norm_forward(x, weight, bias, eps, out, out dtype, stats, device, stream)
+// -> y, (y, stats) where stats is a tensor or True, a status, or a text.
+PyObject* norm_forward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 9 || !g_norm_forward) throw Fault{"norm_forward takes 9 arguments"};
+    const Place at_{number(args[7], "device"), number(args[8], "stream")};
+    const at::Tensor& x = unrecorded(args[0], "x");
+    const ar_matrix mx = view(x, "x", 2, -1, -1, at_);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    ar_matrix mw, mb, ms;
+    if (args[1] != Py_None) mw = view(unrecorded(args[1], "weight"), "weight", 1, 1, cols, at_);
+    if (args[2] != Py_None) mb = view(unrecorded(args[2], "bias"), "bias", 1, 1, cols, at_);
+    const double eps = real(args[3], "eps");
+    const int64_t code = number(args[5], "out dtype");
+    at::Tensor y, s;
+    if (args[4] != Py_None) y = unrecorded(args[4], "out");
+    else y = at::empty({rows, cols}, x.options().dtype(scalar_of(code, x.scalar_type())));
+    if (args[6] == Py_True) s = at::empty({rows, 2}, x.options().dtype(at::kFloat));
+    else if (args[6] != Py_None && args[6] != Py_False) s = unrecorded(args[6], "stats");
+    const ar_matrix my = view(y, "out", 2, rows, cols, at_);
+    if (s.defined()) ms = view(s, "stats", 2, rows, 2, at_);
+    ar_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = g_norm_forward(rows, cols, &mx, args[1] != Py_None ? &mw : nullptr, args[2] != Py_None ? &mb : nullptr, eps,
+                        &my, s.defined() ? &ms : nullptr, at_.hip());
+    Py_END_ALLOW_THREADS
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    written(args[4], y);
+    if (s.defined()) written(args[6], s);
+    return with_kept(y, s);
+  });
+}
+
+// norm_backward(dy, x, stats, weight, residual, dx, dw, db, dw dtype, accumulate, device, stream)
+// -> (dx, dw, db) with None for what was not wanted, a status, or a text.
+PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 12 || !g_norm_backward) throw Fault{"norm_backward takes 12 arguments"};
+    const Place at_{number(args[10], "device"), number(args[11], "stream")};
+    const at::Tensor& dy = tensor(args[0], "dy");
+    const at::Tensor& x = tensor(args[1], "x");
+    const ar_matrix mdy = view(dy, "dy", 2, -1, -1, at_);
+    const int64_t rows = dy.size(0), cols = dy.size(1);
+    const ar_matrix mx = view(x, "x", 2, rows, cols, at_);
+    const ar_matrix ms = view(tensor(args[2], "stats"), "stats", 2, rows, 2, at_);
+    ar_matrix mw, mr, mdx, mdw, mdb;
+    if (args[3] != Py_None) mw = view(tensor(args[3], "weight"), "weight", 1, 1, cols, at_);
+    if (args[4] != Py_None) mr = view(tensor(args[4], "residual"), "residual", 2, rows, cols, at_);
+    const auto same = x.options();
+    const auto other = same.dtype(scalar_of(number(args[8], "dw dtype"), x.scalar_type()));
+    const bool accumulate = args[9] == Py_True;
+    if (accumulate && (args[6] == Py_True || args[7] == Py_True))
+      throw Fault{"accumulate adds to the dw and db that are given: they must be tensors"};
+    const at::Tensor dx = wanted(args[5], "dx", {rows, cols}, same);
+    const at::Tensor dw = wanted(args[6], "dw", {cols}, other), db = wanted(args[7], "db", {cols}, other);
+    if (dx.defined()) mdx = view(dx, "dx", 2, rows, cols, at_);
+    if (dw.defined()) mdw = view(dw, "dw", 1, 1, cols, at_);
+    if (db.defined()) mdb = view(db, "db", 1, 1, cols, at_);
+    const ar_matrix* pw = args[3] != Py_None ? &mw : nullptr;
+    const ar_matrix* pr = args[4] != Py_None ? &mr : nullptr;
+    const ar_matrix* pdx = dx.defined() ? &mdx : nullptr;
+    const ar_matrix* pdw = dw.defined() ? &mdw : nullptr;
+    const ar_matrix* pdb = db.defined() ? &mdb : nullptr;
+    int64_t bytes = 0;
+    ar_status st = g_norm_backward_workspace(rows, cols, &mdy, &mx, &ms, pw, pr, pdx, pdw, pdb, &bytes);
+    if (st == AR_OK) {
+      const at::Tensor ws = workspace(bytes, dy);
+      Py_BEGIN_ALLOW_THREADS
+      st = g_norm_backward(rows, cols, &mdy, &mx, &ms, pw, pr, pdx, pdw, pdb, accumulate, address(ws), bytes, at_.hip());
+      Py_END_ALLOW_THREADS
+    }
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    return gradients(args + 5, dx, dw, db);
+  });
+}
+
+// bind_layers(addresses of the functions above, in their order)
 PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  int64_t a[5];
-  for (int i = 0; i < 5; ++i) {
-    if (nargs != 5 || !as_int(args[i], &a[i])) {
-      PyErr_SetString(PyExc_TypeError, "bind_layers takes five addresses");
+  constexpr int kFunctions = 8;
+  int64_t a[kFunctions];
+  for (int i = 0; i < kFunctions; ++i) {
+    if (nargs != kFunctions || !as_int(args[i], &a[i])) {
+      PyErr_SetString(PyExc_TypeError, "bind_layers takes the address of each layer function");
       return nullptr;
     }
   }
@@ -408,6 +512,9 @@ PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   g_linear_backward = reinterpret_cast<decltype(g_linear_backward)>(a[2]);
   g_linear_backward_workspace = reinterpret_cast<decltype(g_linear_backward_workspace)>(a[3]);
   g_dropout_forward = reinterpret_cast<decltype(g_dropout_forward)>(a[4]);
+  g_norm_forward = reinterpret_cast<decltype(g_norm_forward)>(a[5]);
+  g_norm_backward = reinterpret_cast<decltype(g_norm_backward)>(a[6]);
+  g_norm_backward_workspace = reinterpret_cast<decltype(g_norm_backward_workspace)>(a[7]);
   Py_RETURN_NONE;
 }
 
@@ -418,6 +525,8 @@ PyMethodDef kMethods[] = {
     {"linear_forward", fastcall(linear_forward), METH_FASTCALL, nullptr},
     {"linear_backward", fastcall(linear_backward), METH_FASTCALL, nullptr},
     {"dropout", fastcall(dropout), METH_FASTCALL, nullptr},
+    {"norm_forward", fastcall(norm_forward), METH_FASTCALL, nullptr},
+    {"norm_backward", fastcall(norm_backward), METH_FASTCALL, nullptr},
     {"bind_layers", fastcall(bind_layers), METH_FASTCALL, nullptr},
     {"execute", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(execute)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(bind)), METH_FASTCALL, nullptr},
