@@ -574,6 +574,38 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
                                            const ar_matrix* dx, const ar_matrix* dw, const ar_matrix* db,
                                            int64_t* bytes);
 
+/* The orthogonalised update of weights (Newton-Schulz products, as the Muon
+ * optimiser takes them of a summed gradient's momentum): for each of `batch`
+ * matrices x [M, N], of any of the three types, x_stride elements from one to the
+ * next,
+ *   X = x / (|x| + eps)                       |x| the Frobenius norm
+ *   A = X X^T,  X = a X + (b A + c A A) X     steps times (M > N: of X^T)
+ *   y = residual + scale X                    [M, N], of any of the types
+ * with a, b, c the three numbers of each step in coefficients (3 * steps, read
+ * by the call).  X keeps x's singular vectors; its singular values are taken
+ * through a s + b s^3 + c s^5, with (3.4445, -4.7750, 2.0315) five times to about
+ * 0.7 to 1.2 from 0.004 up.
+ *
+ * X is held in 22 bits; products are summed in 32.  Towards a y of bfloat16 their
+ * operands are rounded to 11 bits, which leaves X off by up to 2e-3 of its norm
+ * before its rounding, whatever its rank; towards float32 and float16 they are
+ * taken in 22 bits, in three products.  Coefficients that can take a singular
+ * value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1, steps
+ * after one another) are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN
+ * gives NaN throughout; others of the batch do not see it.
+ *
+ * residual (NULL: none) has y's type; y may be residual or x where data, ld,
+ * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).
+ * steps: 1 to 64.  AR_ERR_UNSUPPORTED: a shorter side above 32768, a longer one
+ * above 2^21, 65536 matrices or more, more than 2^34 elements in all (sides
+ * rounded up to 256).  Workspace (about 10 bytes an element, in whole tiles of 128
+ * or 256) and errors as of ar_linear_forward. */
+ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix* x, int64_t x_stride, int32_t steps,
+                           const double* coefficients, double eps, double scale, const ar_matrix* residual,
+                           int64_t residual_stride, const ar_matrix* y, int64_t y_stride, void* workspace,
+                           int64_t workspace_bytes, hipStream_t stream);
+ar_status ar_orthogonalize_workspace(int64_t batch, int64_t M, int64_t N, const ar_matrix* y, int64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

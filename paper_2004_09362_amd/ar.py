@@ -45,6 +45,7 @@ EXPORTS = [
     "ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward", "ar_linear_backward_workspace",
     "ar_dropout_forward", "ar_dropout_backward",
     "ar_layer_norm_forward", "ar_layer_norm_backward", "ar_layer_norm_backward_workspace",
+    "ar_orthogonalize", "ar_orthogonalize_workspace",
 ]
 
 
@@ -163,7 +164,11 @@ def _load():
     L.ar_layer_norm_forward.argtypes = [i64, i64, mp, mp, mp, dbl, mp, mp, vp]
     L.ar_layer_norm_backward.argtypes = [i64, i64, mp, mp, mp, mp, mp, mp, mp, mp, i32, vp, i64, vp]
     L.ar_layer_norm_backward_workspace.argtypes = [i64, i64, mp, mp, mp, mp, mp, mp, mp, mp, ctypes.POINTER(i64)]
-    for name in ("ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward",
+    L.ar_orthogonalize.argtypes = [i64, i64, i64, mp, i64, i32, ctypes.POINTER(dbl), dbl, dbl, mp, i64, mp, i64, vp, i64,
+                                   vp]
+    L.ar_orthogonalize_workspace.argtypes = [i64, i64, i64, mp, ctypes.POINTER(i64)]
+    for name in ("ar_orthogonalize", "ar_orthogonalize_workspace",
+                 "ar_linear_forward", "ar_linear_forward_workspace", "ar_linear_backward",
                  "ar_linear_backward_workspace", "ar_dropout_forward", "ar_dropout_backward",
                  "ar_layer_norm_forward", "ar_layer_norm_backward", "ar_layer_norm_backward_workspace"):
         getattr(L, name).restype = ctypes.c_int
@@ -188,7 +193,8 @@ def _load_bind():
     mod.bind_layers(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.ar_linear_forward, lib.ar_linear_forward_workspace, lib.ar_linear_backward,
         lib.ar_linear_backward_workspace, lib.ar_dropout_forward, lib.ar_layer_norm_forward,
-        lib.ar_layer_norm_backward, lib.ar_layer_norm_backward_workspace)))
+        lib.ar_layer_norm_backward, lib.ar_layer_norm_backward_workspace, lib.ar_orthogonalize,
+        lib.ar_orthogonalize_workspace)))
     return mod
 
 
@@ -665,3 +671,30 @@ def ar_layer_norm_backward(dy, x, stats, weight=None, *, residual=None, dx=True,
     return _layer_call("ar_layer_norm_backward", _bind.norm_backward,
                        (dy, x, stats, weight, residual, dx, dw, db, _float_code(dw_dtype, "dw_dtype"), bool(accumulate)),
                        stream)
+
+
+def ar_orthogonalize(x, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                     scale: float = 1.0, residual=None, out=None, out_dtype=None, stream=None):
+    """y = residual + scale X, where X = x / (|x| + eps) goes ``steps`` times
+    through X <- a X + (b A + c A A) X, A = X X^T: x's singular vectors with
+    singular values of about 1 (Newton-Schulz products, as the Muon optimiser
+    takes them of a summed gradient's momentum).
+
+    x is a matrix [M, N] or a stack of them [B, M, N], each by itself.
+    ``coefficients`` is (a, b, c), or one such triple for each step.  y is
+    ``out`` (which may be x or ``residual``: a weight updated in place) or a
+    new tensor of ``out_dtype`` (default x's type; the residual has y's).
+    Towards bfloat16 the products take operands of 11 bits, towards the other
+    types of 22 in three products (see include/ar.h).  torch records no
+    gradient of the call: while it records, a tensor that requires one is
+    refused."""
+    steps = int(steps)
+    flat = tuple(coefficients)
+    if len(flat) == 3 and not any(isinstance(c, (tuple, list)) for c in flat):
+        flat = flat * max(steps, 0)
+    else:
+        if len(flat) != steps or any(not isinstance(c, (tuple, list)) or len(c) != 3 for c in flat):
+            raise ArError(AR_ERR_INVALID_ARG, "coefficients", "(a, b, c), or one such triple for each of %d steps" % steps)
+        flat = tuple(v for c in flat for v in c)
+    return _layer_call("ar_orthogonalize", _bind.orthogonalize,
+                       (x, flat, eps, scale, residual, out, _float_code(out_dtype, "out_dtype")), stream)

@@ -20,7 +20,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ["plan.cpp", "capi.cpp", "kernels.hip"
                                            "fused_free.hip", "fused_small.hip",
                                            "broadcast.hip", "noalloc.hip", "layers.cpp", "gemm_bf16.hip",
                                            "gemm_f16.hip", "gemm_f32.hip", "gemm_few.hip", "rowwise.hip",
-                                           "training.cpp", "norm.hip"]]
+                                           "training.cpp", "norm.hip", "orthogonal.hip"]]
 HEADERS = [os.path.join(CSRC, f) for f in ("ar_internal.hpp", "device_common.hpp", "fused_col.hpp",
                                                "fused_free.hpp", "free_shape.hpp", "layers.hpp",
                                                "layer_device.hpp", "layer_checks.hpp", "gemm.hpp",
@@ -174,7 +174,7 @@ FAMILIES = {
     "bcast": ["broadcast.hip"],
     "layer": ["layers.cpp", "layers.hpp", "layer_checks.hpp", "layer_device.hpp", "gemm.hpp", "gemm_bf16.hip", "gemm_f16.hip",
               "gemm_f32.hip", "gemm_few.hip", "rowwise.hip"],
-    "training": ["training.cpp", "training.hpp", "norm.hip"],
+    "training": ["training.cpp", "training.hpp", "norm.hip", "orthogonal.hip"],
 }
 
 
@@ -189,7 +189,7 @@ def kernel_families(kernel: str) -> list[str]:
                             ("fused_small_kernel", "small"), ("fused_wide_kernel", "col"),
                             ("fused_xor_wide_kernel", "group"), ("broadcast", "bcast"),
                             ("gemm_", "layer"), ("dropout_kernel", "layer"), ("slope_kernel", "layer"),
-                            ("norm_", "training")):
+                            ("norm_", "training"), ("ortho_", "training")):
             if part.startswith(prefix):
                 out.append(fam)
                 break

@@ -16,6 +16,7 @@
 #include <cstdint>
 #include <exception>
 #include <string>
+#include <vector>
 
 #include "../../include/ar.h"
 
@@ -132,6 +133,10 @@ ar_status (*g_norm_backward)(int64_t, int64_t, const ar_matrix*, const ar_matrix
 ar_status (*g_norm_backward_workspace)(int64_t, int64_t, const ar_matrix*, const ar_matrix*, const ar_matrix*,
                                        const ar_matrix*, const ar_matrix*, const ar_matrix*, const ar_matrix*,
                                        const ar_matrix*, int64_t*) = nullptr;
+
+ar_status (*g_orthogonalize)(int64_t, int64_t, int64_t, const ar_matrix*, int64_t, int32_t, const double*, double, double,
+                             const ar_matrix*, int64_t, const ar_matrix*, int64_t, void*, int64_t, hipStream_t) = nullptr;
+ar_status (*g_orthogonalize_workspace)(int64_t, int64_t, int64_t, const ar_matrix*, int64_t*) = nullptr;
 
 struct Fault {
   std::string text;
@@ -497,9 +502,62 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   });
 }
 
+// A matrix or a stack of them (3 dimensions) as its first matrix; stride: elements from one to the next.
+ar_matrix stack(const at::Tensor& t, const char* name, at::IntArrayRef shape, const Place& at_, int64_t* stride) {
+  if (t.dim() != int64_t(shape.size()) || (t.dim() == 3 && t.size(0) != shape[0]))
+    throw Fault{std::string(name) + " must have x's shape"};
+  *stride = 0;
+  if (t.dim() == 2) return view(t, name, 2, shape[0], shape[1], at_);
+  if (t.size(0) > 0) {
+    *stride = t.stride(0);
+    return view(t.select(0, 0), name, 2, shape[1], shape[2], at_);
+  }
+  (void)view(t.flatten(0, 1), name, 2, 0, shape[2], at_);  // its type and device
+  ar_matrix m{};
+  m.dtype = dtype_of(t, name);
+  return m;
+}
+
+// orthogonalize(x, coefficients, eps, scale, residual, out, out dtype, device, stream) -> y, a status, or a text.
+PyObject* orthogonalize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  return answer([&]() -> PyObject* {
+    if (nargs != 9 || !g_orthogonalize) throw Fault{"orthogonalize takes 9 arguments"};
+    const Place at_{number(args[7], "device"), number(args[8], "stream")};
+    const at::Tensor& x = unrecorded(args[0], "x");
+    if (x.layout() != at::kStrided || x.dim() < 2 || x.dim() > 3) throw Fault{"x must be a matrix or a stack of matrices (2 or 3 dimensions)"};
+    int64_t sx = 0, sr = 0, sy = 0;
+    const ar_matrix mx = stack(x, "x", x.sizes(), at_, &sx);
+    const bool one = x.dim() == 2;
+    const int64_t batch = one ? 1 : x.size(0), M = x.size(one ? 0 : 1), N = x.size(one ? 1 : 2);
+    if (!PyTuple_Check(args[1])) throw Fault{"coefficients must be three numbers for each step"};
+    std::vector<double> c(size_t(PyTuple_GET_SIZE(args[1])));
+    for (size_t i = 0; i < c.size(); ++i) c[i] = real(PyTuple_GET_ITEM(args[1], Py_ssize_t(i)), "a coefficient");
+    const double eps = real(args[2], "eps"), scale = real(args[3], "scale");
+    ar_matrix mr;
+    if (args[4] != Py_None) mr = stack(unrecorded(args[4], "residual"), "residual", x.sizes(), at_, &sr);
+    const int64_t code = number(args[6], "out dtype");
+    at::Tensor y;
+    if (args[5] != Py_None) y = unrecorded(args[5], "out");
+    else y = at::empty(x.sizes(), x.options().dtype(scalar_of(code, x.scalar_type())));
+    const ar_matrix my = stack(y, "out", x.sizes(), at_, &sy);
+    int64_t bytes = 0;
+    ar_status st = g_orthogonalize_workspace(batch, M, N, &my, &bytes);
+    if (st == AR_OK) {
+      const at::Tensor ws = workspace(bytes, x);
+      Py_BEGIN_ALLOW_THREADS
+      st = g_orthogonalize(batch, M, N, &mx, sx, int32_t(c.size() / 3), c.data(), eps, scale,
+                           args[4] != Py_None ? &mr : nullptr, sr, &my, sy, address(ws), bytes, at_.hip());
+      Py_END_ALLOW_THREADS
+    }
+    if (st != AR_OK) return PyLong_FromLong(long(st));
+    written(args[5], y);
+    return THPVariable_Wrap(y);
+  });
+}
+
 // bind_layers(addresses of the functions above, in their order)
 PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
-  constexpr int kFunctions = 8;
+  constexpr int kFunctions = 10;
   int64_t a[kFunctions];
   for (int i = 0; i < kFunctions; ++i) {
     if (nargs != kFunctions || !as_int(args[i], &a[i])) {
@@ -515,6 +573,8 @@ PyObject* bind_layers(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   g_norm_forward = reinterpret_cast<decltype(g_norm_forward)>(a[5]);
   g_norm_backward = reinterpret_cast<decltype(g_norm_backward)>(a[6]);
   g_norm_backward_workspace = reinterpret_cast<decltype(g_norm_backward_workspace)>(a[7]);
+  g_orthogonalize = reinterpret_cast<decltype(g_orthogonalize)>(a[8]);
+  g_orthogonalize_workspace = reinterpret_cast<decltype(g_orthogonalize_workspace)>(a[9]);
   Py_RETURN_NONE;
 }
 
@@ -527,6 +587,7 @@ PyMethodDef kMethods[] = {
     {"dropout", fastcall(dropout), METH_FASTCALL, nullptr},
     {"norm_forward", fastcall(norm_forward), METH_FASTCALL, nullptr},
     {"norm_backward", fastcall(norm_backward), METH_FASTCALL, nullptr},
+    {"orthogonalize", fastcall(orthogonalize), METH_FASTCALL, nullptr},
     {"bind_layers", fastcall(bind_layers), METH_FASTCALL, nullptr},
     {"execute", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(execute)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(bind)), METH_FASTCALL, nullptr},

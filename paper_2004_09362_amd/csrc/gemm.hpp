@@ -577,6 +577,100 @@ __device__ __forceinline__ void direct_full(const GemmArgs& g, const f32x4v (&ac
   }
 }
 
+// Where the tiles of an operand lie: one after the other along the inner length.
+struct Straight {
+  template <typename Op>
+  __device__ __forceinline__ const char* at(const Op& op, int32_t t) const { return op.at(t); }
+  // from the tile before t to t, which is below whole or not there
+  template <typename Op>
+  __device__ __forceinline__ void move(const char*& p, const Op& op, int32_t t, int32_t whole) const {
+    p += t < whole ? op.step() : 0;
+  }
+};
+
+// The products of `whole` tiles of the inner length, added to acc.  Operands take
+// the 2 D + 1 places in LDS in turn: a of tile 0, b of tile 0, a of tile 1, and
+// so on.  Slice 0 of tile t is multiplied while slice 1 is read, and slice 1
+// while slice 0 of tile t + 1 is.  Once every wave has read the whole of tile t,
+// b of t + D is loaded to where a of t lay, and then a of t + D + 1 to where b of t
+// lay; the waves' next meeting waits for tile t + 2 and before.  fa and fb are the
+// fragments of both slices, whose contents do not matter before and after.
+template <typename T, int MT, int NT, int D, typename OpA, typename OpB, typename FragA, typename FragB, typename Where>
+__device__ __forceinline__ void multiply_ring(f32x4v (&acc)[MT][NT], const OpA& a, const OpB& b, const FragA& ra,
+                                              const FragB& rb, i32x4v (&fa)[2][MT], i32x4v (&fb)[2][NT], char* lds, int wave,
+                                              int32_t whole, const Where& where) {
+  constexpr uint32_t kPlace = OpA::kBytes, kRing = (2 * D + 1) * kPlace;
+  constexpr bool kPinned = MT * NT == 64;
+  constexpr int kReads = MT + NT, kProducts = MT * NT, kLoadsA = OpA::kSlots, kLoadsB = OpB::kSlots;
+  static_assert(kLoadsA == kLoadsB && OpB::kBytes == kPlace, "operands of one size");
+  const uint32_t lds0 = lds_offset(lds);
+  auto after = [](uint32_t place) { return place == kRing - kPlace ? 0 : place + kPlace; };
+  // fragment x of slice s, first those of b
+  auto read = [&](int s, uint32_t at_a, uint32_t at_b, int x) {
+    if (x < NT) fb[s][x] = rb.read(lds + at_b, x, s);
+    else fa[s][x - NT] = ra.read(lds + at_a, x - NT, s);
+  };
+  auto product = [&](int s, int x) {
+    const int i = x / NT, j = x % NT;
+    if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
+    else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
+  };
+  // all of an operand's tile t, or of the last one
+  auto load_all = [&](const auto& op, int32_t t, uint32_t at) {
+    const char* p = settled(where.at(op, t < whole ? t : whole - 1));
+#pragma unroll
+    for (int x = 0; x < kLoadsA; ++x) {
+      op.aim(x, lds0 + at, wave);
+      asm volatile("s_nop 0");
+      op.issue(p, x);
+    }
+  };
+  uint32_t at_a = 0, at_b = kPlace;
+  if (whole > 0) {
+#pragma unroll
+    for (int x = 0; x <= 2 * D; ++x) {
+      if (x % 2 == 0) load_all(a, x / 2, uint32_t(x) * kPlace);
+      else load_all(b, x / 2, uint32_t(x) * kPlace);
+    }
+    wait_all<(2 * D - 1) * kLoadsA>();
+#pragma unroll
+    for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
+  }
+  // The instruction stream of a tile: between two matrix instructions goes
+  // at most one other of each kind, so that the matrix unit always has its
+  // next one, and the loads are spread, since each keeps the address unit
+  // busy for 16 cycles.  Slice 1 is read within the first half of slice 0's
+  // products; after kMeet of them the waves meet.  The last tiles run the
+  // same stream: their loads take the last tile again, which nobody reads.
+  constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
+  constexpr int kGapB = kProducts >= 64 ? 5 : 2, kGapA = kProducts >= 64 ? 6 : 3, kMeetA = kMeet + kGapB * kLoadsB;
+  static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA <= 2 * kProducts, "everything within a tile");
+  const char* pb = settled(where.at(b, whole > D ? D : whole - 1));
+  const char* pa = settled(where.at(a, whole > D + 1 ? D + 1 : whole - 1));
+  for (int32_t t = 0; t < whole; ++t) {
+    const uint32_t next_a = after(at_b), next_b = after(next_a);
+    const char* const from_a = settled(pa);
+    const char* const from_b = settled(pb);
+    if constexpr (kPinned) mma_ready();
+    unrolled([&](auto index) {
+      constexpr int x = decltype(index)::value, y = x - kProducts, zb = x - kMeet, za = x - kMeetA;
+      if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, at_a, at_b, x / kReadGap);
+      if constexpr (x == kMeet) wait_all<(2 * D - 3) * kLoadsA>();
+      if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, next_a, next_b, y / kReadGap1);
+      if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
+      if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(from_b, zb / kGapB);
+      if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
+      if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(from_a, za / kGapA);
+      product(x / kProducts, x % kProducts);
+      __builtin_amdgcn_sched_barrier(0);
+    }, std::make_integer_sequence<int, 2 * kProducts>{});
+    where.move(pb, b, t + D + 1, whole);
+    where.move(pa, a, t + D + 2, whole);
+    at_a = next_a;
+    at_b = next_b;
+  }
+}
+
 // LDS of a workgroup: five places, each for one operand of a tile.
 constexpr int ring_bytes(int tile) { return 5 * tile * kTileKBytes; }
 
@@ -621,82 +715,9 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
 
   const int32_t tiles = (klen + kInner - 1) / kInner;
   if constexpr (ASYNC) {
-    // Operands take the five places in turn: a of tile 0, b of tile 0, a of
-    // tile 1, and so on.  Slice 0 of tile t is multiplied while slice 1 is
-    // read, and slice 1 while slice 0 of tile t + 1 is.  Once every wave has
-    // read the whole of tile t, b of t + 2 is loaded to where a of t lay, and
-    // then a of t + 3 to where b of t lay; the waves' next meeting waits for
-    // all but the latter.
-    const uint32_t lds0 = lds_offset(lds);
-    i32x4v fa[2][MT], fb[2][NT];
-    constexpr int kReads = MT + NT, kProducts = MT * NT, kLoadsA = OpA::kSlots, kLoadsB = OpB::kSlots;
-    auto after = [](uint32_t place) { return place == kRing - kPlace ? 0 : place + kPlace; };
-    // fragment x of slice s, first those of b
-    auto read = [&](int s, uint32_t at_a, uint32_t at_b, int x) {
-      if (x < NT) fb[s][x] = rb.read(lds + at_b, x, s);
-      else fa[s][x - NT] = ra.read(lds + at_a, x - NT, s);
-    };
-    auto product = [&](int s, int x) {
-      const int i = x / NT, j = x % NT;
-      if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
-      else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
-    };
     const int32_t whole = klen / kInner;
-    // all of an operand's tile t, or of the last one
-    auto load_all = [&](const auto& op, int32_t t, uint32_t at) {
-      const char* p = settled(op.at(t < whole ? t : whole - 1));
-#pragma unroll
-      for (int x = 0; x < kLoadsA; ++x) {
-        op.aim(x, lds0 + at, wave);
-        asm volatile("s_nop 0");
-        op.issue(p, x);
-      }
-    };
-    static_assert(kLoadsA == kLoadsB, "operands of one size");
-    uint32_t at_a = 0, at_b = kPlace;
-    if (whole > 0) {
-      load_all(a, 0, 0);
-      load_all(b, 0, kPlace);
-      load_all(a, 1, 2 * kPlace);
-      load_all(b, 1, 3 * kPlace);
-      load_all(a, 2, 4 * kPlace);
-      wait_all<3 * kLoadsA>();
-#pragma unroll
-      for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
-    }
-    // The instruction stream of a tile: between two matrix instructions goes
-    // at most one other of each kind, so that the matrix unit always has its
-    // next one, and the loads are spread, since each keeps the address unit
-    // busy for 16 cycles.  Slice 1 is read within the first half of slice 0's
-    // products; after kMeet of them the waves meet.  The last tiles run the
-    // same stream: their loads take the last tile again, which nobody reads.
-    constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
-    constexpr int kGapB = kProducts >= 64 ? 5 : 2, kGapA = kProducts >= 64 ? 6 : 3, kMeetA = kMeet + kGapB * kLoadsB;
-    static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA <= 2 * kProducts, "everything within a tile");
-    const char* pb = settled(b.at(whole > 2 ? 2 : whole - 1));
-    const char* pa = settled(a.at(whole > 3 ? 3 : whole - 1));
-    for (int32_t t = 0; t < whole; ++t) {
-      const uint32_t next_a = after(at_b), next_b = after(next_a);
-      const char* const from_a = settled(pa);
-      const char* const from_b = settled(pb);
-      if constexpr (kPinned) mma_ready();
-      unrolled([&](auto index) {
-        constexpr int x = decltype(index)::value, y = x - kProducts, zb = x - kMeet, za = x - kMeetA;
-        if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, at_a, at_b, x / kReadGap);
-        if constexpr (x == kMeet) wait_all<kLoadsA>();
-        if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, next_a, next_b, y / kReadGap1);
-        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
-        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(from_b, zb / kGapB);
-        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
-        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(from_a, za / kGapA);
-        product(x / kProducts, x % kProducts);
-        __builtin_amdgcn_sched_barrier(0);
-      }, std::make_integer_sequence<int, 2 * kProducts>{});
-      pb += t + 3 < whole ? b.step() : 0;
-      pa += t + 4 < whole ? a.step() : 0;
-      at_a = next_a;
-      at_b = next_b;
-    }
+    i32x4v fa[2][MT], fb[2][NT];
+    multiply_ring<T, MT, NT, 2>(acc, a, b, ra, rb, fa, fb, lds, wave, whole, Straight{});
     if (whole < tiles) {  // what is left of the inner length, through registers
       wait_all<0>();
       a.copy(whole, klen - int64_t(whole) * kInner, lds, tid);
@@ -705,11 +726,20 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& g, uint32_t tile, uint
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
 #pragma unroll
-        for (int x = 0; x < kReads; ++x) read(s, 0, kPlace, x);
+        for (int x = 0; x < NT; ++x) fb[s][x] = rb.read(lds + kPlace, x, s);
+#pragma unroll
+        for (int x = 0; x < MT; ++x) fa[s][x] = ra.read(lds, x, s);
       }
       if constexpr (kPinned) mma_ready();
 #pragma unroll
-      for (int x = 0; x < 2 * kProducts; ++x) product(x / kProducts, x % kProducts);
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            if constexpr (kPinned) mma_pinned<T>(fb[s][j], fa[s][i], acc[i][j]);
+            else acc[i][j] = mma<T>(fb[s][j], fa[s][i], acc[i][j]);
+          }
     }
     if constexpr (kPinned) mma_done(acc[MT - 1], acc[MT - 2], acc[MT - 3]);
   } else {

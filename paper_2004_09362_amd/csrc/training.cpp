@@ -1,12 +1,14 @@
-// training.cpp -- the C ABI of layer norm and its gradient (include/ar.h,
-// "Layer operators"): argument checks, the choice of kernels, and launches.  The
-// kernels are in norm.hip; nothing here computes on the host.
+// training.cpp -- the C ABI of layer norm, its gradient and the orthogonalised
+// update (include/ar.h, "Layer operators"): argument checks, the choice of
+// kernels, and launches.  The kernels are in norm.hip and orthogonal.hip; nothing
+// here computes on the host.
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
+#include <utility>
 
 #include "../../include/ar.h"
 #include "layer_checks.hpp"
@@ -48,6 +50,157 @@ void check_norm_grad(int64_t rows, int64_t cols, const ar_matrix* dy, const ar_m
 int64_t norm_grad_bytes(int64_t rows, int64_t cols, const ar_matrix* dw, const ar_matrix* db) {
   if ((!dw && !db) || rows == 0 || cols == 0) return 0;
   return int64_t(ar::norm_grad_blocks(rows, cols)) * 2 * cols * 4;
+}
+
+// ---- the orthogonalised update ----
+
+constexpr int32_t kMaxSteps = 64;
+constexpr int64_t kMaxShort = 32768, kMaxLong = int64_t(1) << 21, kMaxBatch = 65535, kMaxElements = int64_t(1) << 34;
+constexpr int64_t kCus = 256;
+
+// How one of a step's products runs.
+struct OrthoPlanPart {
+  int64_t tiles = 0, steps = 0, share = 0, workgroups = 0;
+  bool deep = false;
+  double micros = 0.0;
+  int64_t parts(int64_t tile) const { return share % steps == 0 ? 0 : workgroups * 2 * tile * tile * 4; }
+};
+
+OrthoPlanPart plan_part(int64_t tiles, int64_t batch, int64_t steps, int32_t shape) {
+  OrthoPlanPart best;
+  const int64_t all = tiles * batch * steps, tile = ar::tile_rows(shape);
+  auto offer = [&](int64_t share, bool deep) {
+    OrthoPlanPart p;
+    p.tiles = tiles;
+    p.steps = steps;
+    p.share = share;
+    p.workgroups = ceil_div(all, share);
+    p.deep = deep;
+    const bool large = shape == ar::kTile256;
+    const int64_t places = large || deep ? kCus : 2 * kCus, rounds = ceil_div(p.workgroups, places);
+    const double step = large ? 1.42 : deep ? 0.4 : 1.18, fixed = large ? 10.0 : 5.0;
+    // a share that is no whole number of tiles starts and ends within some
+    const double pieces = share % steps == 0 ? double(share / steps) : double(share) / double(steps) + 1.0;
+    p.micros = double(rounds) * (double(share) * step + pieces * fixed);
+    if (share % steps != 0) p.micros += 4.0 + double(p.parts(tile)) * 1.5 / 5e6;
+    if (best.share == 0 || p.micros < best.micros) best = p;
+  };
+  for (const bool deep : {false, true}) {
+    if (deep && shape == ar::kTile256) continue;
+    offer(steps, deep);
+    const int64_t places = deep || shape == ar::kTile256 ? kCus : 2 * kCus;
+    if (tiles * batch <= 8 * kCus) {
+      for (const int64_t w : {places, places / 2, places / 4}) {
+        const int64_t share = ceil_div(all, w);
+        if (share >= 4) offer(share, deep);
+      }
+    }
+  }
+  return best;
+}
+
+struct OrthoPlan {
+  ar::OrthoShape s{};
+  int32_t planes = 1, shape = ar::kTile128;
+  OrthoPlanPart part[3];
+  int64_t sums = 0, x = 0, a = 0, diag = 0, parts = 0;  // bytes of each
+  int64_t total() const { return sums + 2 * x + 2 * a + diag + parts; }
+};
+
+OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
+  OrthoPlan best;
+  double least = 0.0;
+  for (const int32_t shape : {ar::kTile128, ar::kTile256}) {
+    OrthoPlan p;
+    p.shape = shape;
+    p.planes = y == AR_BFLOAT16 ? 1 : 2;
+    p.s.rows = M;
+    p.s.cols = N;
+    p.s.batch = int32_t(batch);
+    p.s.turned = M > N;
+    const int64_t tile = ar::tile_rows(shape), pairs = p.planes == 2 ? 3 : 1;
+    p.s.mp = round_up(std::min(M, N), tile);
+    p.s.np = round_up(std::max(M, N), tile);
+    const int64_t tm = p.s.mp / tile, tn = p.s.np / tile;
+    p.part[ar::kOrthoGram] = plan_part(tm * (tm + 1) / 2, batch, pairs * (p.s.np / 64), shape);
+    p.part[ar::kOrthoSquare] = plan_part(tm * (tm + 1) / 2, batch, pairs * (p.s.mp / 64), shape);
+    p.part[ar::kOrthoApply] = plan_part(tm * tn, batch, pairs * (p.s.mp / 64), shape);
+    const double micros = p.part[0].micros + p.part[1].micros + p.part[2].micros;
+    if (least > 0.0 && micros >= least) continue;
+    least = micros;
+    p.sums = round_up(batch * ar::kOrthoSumBlocks * 8, kWorkspaceAlign);
+    p.x = batch * 2 * p.s.mp * p.s.np * 2;
+    p.a = batch * p.planes * p.s.mp * p.s.mp * 2;
+    p.diag = round_up(batch * p.s.mp * 4, kWorkspaceAlign);
+    p.parts = 0;
+    for (const OrthoPlanPart& q : p.part) p.parts = std::max(p.parts, q.parts(tile));
+    best = p;
+  }
+  return best;
+}
+
+void check_ortho_sizes(int64_t batch, int64_t M, int64_t N, const ar_matrix* y) {
+  check_length("batch", batch);
+  check_length("M", M);
+  check_length("N", N);
+  if (!y) refuse(AR_ERR_INVALID_ARG, "y is NULL");
+  if (!is_float(y->dtype)) refuse(AR_ERR_UNSUPPORTED, "y must be float32, float16 or bfloat16");
+  if (batch == 0 || M == 0 || N == 0) return;
+  if (batch > kMaxBatch) refuse(AR_ERR_UNSUPPORTED, "batch must be below 65536");
+  if (std::min(M, N) > kMaxShort || std::max(M, N) > kMaxLong)
+    refuse(AR_ERR_UNSUPPORTED, "the shorter side of a matrix must be at most 32768, the longer one 2^21");
+  if (round_up(M, 256) * round_up(N, 256) > kMaxElements / batch)
+    refuse(AR_ERR_UNSUPPORTED, "the matrices have more than 2^34 elements in whole tiles");
+}
+
+// `batch` matrices, `stride` elements from one to the next.
+void check_stack(const char* name, const ar_matrix* m, int64_t stride, int64_t batch, int64_t M, int64_t N, bool written) {
+  check_matrix(name, m, batch == 0 ? 0 : M, N);
+  if (batch <= 1 || M == 0 || N == 0) return;
+  const int64_t covers = (M > 1 ? (M - 1) * m->ld : 0) + N;
+  if (stride < 0 || stride > (int64_t(1) << 44))
+    refuse(AR_ERR_INVALID_ARG, std::string(name) + "'s stride must be in [0, 2^44]");
+  if (written && stride < covers) refuse(AR_ERR_INVALID_ARG, std::string(name) + "'s matrices overlap: the stride must be at least " + std::to_string(covers));
+}
+Extent stack_extent(const ar_matrix* m, int64_t stride, int64_t batch, int64_t M, int64_t N) {
+  if (!m || batch == 0) return Extent();
+  Extent e = extent(m, M, N);
+  if (batch == 1 || e.empty()) return e;
+  if (M > 1 && stride == M * m->ld) {  // rows of one pitch throughout
+    e.rows = batch * M;
+    return e;
+  }
+  const int64_t bytes = int64_t(e.end() - e.at) + (batch - 1) * stride * size_of(m->dtype);
+  e.row = e.pitch = bytes;
+  e.rows = 1;
+  return e;
+}
+
+// The coefficients of a step keep singular values that are at most `most` within
+// the range that the halves hold; `most` becomes the bound after the step.
+void check_coefficients(double a, double b, double c, double& most) {
+  if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) refuse(AR_ERR_INVALID_ARG, "the coefficients must be finite");
+  const double end = most * most;
+  double value = 0.0, q = 0.0;
+  auto look = [&](double s) {  // s: a square
+    if (!(s >= 0.0 && s <= end)) return;
+    value = std::max(value, std::sqrt(s) * std::fabs(a + s * (b + s * c)));
+    q = std::max(q, std::fabs(s * (b + s * c)));
+  };
+  look(end);
+  if (c != 0.0) {
+    const double root = 9.0 * b * b - 20.0 * a * c;
+    if (root >= 0.0) {  // the ends of a + 3 b s + 5 c s^2
+      look((-3.0 * b + std::sqrt(root)) / (10.0 * c));
+      look((-3.0 * b - std::sqrt(root)) / (10.0 * c));
+    }
+    look(-b / (2.0 * c));
+  } else if (b != 0.0) {
+    look(-a / (3.0 * b));
+  }
+  if (!(value <= 2.5) || !(q <= 15.0))
+    refuse(AR_ERR_INVALID_ARG, "the coefficients take a singular value past 2.5, or |b s + c s^2| of its square s past 15");
+  most = value;
 }
 
 }  // namespace
@@ -179,6 +332,105 @@ ar_status ar_layer_norm_backward(int64_t rows, int64_t cols, const ar_matrix* dy
       launched(ar::launch_norm_grad(c, elem_of(x->dtype), elem_of(dy->dtype), stream), "layer norm gradient kernel launch");
     }
     if (dw || db) launched(ar::launch_norm_join(j, stream), "join kernel launch");
+  });
+}
+
+ar_status ar_orthogonalize_workspace(int64_t batch, int64_t M, int64_t N, const ar_matrix* y, int64_t* bytes) {
+  return guarded([&] {
+    if (!bytes) refuse(AR_ERR_INVALID_ARG, "bytes is NULL");
+    *bytes = 0;
+    check_ortho_sizes(batch, M, N, y);
+    if (batch > 0 && M > 0 && N > 0) *bytes = plan_ortho(batch, M, N, y->dtype).total();
+  });
+}
+
+ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix* x, int64_t x_stride, int32_t steps,
+                           const double* coefficients, double eps, double scale, const ar_matrix* residual,
+                           int64_t residual_stride, const ar_matrix* y, int64_t y_stride, void* workspace,
+                           int64_t workspace_bytes, hipStream_t stream) {
+  return guarded([&] {
+    check_ortho_sizes(batch, M, N, y);
+    check_stack("x", x, x_stride, batch, M, N, false);
+    check_stack("y", y, y_stride, batch, M, N, true);
+    if (residual) {
+      check_stack("residual", residual, residual_stride, batch, M, N, false);
+      if (residual->dtype != y->dtype) refuse(AR_ERR_UNSUPPORTED, "residual must have y's type");
+    }
+    if (steps < 1 || steps > kMaxSteps) refuse(AR_ERR_INVALID_ARG, "steps must be in [1, 64]");
+    if (!coefficients) refuse(AR_ERR_INVALID_ARG, "coefficients is NULL");
+    double most = 1.0;
+    for (int32_t k = 0; k < steps; ++k) check_coefficients(coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], most);
+    if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(AR_ERR_INVALID_ARG, "eps must be finite and at least 0");
+    if (!std::isfinite(scale)) refuse(AR_ERR_INVALID_ARG, "scale must be finite");
+    if (batch == 0 || M == 0 || N == 0) return;
+    const Extent ex = stack_extent(x, x_stride, batch, M, N), ey = stack_extent(y, y_stride, batch, M, N);
+    const Extent er = stack_extent(residual, residual_stride, batch, M, N);
+    auto same = [&](const ar_matrix* m, int64_t stride) { return same_place(m, y, M) && (batch == 1 || stride == y_stride); };
+    if (!same(x, x_stride)) check_apart("y", ey, "x", ex);
+    if (residual && !same(residual, residual_stride)) check_apart("y", ey, "residual", er);
+    const OrthoPlan p = plan_ortho(batch, M, N, y->dtype);
+    const Extent ews = check_workspace(workspace, workspace_bytes, p.total());
+    check_apart("the workspace", ews, "x", ex);
+    check_apart("the workspace", ews, "y", ey);
+    check_apart("the workspace", ews, "residual", er);
+    check_device();
+    char* at = static_cast<char*>(workspace);
+    auto take = [&](int64_t bytes) {
+      char* const here = at;
+      at += bytes;
+      return here;
+    };
+    double* const sums = reinterpret_cast<double*>(take(p.sums));
+    void* X[2] = {take(p.x), nullptr};
+    X[1] = take(p.x);
+    void* const A = take(p.a);
+    void* const Q = take(p.a);
+    float* const diag = reinterpret_cast<float*>(take(p.diag));
+    float* const parts = reinterpret_cast<float*>(take(p.parts));
+    const ar::OrthoOuter ox{x->data, x->ld, x_stride, elem_of(x->dtype)}, oy{y->data, y->ld, y_stride, elem_of(y->dtype)};
+    ar::OrthoOuter ores{};
+    if (residual) ores = {residual->data, residual->ld, residual_stride, elem_of(residual->dtype)};
+    launched(ar::launch_ortho_norm(p.s, ox, sums, stream), "norm kernel launch");
+    launched(ar::launch_ortho_load(p.s, ox, sums, eps, X[0], stream), "load kernel launch");
+    const int64_t plane_x = p.s.mp * p.s.np, plane_a = p.s.mp * p.s.mp;
+    for (int32_t k = 0; k < steps; ++k) {
+      for (const int32_t kind : {ar::kOrthoGram, ar::kOrthoSquare, ar::kOrthoApply}) {
+        const OrthoPlanPart& q = p.part[kind];
+        const bool gram = kind == ar::kOrthoGram, apply = kind == ar::kOrthoApply;
+        ar::OrthoProduct g{};
+        g.left = gram ? X[0] : apply ? Q : A;
+        g.right = gram || apply ? X[0] : A;
+        g.old = apply ? X[0] : A;
+        g.out = gram ? A : apply ? X[1] : Q;
+        g.diag = diag;
+        g.parts = parts;
+        g.ld_left = gram ? p.s.np : p.s.mp;
+        g.ld_right = gram || apply ? p.s.np : p.s.mp;
+        g.ld_out = apply ? p.s.np : p.s.mp;
+        g.plane_left = gram ? plane_x : plane_a;
+        g.plane_right = gram || apply ? plane_x : plane_a;
+        g.plane_out = apply ? plane_x : plane_a;
+        g.batch_left = gram ? 2 * plane_x : p.planes * plane_a;
+        g.batch_right = gram || apply ? 2 * plane_x : p.planes * plane_a;
+        g.batch_out = apply ? 2 * plane_x : p.planes * plane_a;
+        g.M = int32_t(p.s.mp);
+        g.N = int32_t(apply ? p.s.np : p.s.mp);
+        g.K = int32_t(gram ? p.s.np : p.s.mp);
+        g.tiles_m = int32_t(p.s.mp / ar::tile_rows(p.shape));
+        g.tiles_n = g.N / ar::tile_rows(p.shape);
+        g.tiles = int32_t(q.tiles);
+        g.batch = int32_t(batch);
+        g.steps = int32_t(q.steps);
+        g.share = int32_t(q.share);
+        g.workgroups = int32_t(q.workgroups);
+        g.a = float(coefficients[3 * k]);
+        g.b = float(coefficients[3 * k + 1]);
+        g.c = float(coefficients[3 * k + 2]);
+        launched(ar::launch_ortho_product(g, kind, p.planes, p.shape, q.deep, stream), "Newton-Schulz product launch");
+      }
+      std::swap(X[0], X[1]);
+    }
+    launched(ar::launch_ortho_store(p.s, X[0], float(scale), ores, oy, stream), "store kernel launch");
   });
 }
 

@@ -59,4 +59,62 @@ struct NormJoinCall {
 };
 int launch_norm_join(const NormJoinCall& c, void* stream);
 
+// The orthogonalised update (orthogonal.hip).  Its matrices lie in the workspace
+// as halves, each value times a power of two: a value is the sum of two halves,
+// "high" and "low" (22 bits), in two planes.  They have m rows and n columns, m
+// the shorter side, padded with zeros to whole tiles (mp, np).
+constexpr float kOrthoScaleX = 8192.0f, kOrthoScaleA = 8192.0f, kOrthoScaleQ = 4096.0f;
+
+// x or y, in the user's layout: `rows` x `cols`; turned: m is its columns.
+struct OrthoOuter {
+  const void* data;
+  int64_t ld, stride;  // elements from row to row, and from matrix to matrix
+  int32_t elem;
+};
+struct OrthoShape {
+  int64_t rows, cols, mp, np;
+  int32_t batch, turned;
+};
+
+// sums[matrix][block] of the squares of x, in 64 bits.
+constexpr int32_t kOrthoSumBlocks = 128;
+int launch_ortho_norm(const OrthoShape& s, const OrthoOuter& x, double* sums, void* stream);
+// X = x / (|x| + eps), both planes.
+int launch_ortho_load(const OrthoShape& s, const OrthoOuter& x, const double* sums, double eps, void* planes, void* stream);
+// y = residual + scale X (residual.data NULL: none).
+int launch_ortho_store(const OrthoShape& s, const void* planes, float scale, const OrthoOuter& residual, const OrthoOuter& y,
+                       void* stream);
+
+// The three products of a step.
+enum OrthoKind : int32_t {
+  kOrthoGram = 0,    // A = X X^T
+  kOrthoSquare = 1,  // Q = b A + c A A without its diagonal, which goes to diag in 32 bits
+  kOrthoApply = 2    // X = a X + (Q + diag) X
+};
+
+// One product of each of `batch` matrices: out[m][n] of sums over k of
+// left(m, k) right(n, k), or of left(m, k) right(k, n) for kOrthoApply.  Tiles are
+// dealt out as steps (128 bytes of inner length of one tile and pair of planes):
+// workgroup w takes steps [w share, (w + 1) share) of all.  A tile that lies in
+// one share is finished there; of others the parts go to `parts` and are joined
+// by a second launch.
+struct OrthoProduct {
+  const void* left;
+  const void* right;
+  const void* old;   // kOrthoSquare: A, kOrthoApply: X
+  void* out;
+  float* diag;       // [batch][M]
+  float* parts;
+  int64_t ld_left, ld_right, ld_out;              // elements
+  int64_t plane_left, plane_right, plane_out;     // elements from the high plane to the low one
+  int64_t batch_left, batch_right, batch_out;     // from matrix to matrix
+  int32_t M, N, K;                                // multiples of the tile, K of 64
+  int32_t tiles_m, tiles_n, tiles;                // of a matrix; symmetric results: those on and below the diagonal
+  int32_t batch, steps, share, workgroups;        // steps of a tile
+  float a, b, c;
+};
+// How a product runs: its tile, and how many tiles ahead it loads (deep: one
+// workgroup to a compute unit).
+int launch_ortho_product(const OrthoProduct& g, int32_t kind, int32_t planes, int32_t shape, bool deep, void* stream);
+
 }  // namespace ar

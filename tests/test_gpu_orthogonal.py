@@ -1,0 +1,332 @@
+"""The orthogonalised update on the GPU: results that are exact in every bit where
+the arithmetic is (rows of Hadamard matrices, permutations), and distances from the
+definition in 64 bits elsewhere; wide and tall matrices, one element to many tiles,
+stacks, every type, any strides, low rank, in place, streams, graphs, NaN and
+infinities.
+
+How far a result may be off.  Towards float32 and float16 the steps hold X in 22
+bits, whose rounding is at most twice that of 32-bit arithmetic (24 bits, half of
+it in the sums), and sum in 32 bits: their distance from 64 bits, in the Frobenius
+norm, is at most twice that of the same steps in float32, and 2^-22.  Towards
+bfloat16 the operands' rounding to 11 bits is part of the definition: the same
+roundings in 64 bits, at the same places, say how far it takes the result, and the
+kernels', which differ where a sum in 32 bits falls on the other side of a
+rounding, at most half as much again.  Then y is rounded once."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import layer_reference as ref
+import training_reference as tref
+from paper_2004_09362_amd import ar
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+TYPES = [torch.bfloat16, torch.float16, torch.float32]
+IDS = ["bf16", "f16", "f32"]
+
+
+def seeded(*key):
+    return torch.Generator().manual_seed(hash(key) & 0x7FFFFFFF)
+
+
+def normal(g, *shape, dtype=torch.float32, std=1.0, pad=0):
+    t = torch.empty(*shape[:-1], shape[-1] + pad).normal_(0, std, generator=g).to(dtype).to(DEV)
+    return t[..., :shape[-1]]
+
+
+def distance(a, b):
+    return float((a.double().cpu() - b.double().cpu()).norm())
+
+
+def near(y, x, **kw):
+    """y of ar_orthogonalize(x, **kw) within what its type allows."""
+    scale = kw.pop("scale", 1.0)
+    residual = kw.pop("residual", None)
+    want = tref.orthogonal(x, **kw)
+    size = float(want.norm())
+    if y.dtype == torch.bfloat16:
+        off = 1.5 * distance(tref.orthogonal(x, rounded=True, **kw), want) + 2.0 ** -20 * size
+    else:
+        off = 2 * distance(tref.orthogonal(x, dtype=torch.float32, **kw), want) + 2.0 ** -22 * size
+    want = scale * want
+    if residual is not None:
+        want = residual.double().cpu() + want
+    # a rounding is off by u of its value at most (in float16 below its normal numbers by 2^-25)
+    off = abs(scale) * off + ref.U[y.dtype] * float(want.norm()) + (2.0 ** -25 * math.sqrt(y.numel()) if y.dtype == torch.float16 else 0)
+    far = distance(y, want)
+    assert far <= off, (tuple(x.shape), y.dtype, far / size, off / size)
+
+
+def hadamard(n):
+    """n x n, by Sylvester's doubling."""
+    h = torch.ones(1, 1)
+    while h.shape[0] < n:
+        h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+    return h
+
+
+# m n a power of four, so that the norm is a power of two
+EXACT = [(1, 4), (2, 8), (64, 64), (64, 256), (128, 512), (512, 128), (256, 256), (256, 1024), (1024, 64), (512, 2048), (1024, 1024),
+         (1024, 4096), (4096, 256), (2048, 2048)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("size", EXACT, ids=lambda s: "x".join(map(str, s)))
+def test_exact_steps(size, dtype):
+    """Rows of a Hadamard matrix, rows and columns shuffled: A is a multiple of the identity, every product and sum is a
+    number of few bits, and so the result is x times a number in every bit, which a wrong index anywhere breaks."""
+    M, N = size
+    m, n = min(size), max(size)
+    g = seeded(1, M, N)
+    h = hadamard(n)[torch.randperm(n, generator=g)[:m]][:, torch.randperm(n, generator=g)]
+    x = (h if M <= N else h.t().contiguous()).to(dtype).to(DEV)
+    # X has 22 bits, which end at 2^-21 of a factor from 1 up; with m = 2048 the fifth power of (1.5, -1, 0.5) gives 2^-23
+    fifth = (1.5, -1.0, 0.5) if m <= 1024 else (0.0, 0.0, 0.5)
+    for coefficients, steps in (((1.5, -0.5, 0.0), 1), (fifth, 1), ((0.5, 0.0, 2.0) if m <= 1024 else (0.0, 0.0, 2.0), 1), ((0.0, 2.0, 0.0), 1)):
+        print("[gpu] exact", size, dtype, coefficients, flush=True)
+        y = ar.ar_orthogonalize(x, steps=steps, coefficients=coefficients, eps=0.0, out_dtype=torch.float32)
+        s2 = n / (m * n)  # each singular value's square: x x^T = n I, over the norm's square
+        a, b, c = coefficients
+        factor = (a + b * s2 + c * s2 * s2) / math.sqrt(m * n)
+        assert torch.equal(y, x.float() * factor)
+        low = ar.ar_orthogonalize(x, steps=steps, coefficients=coefficients, eps=0.0, out_dtype=torch.bfloat16)
+        assert torch.equal(low, (x.float() * factor).bfloat16())
+
+
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_exact_batches(out):
+    """Stacks, whose matrices are dealt out together, of shuffled identities and Hadamard rows times different numbers."""
+    g = seeded(2, 0)
+    for B, m, n in ((3, 16, 64), (24, 256, 256), (40, 128, 128), (5, 512, 512), (2, 1024, 256)):
+        hs = []
+        for k in range(B):
+            base = hadamard(max(m, n))[torch.randperm(max(m, n), generator=g)[:min(m, n)]]
+            base = base[:, torch.randperm(max(m, n), generator=g)] * 2.0 ** (k % 7 - 3)
+            hs.append(base if m <= n else base.t())
+        x = torch.stack(hs).to(DEV)
+        y = ar.ar_orthogonalize(x, steps=1, coefficients=(1.5, -0.5, 0.0), eps=0.0, out_dtype=out)
+        s2 = 1 / min(m, n)
+        want = x.sign() * ((1.5 - 0.5 * s2) / math.sqrt(m * n))
+        assert torch.equal(y, want.to(out))
+
+
+SIZES = [(1, 1), (1, 7), (5, 3), (40, 1), (1, 3000), (64, 64), (77, 130), (128, 129), (300, 200), (257, 1000), (640, 640), (1000, 2047),
+         (3000, 70), (1500, 1500)]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_against_64_bits(size, dtype):
+    g = seeded(3, *size)
+    for out, pad, res in ((torch.bfloat16, 0, False), (torch.float32, 3, True), (torch.float16, 8, False)):
+        print("[gpu] orthogonalize", size, dtype, out, flush=True)
+        x = normal(g, *size, dtype=dtype, std=0.01, pad=pad)
+        r = normal(g, *size, dtype=out, std=0.02, pad=1) if res else None
+        kw = dict(residual=r, scale=-0.05) if res else {}
+        near(ar.ar_orthogonalize(x, out_dtype=out, **kw), x, **kw)
+
+
+@pytest.mark.parametrize("out", TYPES, ids=IDS)
+def test_rank_and_spectrum(out):
+    """Low rank, where rounding of X would fill the other directions; singular values over four orders; equal ones."""
+    g = seeded(4, 0)
+    q1, q2 = (torch.linalg.qr(torch.empty(300, 300, dtype=torch.float64).normal_(generator=g))[0] for _ in range(2))
+    for name, x in (("rank 1", normal(g, 200, 1) @ normal(g, 1, 300)), ("rank 8", normal(g, 200, 8) @ normal(g, 8, 300)),
+                    ("rank 64", normal(g, 300, 64) @ normal(g, 64, 200)),
+                    ("low rank and noise", normal(g, 200, 4) @ normal(g, 4, 300) * 3 + 0.05 * normal(g, 200, 300)),
+                    ("decaying", ((q1 * torch.logspace(0, -4, 300, dtype=torch.float64)) @ q2).float().contiguous().to(DEV)),
+                    ("orthogonal", q1.float().contiguous().to(DEV)), ("ones", torch.ones(200, 300, device=DEV)),
+                    ("diagonal", torch.diag(torch.linspace(0.01, 1, 200)).to(DEV))):
+        print("[gpu] spectrum", name, out, flush=True)
+        near(ar.ar_orthogonalize(x, out_dtype=out), x)
+
+
+def test_steps_and_coefficients():
+    g = seeded(5, 0)
+    x = normal(g, 150, 220)
+    for steps in (1, 2, 9, 64):
+        near(ar.ar_orthogonalize(x, steps=steps), x, steps=steps)
+    triples = [(2.0, -1.5, 0.5), (3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0)]
+    near(ar.ar_orthogonalize(x, steps=3, coefficients=triples), x, steps=3, coefficients=triples)
+    # to singular values of 1 by the cubic that keeps them: the result's rows are orthogonal
+    y = ar.ar_orthogonalize(x, steps=20, coefficients=(1.5, -0.5, 0.0))
+    assert float((y @ y.t() - torch.eye(150, device=DEV)).abs().max()) < 1e-5
+    near(ar.ar_orthogonalize(x, eps=3.0), x, eps=3.0)
+
+
+def test_sizes_of_values():
+    """The norm is taken in 64 bits: squares past 32 bits' range on either side, and below the smallest normal numbers."""
+    g = seeded(6, 0)
+    x = normal(g, 60, 90)
+    for s in (2.0 ** 120, 2.0 ** 60, 2.0 ** -60, 2.0 ** -120):
+        near(ar.ar_orthogonalize(x * s, eps=0.0), x, eps=0.0)
+    z = torch.zeros(60, 90, device=DEV)
+    r = normal(g, 60, 90)
+    assert torch.equal(ar.ar_orthogonalize(z), z)
+    assert torch.equal(ar.ar_orthogonalize(z, residual=r), r)
+    assert bool(ar.ar_orthogonalize(z, eps=0.0).isnan().all())
+
+
+def test_infinities_and_nan_stay_in_their_matrix():
+    g = seeded(7, 0)
+    x = normal(g, 5, 140, 200)
+    bad = x.clone()
+    bad[1, 3, 7], bad[3, 139, 199] = math.inf, math.nan
+    for out in (torch.float32, torch.bfloat16):
+        y, want = ar.ar_orthogonalize(bad, out_dtype=out), ar.ar_orthogonalize(x, out_dtype=out)
+        assert bool(y[[1, 3]].isnan().all()) and torch.equal(y[[0, 2, 4]], want[[0, 2, 4]])
+
+
+def test_in_place_strides_and_stacks():
+    g = seeded(8, 0)
+    x = normal(g, 4, 70, 90)
+    want = ar.ar_orthogonalize(x, scale=-0.1, residual=x)
+    w = x.clone()
+    assert ar.ar_orthogonalize(x, scale=-0.1, residual=w, out=w).data_ptr() == w.data_ptr()
+    assert torch.equal(w, want)
+    w = x.clone()
+    ar.ar_orthogonalize(w, scale=-0.1, residual=w, out=w)
+    assert torch.equal(w, want)
+    # views of one vector of weights, with other things between them; and between rows
+    flat = torch.full((4, 7000), 5.0, device=DEV)
+    view = flat[:, 11:11 + 6300].view(4, 70, 90)
+    view.copy_(x)
+    ar.ar_orthogonalize(x, scale=-0.1, residual=view, out=view)
+    assert torch.equal(view, want)
+    assert bool((flat[:, :11] == 5).all()) and bool((flat[:, 6311:] == 5).all())
+    wide = torch.full((4, 72, 101), 5.0, device=DEV)
+    ar.ar_orthogonalize(x, scale=-0.1, residual=x, out=wide[:, 1:71, 3:93])
+    assert torch.equal(wide[:, 1:71, 3:93], want)
+    wide[:, 1:71, 3:93] = 5
+    assert bool((wide == 5).all())
+    # one matrix for all, matrices whose rows alternate
+    y = ar.ar_orthogonalize(x[2].expand(3, 70, 90))
+    assert torch.equal(y[0], y[1]) and torch.equal(y[0], y[2])
+    near(y[0], x[2])
+    between = normal(g, 70, 4, 90).transpose(0, 1)
+    assert torch.equal(ar.ar_orthogonalize(between), ar.ar_orthogonalize(between.contiguous()))
+    # rows and columns of a wider matrix
+    big = normal(g, 300, 400)
+    assert torch.equal(ar.ar_orthogonalize(big[7:207, 33:334]), ar.ar_orthogonalize(big[7:207, 33:334].contiguous()))
+    # its transpose goes the same way
+    near(ar.ar_orthogonalize(big[7:207, 33:334].t().contiguous()), big[7:207, 33:334].t())
+
+
+def test_matrices_further_apart_than_32_bits():
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 10 GB")
+    g = seeded(9, 0)
+    x = normal(g, 2, 50, 60, dtype=torch.bfloat16)
+    big = torch.zeros((1 << 32) + 4096, dtype=torch.bfloat16, device=DEV)
+    far = big.as_strided((2, 50, 60), ((1 << 32) + 8, 64, 1))
+    far.copy_(x)
+    want = ar.ar_orthogonalize(x)
+    assert torch.equal(ar.ar_orthogonalize(far, out=far), want) and torch.equal(far, want)
+
+
+def test_empty_sizes():
+    for shape in ((0, 5), (5, 0), (0, 4, 4), (3, 0, 4), (3, 4, 0)):
+        x = torch.empty(*shape, device=DEV)
+        assert ar.ar_orthogonalize(x).shape == shape
+        assert ar.ar_orthogonalize(x, residual=x, out_dtype=torch.float32).shape == shape
+
+
+def test_results_do_not_depend_on_timing_or_stream():
+    g = seeded(10, 0)
+    for shape, out in (((500, 900), torch.bfloat16), ((256, 4000), torch.float32), ((6, 300, 300), torch.bfloat16)):
+        x = normal(g, *shape)
+        want = ar.ar_orthogonalize(x, out_dtype=out)
+        other = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        for stream in (None, other, other.cuda_stream):
+            got = [ar.ar_orthogonalize(x, out_dtype=out, stream=stream) for _ in range(3)]
+            torch.cuda.synchronize()
+            assert all(torch.equal(y, want) for y in got)
+
+
+def test_two_streams_at_once():
+    """Calls that overlap keep to their own workspaces."""
+    g = seeded(11, 0)
+    xs = [normal(g, 400, 700) for _ in range(2)]
+    want = [ar.ar_orthogonalize(x) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        got = [ar.ar_orthogonalize(x, stream=s) for x, s in zip(xs, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_graph_capture_and_replay():
+    """Two captured graphs, replayed in turn with other inputs and eager calls between."""
+    g = seeded(12, 0)
+    x = normal(g, 300, 1000)
+    s = normal(g, 3, 200, 150)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        ar.ar_orthogonalize(x, out_dtype=torch.bfloat16)
+        ar.ar_orthogonalize(s)
+    torch.cuda.synchronize()
+    first, second = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(first):
+        y = ar.ar_orthogonalize(x, out_dtype=torch.bfloat16)
+    with torch.cuda.graph(second):
+        z = ar.ar_orthogonalize(s)
+    for i in range(4):
+        x.copy_(normal(g, 300, 1000, std=1.0 + i))
+        s.copy_(normal(g, 3, 200, 150))
+        want = ar.ar_orthogonalize(x, out_dtype=torch.bfloat16), ar.ar_orthogonalize(s)
+        first.replay()
+        second.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(z, want[1])
+
+
+def test_c_call_with_raw_addresses():
+    g = seeded(13, 0)
+    x = normal(g, 2, 90, 60, dtype=torch.float16, pad=4)
+    want = ar.ar_orthogonalize(x, steps=3, scale=2.0, out_dtype=torch.float32)
+    y = torch.full((2, 90 * 61 + 5), 7.0, device=DEV)
+    mat = lambda t, ld: ctypes.byref(ar.Matrix(t.data_ptr(), ld, ar._FLOAT_CODES[t.dtype]))
+    need = ctypes.c_int64()
+    assert ar.lib.ar_orthogonalize_workspace(2, 90, 60, mat(y, 61), ctypes.byref(need)) == ar.AR_OK
+    ws = torch.full((need.value + 256,), 85, dtype=torch.uint8, device=DEV)
+    coefficients = (ctypes.c_double * 9)(*(3.4445, -4.7750, 2.0315) * 3)
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    assert ar.lib.ar_orthogonalize(2, 90, 60, mat(x, 64), 90 * 64, 3, coefficients, 1e-7, 2.0, None, 0, mat(y, 61), 90 * 61 + 5,
+                                   ctypes.c_void_p(ws.data_ptr()), need.value, stream) == ar.AR_OK
+    got = y[:, :90 * 61].view(2, 90, 61)
+    assert torch.equal(got[:, :, :60], want) and bool((got[:, :, 60:] == 7).all()) and bool((y[:, 90 * 61:] == 7).all())
+    assert bool((ws[need.value:] == 85).all())
+
+
+def test_refusals_of_device_tensors():
+    x = torch.ones(8, 12, device=DEV)
+    s = torch.ones(3, 8, 12, device=DEV)
+    for call, text in (
+            (lambda: ar.ar_orthogonalize(x[0]), "2 or 3 dimensions"), (lambda: ar.ar_orthogonalize(s[None]), "2 or 3 dimensions"),
+            (lambda: ar.ar_orthogonalize(x.t()), "consecutive"), (lambda: ar.ar_orthogonalize(x.cpu()), "not on a GPU"),
+            (lambda: ar.ar_orthogonalize(x.int()), "float32, float16"),
+            (lambda: ar.ar_orthogonalize(x, residual=s), "residual must have x's shape"),
+            (lambda: ar.ar_orthogonalize(s, residual=s[:2]), "residual must have x's shape"),
+            (lambda: ar.ar_orthogonalize(x, residual=x.half()), "residual must have y's type"),
+            (lambda: ar.ar_orthogonalize(x, out=x[:, :11]), "out is 8 x 11"),
+            (lambda: ar.ar_orthogonalize(s, out=x.expand(3, 8, 12)), "y's matrices overlap"),
+            (lambda: ar.ar_orthogonalize(s[0], out=s.view(-1)[5:101].view(8, 12)), "y overlaps x"),
+            (lambda: ar.ar_orthogonalize(s[:2], out=s[1:]), "y overlaps x"),
+            (lambda: ar.ar_orthogonalize(x, steps=0), "steps must be"), (lambda: ar.ar_orthogonalize(x, steps=65), "steps must be"),
+            (lambda: ar.ar_orthogonalize(x, coefficients=(4.0, 0.0, 0.0)), "past 2.5"),
+            (lambda: ar.ar_orthogonalize(x, coefficients=(math.nan, 0.0, 0.0)), "must be finite"),
+            (lambda: ar.ar_orthogonalize(x, eps=-1.0), "eps must be"), (lambda: ar.ar_orthogonalize(x, scale=math.inf), "scale must be"),
+            (lambda: ar.ar_orthogonalize(x.clone().requires_grad_(True)), "x requires a gradient")):
+        with pytest.raises(ar.ArError, match=text):
+            call()
+    with torch.no_grad():
+        ar.ar_orthogonalize(x.clone().requires_grad_(True))
+    version = x._version
+    ar.ar_orthogonalize(s[0], out=x)
+    assert x._version == version + 1

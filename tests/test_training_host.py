@@ -129,3 +129,99 @@ def test_binding_refusals_without_a_gpu():
     with pytest.raises(ar.ArError, match="not on a GPU"):
         with torch.no_grad():
             ar.ar_layer_norm_forward(torch.zeros(4, 8, requires_grad=True))
+
+
+CO = (ctypes.c_double * 15)(*(3.4445, -4.7750, 2.0315) * 5)
+
+
+def coefficients(*triples):
+    flat = [v for t in triples for v in t]
+    return (ctypes.c_double * len(flat))(*flat), len(triples)
+
+
+def ortho(batch=2, M=4, N=6, x=None, x_stride=24, steps=5, co=CO, eps=1e-7, scale=1.0, residual=None, residual_stride=24, y=None,
+          y_stride=24, ws=A + 0xA00000, ws_bytes=1 << 40):
+    return ar.lib.ar_orthogonalize(batch, M, N, x or mat(X, 6), x_stride, steps, co, eps, scale, residual, residual_stride,
+                                   y or mat(Y, 6), y_stride, ws, ws_bytes, None)
+
+
+def with_coefficients(*triples):
+    co, n = coefficients(*triples)
+    return dict(co=co, steps=n)
+
+
+@pytest.mark.parametrize("status,kw,text", [
+    (INVALID, dict(batch=-1), "batch must be"), (INVALID, dict(M=-1), "M must be"), (INVALID, dict(N=(1 << 30) + 1), "N must be"),
+    (INVALID, dict(x=mat(None, 6)), "x's data"), (INVALID, dict(x=mat(X, 5)), "x's ld"), (INVALID, dict(y=mat(Y + 1, 6)), "multiple"),
+    (UNSUPPORTED, dict(x=mat(X, 6, 0)), "float32, float16"), (UNSUPPORTED, dict(y=mat(Y, 6, 7)), "y must be"),
+    (UNSUPPORTED, dict(residual=mat(R, 6, F32)), "residual must have y's type"),
+    (INVALID, dict(x_stride=-1), "x's stride"), (INVALID, dict(y_stride=23), "y's matrices overlap"),
+    (INVALID, dict(residual=mat(R, 6), residual_stride=-5), "residual's stride"),
+    (INVALID, dict(steps=0), "steps must be"), (INVALID, dict(steps=65), "steps must be"), (INVALID, dict(co=None), "coefficients is NULL"),
+    (INVALID, dict(eps=-1.0), "eps must be"), (INVALID, dict(eps=math.nan), "eps must be"), (INVALID, dict(scale=math.nan), "scale must be"),
+    (INVALID, with_coefficients((math.inf, 0, 0)), "must be finite"), (INVALID, with_coefficients((2.6, 0, 0)), "past 2.5"),
+    (INVALID, with_coefficients((3.0, 0, 0)), "past 2.5"), (INVALID, with_coefficients((0, 5.0, 0)), "past 2.5"),
+    # 2.4 after the first step, past 2.5 after the second
+    (INVALID, with_coefficients((2.4, 0, 0), (1.1, 0, 0)), "past 2.5"),
+    # within 2.5, but Q reaches past 15 between
+    (INVALID, with_coefficients((17.0, -33.0, 16.5)), "past 2.5, or"),
+    (ALIAS, dict(y=mat(X, 6), y_stride=30), "y overlaps x"), (ALIAS, dict(y=mat(X + 2, 6)), "y overlaps x"),
+    (ALIAS, dict(y=mat(X, 6, F16)), "y overlaps x"), (ALIAS, dict(residual=mat(Y + 12, 6)), "y overlaps residual"),
+    (ALIAS, dict(residual=mat(Y, 6), residual_stride=0), "y overlaps residual"),
+    (INVALID, dict(ws=None), "workspace must hold"), (INVALID, dict(ws_bytes=1000), "workspace must hold"),
+    (INVALID, dict(ws=A + 0xA00004), "16-byte"),
+    (ALIAS, dict(ws=X + 16), "the workspace overlaps x"), (ALIAS, dict(ws=Y - 0x1000), "the workspace overlaps y"),
+    (ALIAS, dict(ws=R + 16, residual=mat(R, 6)), "the workspace overlaps residual"),
+    (UNSUPPORTED, dict(batch=65536), "batch must be"), (UNSUPPORTED, dict(M=32769, N=40000), "shorter side"),
+    (UNSUPPORTED, dict(N=(1 << 21) + 1), "shorter side"), (UNSUPPORTED, dict(batch=3, M=32768, N=1 << 18), "2\\^34"),
+])
+def test_orthogonalize_refusals(status, kw, text):
+    import re
+
+    assert ortho(**kw) == status
+    assert re.search(text, ar.ar_last_error_message()), ar.ar_last_error_message()
+
+
+def test_orthogonalize_workspace_and_nothing_to_do():
+    def need_of(batch, M, N, dtype):
+        need = ctypes.c_int64(-1)
+        st = ar.lib.ar_orthogonalize_workspace(batch, M, N, mat(None, N, dtype), ctypes.byref(need))
+        assert st == ar.AR_OK, ar.ar_last_error_message()
+        return need.value
+
+    for batch, M, N in ((0, 4, 4), (3, 0, 4), (3, 4, 0)):
+        assert need_of(batch, M, N, F32) == 0
+        assert ortho(batch=batch, M=M, N=N, x=mat(None, 6), y=mat(None, 6), ws=None, ws_bytes=0) == ar.AR_OK
+    assert need_of(1, 1, 1, F32) > 0 and need_of(1, 4096, 1024, BF16) == need_of(1, 1024, 4096, BF16)
+    # two buffers of X in two halves, A and Q, and little else: 10 bytes an element and 4 of the square
+    assert need_of(1, 4096, 16384, BF16) >= 8 * 4096 * 16384 + 4 * 4096 * 4096
+    assert ar.lib.ar_orthogonalize_workspace(1, 4, 4, mat(None, 4), None) == INVALID
+    assert ar.lib.ar_orthogonalize_workspace(1, 4, 4, None, ctypes.byref(ctypes.c_int64())) == INVALID
+    if torch.cuda.is_available():
+        pytest.skip("the calls below would be launched")
+    for kw in (dict(), dict(y=mat(X, 6)), dict(residual=mat(Y, 6)), dict(x_stride=0), dict(batch=1, x_stride=-7, y_stride=0),
+               dict(x=mat(X, 12), y=mat(X + 12, 12), x_stride=48, y_stride=48),
+               with_coefficients((2.0, -1.5, 0.5)), with_coefficients((8.28, -23.6, 17.3), (1.5, -0.24, 0.0)),
+               with_coefficients(*[(1.5, -0.5, 0.0)] * 64)):
+        assert ortho(**kw) == ar.AR_ERR_NO_DEVICE, (kw, ar.ar_last_error_message())
+
+
+def test_the_bound_of_singular_values_holds_for_the_usual_coefficients():
+    """Accepted step for step: the bound that the check carries along stays below 2.5 for 64 steps."""
+    co, n = coefficients(*[(3.4445, -4.7750, 2.0315)] * 64)
+    st = ortho(steps=n, co=co, ws=None)
+    assert st == INVALID and "workspace" in ar.ar_last_error_message()
+
+
+def test_orthogonalize_binding_refusals_without_a_gpu():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ar.ArError, match="not on a GPU"):
+        ar.ar_orthogonalize(x)
+    for kw, text in ((dict(coefficients=(1.0, 2.0)), "one such triple for each"), (dict(coefficients=[(1, 0, 0)] * 4), "each of 5 steps"),
+                     (dict(out_dtype=torch.float64), "float32, float16 or bfloat16")):
+        with pytest.raises(ar.ArError, match=text):
+            ar.ar_orthogonalize(x, **kw)
+    with pytest.raises(ar.ArError, match="x requires a gradient"):
+        ar.ar_orthogonalize(torch.zeros(4, 8, requires_grad=True))
+    with pytest.raises(ar.ArError, match="x must be a tensor"):
+        ar.ar_orthogonalize("x")

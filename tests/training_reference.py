@@ -58,3 +58,35 @@ def norm_grad(dy, x, stats, weight=None, residual=None):
     # over the rows in any order
     return {"dx": (dx, off), "dw": ((D * h).sum(0), (rows + 8) * E32 * (D * h).abs().sum(0)),
             "db": (D.sum(0), (rows + 8) * E32 * D.abs().sum(0))}
+
+
+def orthogonal(x, steps=5, coefficients=(3.4445, -4.7750, 2.0315), eps=1e-7, dtype=torch.float64, rounded=False):
+    """X after the steps, of one matrix or a stack, on the CPU in `dtype`.  rounded: with the operands of the products
+    rounded to 11 bits as ar_orthogonalize says that it does towards bfloat16 (X in 22 bits; of Q the diagonal in full)."""
+    many = x.double().cpu()
+    turned = many.shape[-2] > many.shape[-1]
+    many = (many.transpose(-2, -1) if turned else many).reshape(-1, *sorted(many.shape[-2:]))
+    triples = [coefficients] * steps if not isinstance(coefficients[0], (tuple, list)) else coefficients
+
+    def bits11(t, scale):
+        return (t * scale).half().to(dtype) / scale
+
+    def bits22(t, scale):
+        high = bits11(t, scale)
+        return high, bits11(t - high, scale)
+
+    got = []
+    for X in many:
+        X = (X / (X.norm() + eps)).to(dtype)
+        for a, b, c in triples:
+            if not rounded:
+                A = X @ X.t()
+                X = a * X + (b * A + c * (A @ A)) @ X
+                continue
+            high, low = bits22(X, 8192)
+            A = bits11(high @ high.t(), 8192)
+            Q = b * A + c * (A @ A)
+            d = torch.diag(Q)
+            X = a * (high + low) + d[:, None] * high + bits11(Q - torch.diag(d), 4096) @ high
+        got.append(X.t() if turned else X)
+    return torch.stack(got).view(x.shape)
