@@ -192,6 +192,15 @@ __device__ __forceinline__ void wait_all() {
   asm volatile("" ::: "memory");
 }
 
+// The same of this wave alone.
+template <int LOADS>
+__device__ __forceinline__ void wait_own() {
+  static_assert(LOADS < 64, "the counter's range");
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((LOADS & 15) | ((LOADS >> 4) << 14) | 0x70);  // vmcnt(LOADS) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
 // The workgroup's LDS writes are done; loads into registers may be on their way.
 __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
@@ -595,7 +604,9 @@ struct Straight {
 // b of t + D is loaded to where a of t lay, and then a of t + D + 1 to where b of t
 // lay; the waves' next meeting waits for tile t + 2 and before.  fa and fb are the
 // fragments of both slices, whose contents do not matter before and after.
-template <typename T, int MT, int NT, int D, typename OpA, typename OpB, typename FragA, typename FragB, typename Where>
+// ALONE: the operands' tiles are one wave's own, in LDS that no other touches,
+// and nobody meets.
+template <typename T, int MT, int NT, int D, bool ALONE = false, typename OpA, typename OpB, typename FragA, typename FragB, typename Where>
 __device__ __forceinline__ void multiply_ring(f32x4v (&acc)[MT][NT], const OpA& a, const OpB& b, const FragA& ra,
                                               const FragB& rb, i32x4v (&fa)[2][MT], i32x4v (&fb)[2][NT], char* lds, int wave,
                                               int32_t whole, const Where& where) {
@@ -632,7 +643,8 @@ __device__ __forceinline__ void multiply_ring(f32x4v (&acc)[MT][NT], const OpA& 
       if (x % 2 == 0) load_all(a, x / 2, uint32_t(x) * kPlace);
       else load_all(b, x / 2, uint32_t(x) * kPlace);
     }
-    wait_all<(2 * D - 1) * kLoadsA>();
+    if constexpr (ALONE) wait_own<(2 * D - 1) * kLoadsA>();
+    else wait_all<(2 * D - 1) * kLoadsA>();
 #pragma unroll
     for (int x = 0; x < kReads; ++x) read(0, at_a, at_b, x);
   }
@@ -642,9 +654,12 @@ __device__ __forceinline__ void multiply_ring(f32x4v (&acc)[MT][NT], const OpA& 
   // busy for 16 cycles.  Slice 1 is read within the first half of slice 0's
   // products; after kMeet of them the waves meet.  The last tiles run the
   // same stream: their loads take the last tile again, which nobody reads.
-  constexpr int kMeet = kProducts * 5 / 8, kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
-  constexpr int kGapB = kProducts >= 64 ? 5 : 2, kGapA = kProducts >= 64 ? 6 : 3, kMeetA = kMeet + kGapB * kLoadsB;
-  static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA <= 2 * kProducts, "everything within a tile");
+  // Alone, a wave has its whole tile read by then, and a load goes with each product.
+  constexpr int kMeet = ALONE ? kProducts / 2 : kProducts * 5 / 8;
+  constexpr int kReadGap = kProducts / 2 / kReads, kReadGap1 = kProducts * 3 / 4 / kReads;
+  constexpr int kGapB = ALONE ? 1 : kProducts >= 64 ? 5 : 2, kGapA = ALONE ? 1 : kProducts >= 64 ? 6 : 3;
+  constexpr int kMeetA = kMeet + kGapB * kLoadsB;
+  static_assert(kReadGap >= 1 && kMeetA + kGapA * kLoadsA + ALONE <= 2 * kProducts, "everything within a tile");
   const char* pb = settled(where.at(b, whole > D ? D : whole - 1));
   const char* pa = settled(where.at(a, whole > D + 1 ? D + 1 : whole - 1));
   for (int32_t t = 0; t < whole; ++t) {
@@ -655,12 +670,20 @@ __device__ __forceinline__ void multiply_ring(f32x4v (&acc)[MT][NT], const OpA& 
     unrolled([&](auto index) {
       constexpr int x = decltype(index)::value, y = x - kProducts, zb = x - kMeet, za = x - kMeetA;
       if constexpr (x < kProducts && x % kReadGap == 0 && x / kReadGap < kReads) read(1, at_a, at_b, x / kReadGap);
-      if constexpr (x == kMeet) wait_all<(2 * D - 3) * kLoadsA>();
+      if constexpr (x == kMeet && !ALONE) wait_all<(2 * D - 3) * kLoadsA>();
+      if constexpr (x == kMeet && ALONE) wait_own<(2 * D - 3) * kLoadsA>();
       if constexpr (y >= 0 && y % kReadGap1 == 0 && y / kReadGap1 < kReads) read(0, next_a, next_b, y / kReadGap1);
-      if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
-      if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(from_b, zb / kGapB);
-      if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
-      if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(from_a, za / kGapA);
+      if constexpr (!ALONE) {
+        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 0) b.aim(zb / kGapB, lds0 + at_a, wave);
+        if constexpr (zb >= 0 && za < 0 && zb % kGapB == 1) b.issue(from_b, zb / kGapB);
+        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 0) a.aim(za / kGapA, lds0 + at_b, wave);
+        if constexpr (za >= 0 && za / kGapA < kLoadsA && za % kGapA == 1) a.issue(from_a, za / kGapA);
+      } else {  // each load goes out before the next one's target is named
+        if constexpr (zb >= 1 && zb <= kLoadsB) b.issue(from_b, zb - 1);
+        if constexpr (za >= 1 && za <= kLoadsA) a.issue(from_a, za - 1);
+        if constexpr (zb >= 0 && zb < kLoadsB) b.aim(zb, lds0 + at_a, wave);
+        if constexpr (za >= 0 && za < kLoadsA) a.aim(za, lds0 + at_b, wave);
+      }
       product(x / kProducts, x % kProducts);
       __builtin_amdgcn_sched_barrier(0);
     }, std::make_integer_sequence<int, 2 * kProducts>{});

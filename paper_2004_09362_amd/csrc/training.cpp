@@ -60,40 +60,51 @@ constexpr int64_t kCus = 256;
 
 // How one of a step's products runs.
 struct OrthoPlanPart {
-  int64_t tiles = 0, steps = 0, share = 0, workgroups = 0;
-  bool deep = false;
+  int64_t tile = 0, tiles = 0, steps = 0, share = 0, workgroups = 0;
   double micros = 0.0;
-  int64_t parts(int64_t tile) const { return share % steps == 0 ? 0 : workgroups * 2 * tile * tile * 4; }
+  int64_t parts() const { return share % steps == 0 ? 0 : workgroups * 2 * tile * tile * 4; }
 };
 
-OrthoPlanPart plan_part(int64_t tiles, int64_t batch, int64_t steps, int32_t shape) {
+// The fastest way by a model of what the kernels measured.  rows, cols: of the
+// result in units of 64, of which tiles divide them; steps of a tile.
+OrthoPlanPart plan_part(int64_t rows, int64_t cols, bool symmetric, int64_t batch, int64_t steps) {
   OrthoPlanPart best;
-  const int64_t all = tiles * batch * steps, tile = ar::tile_rows(shape);
-  auto offer = [&](int64_t share, bool deep) {
-    OrthoPlanPart p;
-    p.tiles = tiles;
-    p.steps = steps;
-    p.share = share;
-    p.workgroups = ceil_div(all, share);
-    p.deep = deep;
-    const bool large = shape == ar::kTile256;
-    const int64_t places = large || deep ? kCus : 2 * kCus, rounds = ceil_div(p.workgroups, places);
-    const double step = large ? 1.42 : deep ? 0.4 : 1.18, fixed = large ? 10.0 : 5.0;
-    // a share that is no whole number of tiles starts and ends within some
-    const double pieces = share % steps == 0 ? double(share / steps) : double(share) / double(steps) + 1.0;
-    p.micros = double(rounds) * (double(share) * step + pieces * fixed);
-    if (share % steps != 0) p.micros += 4.0 + double(p.parts(tile)) * 1.5 / 5e6;
-    if (best.share == 0 || p.micros < best.micros) best = p;
-  };
-  for (const bool deep : {false, true}) {
-    if (deep && shape == ar::kTile256) continue;
-    offer(steps, deep);
-    const int64_t places = deep || shape == ar::kTile256 ? kCus : 2 * kCus;
-    if (tiles * batch <= 8 * kCus) {
-      for (const int64_t w : {places, places / 2, places / 4}) {
-        const int64_t share = ceil_div(all, w);
-        if (share >= 4) offer(share, deep);
+  for (const int64_t tile : {64, 128, 256}) {
+    const int64_t unit = tile / 64;
+    if (rows % unit != 0 || cols % unit != 0) continue;
+    const int64_t tm = rows / unit, tn = cols / unit, tiles = symmetric ? tm * (tm + 1) / 2 : tm * tn, all = tiles * batch * steps;
+    auto offer = [&](int64_t share) {
+      OrthoPlanPart p;
+      p.tile = tile;
+      p.tiles = tiles;
+      p.steps = steps;
+      p.share = share;
+      p.workgroups = ceil_div(all, share);
+      const bool split = share % steps != 0;
+      const double busy = double(std::min(p.workgroups, kCus)) / double(kCus);
+      const double pieces = split ? double(share) / double(steps) + 1.0 : double(share / steps);
+      if (tile == 64) {
+        const double rounds = double(ceil_div(p.workgroups, kCus));
+        p.micros = 1.5 + rounds * (3.0 + double(steps) * (0.11 + 0.10 * busy));
+      } else if (tile == 128) {
+        const double rounds = std::max(1.0, double(p.workgroups) / double(2 * kCus));
+        if (p.workgroups <= kCus) p.micros = 3.0 + pieces * (symmetric ? 1.7 : 3.0 + 3.0 * busy) + double(share) * (0.43 + 0.06 * busy);
+        else p.micros = 3.0 + rounds * (pieces * (symmetric ? 2.5 : 7.0) + double(share) * (symmetric ? 1.35 : 0.88));
+      } else {
+        const double rounds = double(ceil_div(p.workgroups, kCus));
+        // parts of one tile read other parts of the operands at a time than their neighbours: the memory bounds them
+        const double step = split ? 0.9 + 1.3 * busy : symmetric ? 0.75 + 0.4 * busy : 0.9 + 0.4 * busy;
+        p.micros = rounds * (2.0 + pieces * (symmetric ? 14.0 : 18.0) + double(share) * step);
       }
+      if (split) p.micros += 4.5 + double(p.workgroups + tiles * batch) * double(tile * tile) * 8.0 / 5e6;
+      if (best.share == 0 || p.micros < best.micros) best = p;
+    };
+    offer(steps);
+    if (tile == 64) continue;
+    if (tile == 256 && tiles * batch > kCus) offer(steps * ceil_div(tiles * batch, kCus));
+    if (tiles * batch <= kCus) {
+      for (const int64_t w : {kCus, kCus / 2, kCus / 4})
+        if (ceil_div(all, w) >= 4 && ceil_div(all, w) < steps) offer(ceil_div(all, w));
     }
   }
   return best;
@@ -101,7 +112,7 @@ OrthoPlanPart plan_part(int64_t tiles, int64_t batch, int64_t steps, int32_t sha
 
 struct OrthoPlan {
   ar::OrthoShape s{};
-  int32_t planes = 1, shape = ar::kTile128;
+  int32_t planes = 1;
   OrthoPlanPart part[3];
   int64_t sums = 0, x = 0, a = 0, diag = 0, parts = 0;  // bytes of each
   int64_t total() const { return sums + 2 * x + 2 * a + diag + parts; }
@@ -110,30 +121,31 @@ struct OrthoPlan {
 OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
   OrthoPlan best;
   double least = 0.0;
-  for (const int32_t shape : {ar::kTile128, ar::kTile256}) {
+  for (const int64_t whole : {64, 128, 256}) {  // the sides' multiple
     OrthoPlan p;
-    p.shape = shape;
     p.planes = y == AR_BFLOAT16 ? 1 : 2;
     p.s.rows = M;
     p.s.cols = N;
     p.s.batch = int32_t(batch);
     p.s.turned = M > N;
-    const int64_t tile = ar::tile_rows(shape), pairs = p.planes == 2 ? 3 : 1;
-    p.s.mp = round_up(std::min(M, N), tile);
-    p.s.np = round_up(std::max(M, N), tile);
-    const int64_t tm = p.s.mp / tile, tn = p.s.np / tile;
-    p.part[ar::kOrthoGram] = plan_part(tm * (tm + 1) / 2, batch, pairs * (p.s.np / 64), shape);
-    p.part[ar::kOrthoSquare] = plan_part(tm * (tm + 1) / 2, batch, pairs * (p.s.mp / 64), shape);
-    p.part[ar::kOrthoApply] = plan_part(tm * tn, batch, pairs * (p.s.mp / 64), shape);
+    const int64_t pairs = p.planes == 2 ? 3 : 1;
+    p.s.mp = round_up(std::min(M, N), whole);
+    p.s.np = round_up(std::max(M, N), whole);
+    const int64_t m = p.s.mp / 64, n = p.s.np / 64;
+    p.part[ar::kOrthoGram] = plan_part(m, m, true, batch, pairs * n);
+    p.part[ar::kOrthoSquare] = plan_part(m, m, true, batch, pairs * m);
+    p.part[ar::kOrthoApply] = plan_part(m, n, false, batch, pairs * m);
     const double micros = p.part[0].micros + p.part[1].micros + p.part[2].micros;
     if (least > 0.0 && micros >= least) continue;
     least = micros;
-    p.sums = round_up(batch * ar::kOrthoSumBlocks * 8, kWorkspaceAlign);
+    // four groups of 8 to a thread and more, and 8 workgroups to a compute unit
+    p.s.blocks = int32_t(std::max<int64_t>(1, std::min(8 * kCus / batch, ceil_div(M * ceil_div(N, 8), 1024))));
+    p.sums = round_up(batch * p.s.blocks * 8, kWorkspaceAlign);
     p.x = batch * 2 * p.s.mp * p.s.np * 2;
     p.a = batch * p.planes * p.s.mp * p.s.mp * 2;
     p.diag = round_up(batch * p.s.mp * 4, kWorkspaceAlign);
     p.parts = 0;
-    for (const OrthoPlanPart& q : p.part) p.parts = std::max(p.parts, q.parts(tile));
+    for (const OrthoPlanPart& q : p.part) p.parts = std::max(p.parts, q.parts());
     best = p;
   }
   return best;
@@ -416,8 +428,8 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
         g.M = int32_t(p.s.mp);
         g.N = int32_t(apply ? p.s.np : p.s.mp);
         g.K = int32_t(gram ? p.s.np : p.s.mp);
-        g.tiles_m = int32_t(p.s.mp / ar::tile_rows(p.shape));
-        g.tiles_n = g.N / ar::tile_rows(p.shape);
+        g.tiles_m = int32_t(p.s.mp / q.tile);
+        g.tiles_n = int32_t(g.N / q.tile);
         g.tiles = int32_t(q.tiles);
         g.batch = int32_t(batch);
         g.steps = int32_t(q.steps);
@@ -426,11 +438,18 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
         g.a = float(coefficients[3 * k]);
         g.b = float(coefficients[3 * k + 1]);
         g.c = float(coefficients[3 * k + 2]);
-        launched(ar::launch_ortho_product(g, kind, p.planes, p.shape, q.deep, stream), "Newton-Schulz product launch");
+        if (apply && k == steps - 1) {
+          g.y = oy;
+          g.residual = ores;
+          g.rows = M;
+          g.cols = N;
+          g.turned = p.s.turned;
+          g.scale = float(scale);
+        }
+        launched(ar::launch_ortho_product(g, kind, p.planes, int32_t(q.tile), stream), "Newton-Schulz product launch");
       }
       std::swap(X[0], X[1]);
     }
-    launched(ar::launch_ortho_store(p.s, X[0], float(scale), ores, oy, stream), "store kernel launch");
   });
 }
 

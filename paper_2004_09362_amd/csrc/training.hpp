@@ -73,23 +73,18 @@ struct OrthoOuter {
 };
 struct OrthoShape {
   int64_t rows, cols, mp, np;
-  int32_t batch, turned;
+  int32_t batch, turned, blocks;  // blocks: of a matrix' sum of squares
 };
 
 // sums[matrix][block] of the squares of x, in 64 bits.
-constexpr int32_t kOrthoSumBlocks = 128;
 int launch_ortho_norm(const OrthoShape& s, const OrthoOuter& x, double* sums, void* stream);
 // X = x / (|x| + eps), both planes.
 int launch_ortho_load(const OrthoShape& s, const OrthoOuter& x, const double* sums, double eps, void* planes, void* stream);
-// y = residual + scale X (residual.data NULL: none).
-int launch_ortho_store(const OrthoShape& s, const void* planes, float scale, const OrthoOuter& residual, const OrthoOuter& y,
-                       void* stream);
-
 // The three products of a step.
 enum OrthoKind : int32_t {
   kOrthoGram = 0,    // A = X X^T
   kOrthoSquare = 1,  // Q = b A + c A A without its diagonal, which goes to diag in 32 bits
-  kOrthoApply = 2    // X = a X + (Q + diag) X
+  kOrthoApply = 2    // X = a X + (Q + diag) X, or y of it
 };
 
 // One product of each of `batch` matrices: out[m][n] of sums over k of
@@ -112,9 +107,14 @@ struct OrthoProduct {
   int32_t tiles_m, tiles_n, tiles;                // of a matrix; symmetric results: those on and below the diagonal
   int32_t batch, steps, share, workgroups;        // steps of a tile
   float a, b, c;
+  // The last product of all: y = residual + scale X (residual.data NULL: none);
+  // rows and cols of y, which is turned where m is its columns.  y.data NULL: to out.
+  OrthoOuter residual, y;
+  int64_t rows, cols;
+  int32_t turned;
+  float scale;
 };
-// How a product runs: its tile, and how many tiles ahead it loads (deep: one
-// workgroup to a compute unit).
-int launch_ortho_product(const OrthoProduct& g, int32_t kind, int32_t planes, int32_t shape, bool deep, void* stream);
+// tile: 256, 128, or 64 (whole tiles only: share = steps).
+int launch_ortho_product(const OrthoProduct& g, int32_t kind, int32_t planes, int32_t tile, void* stream);
 
 }  // namespace ar

@@ -33,4 +33,4 @@ def test_wait_states_and_registers(listing):
         assert sum(op.startswith("v_mfma") for op, _ in loop) > 10, name
         assert not any(op.startswith("scratch_") for op, _ in body), name
         assert "Li8ELi8E" not in name or not any(op.startswith("v_accvgpr") for op, _ in loop), name
-    assert products >= 18  # three products, one and three pairs of planes, three forms
+    assert products == 20  # three products and four last ones, with one and with three pairs of planes, on two tiles
