@@ -5,13 +5,17 @@
 // db = sum of dy over the rows.  All in 32 bits, rounded once when stored.
 //
 // Bound by memory: each element is read once and written once.  A row lies in
-// the registers of a team of lanes (8 columns a lane and group, 16 bytes of
-// halves), from which its mean, then its variance about that mean, and then its
-// results are taken: no cancellation, no second reading.  A lane keeps its
-// columns from row to row, so w, b and the sums of the weight's gradient stay in
-// its registers too, and the next row is on its way while one is worked on.
-// Teams of up to 64 lanes sum by exchanges within a wave; larger ones through
-// LDS, with one meeting a sum.
+// the registers of a team of lanes (one or two groups of 8 columns a lane, 16
+// bytes of halves each), from which its mean, then its variance about that mean,
+// and then its results are taken: no cancellation, no second reading.  A lane keeps
+// its columns from row to row, so w, b and the sums of the weight's gradient stay
+// with it, and the next row is on its way while one is worked on.  Teams of up to a
+// wave sum by exchanges of registers; larger ones meet once a sum, in LDS.
+// Forward, 8192 x 8192 bf16 50.2 us (5.3 TB/s; a copy 46), 8192 x 4096 fp32 to bf16
+// 38.3 (35); gradient with a residual 110 (4.9 TB/s), 65536 x 1024 108.
+// Two rows on their way instead of one: 67.4 for 65.6 us then; a wave to each row of
+// 4096 (64 columns a lane) with w and b in LDS: 74.5 for 60.8, 43.6 for 42.3.
+#include <algorithm>
 #include <type_traits>
 
 #include "layer_device.hpp"
@@ -63,80 +67,141 @@ __device__ __forceinline__ void load_params(float (&v)[V], const void* p, int32_
   else of(static_cast<const bf16*>(p));
 }
 
+// v of a lane's partner: within 16 lanes the one at a distance of 1 or 2, or the
+// mirrored one of 8 or 16, whose sums so far are those of the other half.
+template <int CONTROL>
+__device__ __forceinline__ float partner(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CONTROL, 0xf, 0xf, true));
+}
+// The sum over 16 lanes, over 32, over the wave, without LDS: halves are exchanged
+// in the registers.
+__device__ __forceinline__ float sum16(float v) {
+  v += partner<0xb1>(v);
+  v += partner<0x4e>(v);
+  v += partner<0x141>(v);
+  return v + partner<0x140>(v);
+}
+__device__ __forceinline__ float add_halves32(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t x = r[0], y = r[1];
+  return __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+}
+__device__ __forceinline__ float add_halves64(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t x = r[0], y = r[1];
+  return __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+}
+
 // The sum over a team's lanes, for each of K values at once, in all of its lanes.
-template <int K>
+// SMALL: a team is a part of a wave, or one.  Forward, 8192 x 8192 bf16: with
+// exchanges through LDS and a loop over the waves' sums 65.6 us, so 61.0.
+template <int K, bool SMALL>
 struct TeamSum {
   float (*lds)[16][K];  // [2][16 waves]
-  int lanes, first, waves, turn;
+  int lanes, waves, turn, mine;
 
   __device__ __forceinline__ void init(float (*buffer)[16][K], int lanes_) {
     lds = buffer;
     lanes = lanes_;
     waves = lanes >> 6;
-    first = waves > 1 ? int(threadIdx.x >> 6) / waves * waves : 0;
     turn = 0;
+    if (SMALL) return;
+    // the wave of the team whose sum this lane takes, or none
+    const int of = int(threadIdx.x & 15);
+    mine = of < waves ? (int(threadIdx.x >> 6) & ~(waves - 1)) + of : -1;
   }
   __device__ __forceinline__ void operator()(float (&v)[K]) {
+    if constexpr (SMALL) {  // of 8 lanes or more
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      if (m < lanes) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], m);
+      for (int k = 0; k < K; ++k) {
+        v[k] += partner<0xb1>(v[k]);
+        v[k] += partner<0x4e>(v[k]);
+        v[k] += partner<0x141>(v[k]);
+        if (lanes > 8) v[k] += partner<0x140>(v[k]);
+        if (lanes > 16) v[k] = add_halves32(v[k]);
+        if (lanes > 32) v[k] = add_halves64(v[k]);
       }
+    } else {
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = add_halves64(add_halves32(sum16(v[k])));
+      if (waves == 1) return;
+      // the buffer was read two meetings ago
+      if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) lds[turn][threadIdx.x >> 6][k] = v[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] = sum16(mine >= 0 ? lds[turn][mine][k] : 0.0f);
+      turn ^= 1;
     }
-    if (waves <= 1) return;
-    // the buffer was read two meetings ago
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) lds[turn][threadIdx.x >> 6][k] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = 0.0f;
-    for (int w = 0; w < waves; ++w)
-#pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += lds[turn][first + w][k];
-    turn ^= 1;
   }
 };
 
-// The columns of a lane: group q is columns col[q] on, of which V - back[q] are there.
-template <int V, int R>
+// Element i of a row, whose start is the same for a wave: one register of a lane.
+template <typename T>
+__device__ __forceinline__ T* element(T* row, uint32_t i) {
+  using C = std::conditional_t<std::is_const_v<T>, const char, char>;
+  return reinterpret_cast<T*>(reinterpret_cast<C*>(row) + uint64_t(i * uint32_t(sizeof(T))));
+}
+
+// Which of the workgroup's teams a thread is in; teams of more than a wave are
+// known to be the same for it, and so are their rows' addresses.
+template <bool SMALL>
+__device__ __forceinline__ int team_of(int lanes) {
+  const int team = int(threadIdx.x) / lanes;
+  if constexpr (SMALL) return team;
+  else return __builtin_amdgcn_readfirstlane(team);
+}
+
+// The columns of a lane: group q is columns col(q) on, of which V - back(q) are
+// there; it is loaded from column from(q) on.  WHOLE: rows of whole groups, which
+// take fewer instructions (8192 x 8192 bf16 58.9 us for 60.8).
+template <int V, int R, bool WHOLE>
 struct Columns {
-  int32_t col[R], back[R];
-  bool there[R];
+  uint32_t first, apart;
+  int32_t missing[R];  // of group q, V where it is not there
   __device__ __forceinline__ void init(int t, int lanes, int64_t cols) {
+    first = uint32_t(t) * V;
+    apart = uint32_t(lanes) * V;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      col[q] = (q * lanes + t) * V;
-      const int64_t have = cols - col[q];
-      there[q] = have > 0;
-      back[q] = have > 0 && have < V ? V - int(have) : 0;
+      const int have = int(cols) - int(col(q));
+      missing[q] = have >= V ? 0 : have > 0 ? V - have : V;
     }
   }
+  __device__ __forceinline__ uint32_t col(int q) const { return first + uint32_t(q) * apart; }
+  __device__ __forceinline__ bool there(int q) const { return missing[q] < V; }
+  __device__ __forceinline__ int back(int q) const { return WHOLE ? 0 : missing[q]; }
+  __device__ __forceinline__ uint32_t from(int q) const { return col(q) - uint32_t(back(q)); }
+  __device__ __forceinline__ bool there(int q, int i) const { return WHOLE || i < V - missing[q]; }
 };
 
-// Teams of `lanes` lanes take rows in turn.
-template <typename X, typename Y, int V, int R>
+// Teams of `lanes` lanes take rows in turn, the next one on its way.
+template <typename X, typename Y, int V, int R, bool WHOLE>
 __global__ __launch_bounds__(kMaxThreads) void norm_kernel(NormCall c, int32_t lanes) {
   __shared__ float buffer[2][16][1];
-  const int t = int(threadIdx.x) & (lanes - 1), teams = int(blockDim.x) / lanes;
+  const int t = int(threadIdx.x) & (lanes - 1), team = team_of<R == 1>(lanes), teams = int(blockDim.x) / lanes;
   const int64_t step = int64_t(gridDim.x) * teams;
-  int64_t row = int64_t(blockIdx.x) * teams + int(threadIdx.x) / lanes;
-  Columns<V, R> at;
+  Columns<V, R, WHOLE> at;
   at.init(t, lanes, c.cols);
-  TeamSum<1> sum;
+  TeamSum<1, R == 1> sum;
   sum.init(buffer, lanes);
   const float inv = 1.0f / float(c.cols);
   float w[R][V], b[R][V];
   Raw<X, V> raw[R];
   auto fetch = [&](int64_t r) {
+    if (r >= c.rows) return;
     const X* const p = static_cast<const X*>(c.x) + r * c.ldx;
 #pragma unroll
     for (int q = 0; q < R; ++q)
-      if (at.there[q]) raw[q].load(p + at.col[q] - at.back[q]);
+      if (at.there(q)) raw[q].load(element(p, at.from(q)));
   };
-  if (row < c.rows) fetch(row);
+  // the workgroup's teams go round together, as they meet
+  int64_t first = int64_t(blockIdx.x) * teams;
+  fetch(first + team);
 #pragma unroll
   for (int q = 0; q < R; ++q) {
 #pragma unroll
@@ -144,36 +209,37 @@ __global__ __launch_bounds__(kMaxThreads) void norm_kernel(NormCall c, int32_t l
       w[q][i] = 1.0f;
       b[q][i] = 0.0f;
     }
-    if (at.there[q] && c.w) load_params<V>(w[q], c.w, c.we, at.col[q], at.back[q]);
-    if (at.there[q] && c.b) load_params<V>(b[q], c.b, c.be, at.col[q], at.back[q]);
+    if (at.there(q) && c.w) load_params<V>(w[q], c.w, c.we, at.col(q), at.back(q));
+    if (at.there(q) && c.b) load_params<V>(b[q], c.b, c.be, at.col(q), at.back(q));
   }
-  // the workgroup's teams go round together, as they meet
-  for (int64_t first = row - int(threadIdx.x) / lanes; first < c.rows; first += step, row += step) {
+  for (; first < c.rows; first += step) {
+    const int64_t row = first + team;
+    const bool mine = row < c.rows;
     float v[R][V], s[1] = {0.0f};
 #pragma unroll
     for (int q = 0; q < R; ++q) {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[q][i] = 0.0f;
-      if (at.there[q] && row < c.rows) raw[q].get(v[q], at.back[q]);
+      if (at.there(q) && mine) raw[q].get(v[q], at.back(q));
 #pragma unroll
       for (int i = 0; i < V; ++i) s[0] += v[q][i];
     }
-    if (row + step < c.rows) fetch(row + step);
+    fetch(row + step);
     sum(s);
     const float mean = s[0] / float(c.cols);
     s[0] = 0.0f;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (!at.there[q]) continue;
+      if (!at.there(q)) continue;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[q][i] -= mean;
-        s[0] += i < V - at.back[q] ? v[q][i] * v[q][i] : 0.0f;
+        s[0] = at.there(q, i) ? __builtin_fmaf(v[q][i], v[q][i], s[0]) : s[0];
       }
     }
     sum(s);
-    const float rstd = 1.0f / sqrtf(s[0] * inv + c.eps);
-    if (row >= c.rows) continue;
+    const float rstd = 1.0f / sqrtf(__builtin_fmaf(s[0], inv, c.eps));
+    if (!mine) continue;
     if (c.stats && t == 0) {
       c.stats[row * c.lds] = mean;
       c.stats[row * c.lds + 1] = rstd;
@@ -181,10 +247,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_kernel(NormCall c, int32_t l
     Y* const p = static_cast<Y*>(c.y) + row * c.ldy;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (!at.there[q]) continue;
+      if (!at.there(q)) continue;
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[q][i] = v[q][i] * rstd * w[q][i] + b[q][i];
-      store_row<V>(p + at.col[q], v[q], at.back[q]);
+      for (int i = 0; i < V; ++i) v[q][i] = __builtin_fmaf(v[q][i] * rstd, w[q][i], b[q][i]);
+      store_row<V>(element(p, at.col(q)), v[q], at.back(q));
     }
   }
 }
@@ -221,7 +287,7 @@ __device__ __forceinline__ void params_part(float (&v)[8], const void* p, int32_
 template <typename X, typename Y>
 __global__ __launch_bounds__(kMaxThreads) void norm_wide_kernel(NormCall c) {
   __shared__ float buffer[2][16][1];
-  TeamSum<1> sum;
+  TeamSum<1, false> sum;
   sum.init(buffer, int(blockDim.x));
   const float inv = 1.0f / float(c.cols);
   for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
@@ -261,44 +327,64 @@ __global__ __launch_bounds__(kMaxThreads) void norm_wide_kernel(NormCall c) {
 
 // The gradient: as norm_kernel, with the sums of dy h and dy kept by the lanes
 // over their rows, then over the workgroup's teams through LDS, in their order.
-template <typename X, typename D, int V, int R>
+// w lies in LDS, in 32 bits; the sums take its place at the end.
+template <typename X, typename D, int V, int R, bool WHOLE>
 __global__ __launch_bounds__(kMaxThreads) void norm_grad_kernel(NormGradCall c, int32_t lanes) {
   __shared__ float buffer[2][16][2];
-  __shared__ float joined[kMaxThreads * V];
-  const int t = int(threadIdx.x) & (lanes - 1), team = int(threadIdx.x) / lanes, teams = int(blockDim.x) / lanes;
+  extern __shared__ __attribute__((aligned(16))) float shared[];  // lanes R V of w; a team's lanes V for the sums
+  const int t = int(threadIdx.x) & (lanes - 1), team = team_of<R == 1>(lanes), teams = int(blockDim.x) / lanes;
   const int64_t step = int64_t(gridDim.x) * teams;
   int64_t row = int64_t(blockIdx.x) * teams + team;
-  Columns<V, R> at;
+  Columns<V, R, WHOLE> at;
   at.init(t, lanes, c.cols);
-  TeamSum<2> sum;
+  TeamSum<2, R == 1> sum;
   sum.init(buffer, lanes);
   const float inv = 1.0f / float(c.cols);
-  float w[R][V], dw[R][V], db[R][V], mean = 0.0f, rstd = 0.0f;
-  Raw<X, V> rx[R];
+  float dw[R][V], db[R][V], mean = 0.0f, rstd = 0.0f;
+  Raw<X, V> rx[R], rr[sizeof(X) == 2 && sizeof(D) == 2 ? R : 1];
   Raw<D, V> rd[R];
   auto fetch = [&](int64_t r) {
+    if (r >= c.rows) return;
     const X* const p = static_cast<const X*>(c.x) + r * c.ldx;
     const D* const d = static_cast<const D*>(c.dy) + r * c.lddy;
-#pragma unroll
-    for (int q = 0; q < R; ++q) {
-      if (at.there[q]) {
-        rx[q].load(p + at.col[q] - at.back[q]);
-        rd[q].load(d + at.col[q] - at.back[q]);
-      }
-    }
     mean = c.stats[r * c.lds];
     rstd = c.stats[r * c.lds + 1];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      if (at.there(q)) {
+        rx[q].load(element(p, at.from(q)));
+        rd[q].load(element(d, at.from(q)));
+      }
+    }
   };
-  if (row < c.rows) fetch(row);
+  // of 32 bits it would not fit the registers: each group when it is added
+  constexpr bool kAhead = sizeof(X) == 2 && sizeof(D) == 2;
+  auto residual = [&](int q, int64_t r) {
+    rr[kAhead ? q : 0].load(element(static_cast<const X*>(c.res) + r * c.ldr, at.from(q)));
+  };
+  auto fetch_residual = [&](int64_t r) {
+    if (!kAhead || !c.res || r >= c.rows) return;
+#pragma unroll
+    for (int q = 0; q < R; ++q)
+      if (at.there(q)) residual(q, r);
+  };
+  fetch(row);
+  fetch_residual(row);
 #pragma unroll
   for (int q = 0; q < R; ++q) {
+    float w[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      w[q][i] = 1.0f;
+      w[i] = 1.0f;
       dw[q][i] = db[q][i] = 0.0f;
     }
-    if (at.there[q] && c.w) load_params<V>(w[q], c.w, c.we, at.col[q], at.back[q]);
+    if (team == 0 && c.w && at.there(q)) load_params<V>(w, c.w, c.we, at.col(q), at.back(q));
+    if (team == 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) shared[at.col(q) + i] = w[i];
+    }
   }
+  __syncthreads();
   for (int64_t first = row - team; first < c.rows; first += step, row += step) {
     float h[R][V], g[R][V], s[2] = {0.0f, 0.0f};
     const bool mine = row < c.rows;
@@ -307,48 +393,56 @@ __global__ __launch_bounds__(kMaxThreads) void norm_grad_kernel(NormGradCall c, 
     for (int q = 0; q < R; ++q) {
 #pragma unroll
       for (int i = 0; i < V; ++i) h[q][i] = g[q][i] = 0.0f;
-      if (!mine || !at.there[q]) continue;
-      rx[q].get(h[q], at.back[q]);
-      rd[q].get(g[q], at.back[q]);  // 0 past the row's end, which keeps h out of the sums there
+      if (!mine || !at.there(q)) continue;
+      rx[q].get(h[q], at.back(q));
+      rd[q].get(g[q], at.back(q));
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        h[q][i] = i < V - at.back[q] ? (h[q][i] - mean) * scale : 0.0f;
-        dw[q][i] += g[q][i] * h[q][i];
+        h[q][i] = at.there(q, i) ? (h[q][i] - mean) * scale : 0.0f;
+        dw[q][i] = __builtin_fmaf(g[q][i], h[q][i], dw[q][i]);
         db[q][i] += g[q][i];
-        g[q][i] *= w[q][i];
+        g[q][i] *= shared[at.col(q) + i];
         s[0] += g[q][i];
-        s[1] += g[q][i] * h[q][i];
+        s[1] = __builtin_fmaf(g[q][i], h[q][i], s[1]);
       }
+      __builtin_amdgcn_sched_barrier(0);  // a group's temporaries at a time, here and below: 128 registers hold no more
     }
-    if (row + step < c.rows) fetch(row + step);
+    fetch(row + step);
     if (!c.dx) continue;  // the same for all
-    Raw<X, V> rr[R];
-    if (c.res && mine) {
-      const X* const p = static_cast<const X*>(c.res) + row * c.ldr;
-#pragma unroll
-      for (int q = 0; q < R; ++q)
-        if (at.there[q]) rr[q].load(p + at.col[q] - at.back[q]);
-    }
+    __builtin_amdgcn_sched_barrier(0);
     sum(s);
+    __builtin_amdgcn_sched_barrier(0);
     if (!mine) continue;
     const float g0 = s[0] * inv, g1 = s[1] * inv;
     X* const p = static_cast<X*>(c.dx) + row * c.lddx;
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (!at.there[q]) continue;
+      if (!at.there(q)) continue;
       float r[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) g[q][i] = scale * (g[q][i] - g0 - h[q][i] * g1);
+      for (int i = 0; i < V; ++i) g[q][i] = scale * __builtin_fmaf(h[q][i], -g1, g[q][i] - g0);
       if (c.res) {
-        rr[q].get(r, at.back[q]);
+        if (!kAhead) residual(q, row);
+        rr[kAhead ? q : 0].get(r, at.back(q));
 #pragma unroll
         for (int i = 0; i < V; ++i) g[q][i] += r[i];
       }
-      store_row<V>(p + at.col[q], g[q], at.back[q]);
+      store_row<V>(element(p, at.col(q)), g[q], at.back(q));
+      __builtin_amdgcn_sched_barrier(0);
     }
+    fetch_residual(row + step);
   }
   if (!c.parts) return;
   float* const parts = c.parts + int64_t(blockIdx.x) * 2 * c.cols;
+  if (teams == 1) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      if (!at.there(q)) continue;
+      store_row<V>(parts + at.col(q), dw[q], at.back(q));
+      store_row<V>(parts + c.cols + at.col(q), db[q], at.back(q));
+    }
+    return;
+  }
   const int width = lanes * V;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -356,11 +450,11 @@ __global__ __launch_bounds__(kMaxThreads) void norm_grad_kernel(NormGradCall c, 
     for (int q = 0; q < R; ++q) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < V; ++i) joined[team * width + t * V + i] = which ? db[q][i] : dw[q][i];
+      for (int i = 0; i < V; ++i) shared[team * width + t * V + i] = which ? db[q][i] : dw[q][i];
       __syncthreads();
       for (int n = int(threadIdx.x); n < width && q * width + n < c.cols; n += int(blockDim.x)) {
         float v = 0.0f;
-        for (int s = 0; s < teams; ++s) v += joined[s * width + n];
+        for (int s = 0; s < teams; ++s) v += shared[s * width + n];
         parts[which * c.cols + q * width + n] = v;
       }
     }
@@ -371,7 +465,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_grad_kernel(NormGradCall c, 
 template <typename X, typename D>
 __global__ __launch_bounds__(kMaxThreads) void norm_grad_wide_kernel(NormGradCall c) {
   __shared__ float buffer[2][16][2];
-  TeamSum<2> sum;
+  TeamSum<2, false> sum;
   sum.init(buffer, int(blockDim.x));
   const float inv = 1.0f / float(c.cols);
   for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
@@ -491,11 +585,17 @@ int launch_norm_of(const NormCall& c, hipStream_t st) {
     return int(hipGetLastError());
   }
   const int threads = k.lanes > 256 ? k.lanes : 256;
-  const int64_t teams = threads / k.lanes, need = (c.rows + teams - 1) / teams, most = kCus * (2048 / threads);
+  // as many workgroups as their registers let in at once: one more on some units
+  // runs its rows by itself at the end (8192 x 8192 bf16 58.8 us for 50.2)
+  const int waves = k.per == 1 ? 32 : sizeof(X) == 4 ? 20 : 24;
+  const int64_t teams = threads / k.lanes, need = (c.rows + teams - 1) / teams, most = kCus * std::max(1, waves * 64 / threads);
   const dim3 grid(uint32_t(need < most ? need : most));
-  if (k.V == 1) norm_kernel<X, Y, 1, 1><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
-  else if (k.per == 1) norm_kernel<X, Y, 8, 1><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
-  else norm_kernel<X, Y, 8, 2><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
+  const bool whole = c.cols % 8 == 0;
+  if (k.V == 1) norm_kernel<X, Y, 1, 1, true><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
+  else if (k.per == 1 && whole) norm_kernel<X, Y, 8, 1, true><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
+  else if (k.per == 1) norm_kernel<X, Y, 8, 1, false><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
+  else if (whole) norm_kernel<X, Y, 8, 2, true><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
+  else norm_kernel<X, Y, 8, 2, false><<<grid, dim3(threads), 0, st>>>(c, k.lanes);
   return int(hipGetLastError());
 }
 
@@ -532,10 +632,15 @@ int launch_norm_grad_of(const NormGradCall& c, hipStream_t st) {
     }
     return int(hipGetLastError());
   }
-  const dim3 grid(uint32_t(c.blocks)), block(uint32_t(grad_threads(k, c.rows)));
-  if (k.V == 1) norm_grad_kernel<X, D, 1, 1><<<grid, block, 0, st>>>(c, k.lanes);
-  else if (k.per == 1) norm_grad_kernel<X, D, 8, 1><<<grid, block, 0, st>>>(c, k.lanes);
-  else norm_grad_kernel<X, D, 8, 2><<<grid, block, 0, st>>>(c, k.lanes);
+  const int threads = grad_threads(k, c.rows);
+  const dim3 grid(uint32_t(c.blocks)), block{uint32_t(threads)};
+  const int lds = k.V * std::max(k.lanes * k.per, threads) * int(sizeof(float));
+  const bool whole = c.cols % 8 == 0;
+  if (k.V == 1) norm_grad_kernel<X, D, 1, 1, true><<<grid, block, lds, st>>>(c, k.lanes);
+  else if (k.per == 1 && whole) norm_grad_kernel<X, D, 8, 1, true><<<grid, block, lds, st>>>(c, k.lanes);
+  else if (k.per == 1) norm_grad_kernel<X, D, 8, 1, false><<<grid, block, lds, st>>>(c, k.lanes);
+  else if (whole) norm_grad_kernel<X, D, 8, 2, true><<<grid, block, lds, st>>>(c, k.lanes);
+  else norm_grad_kernel<X, D, 8, 2, false><<<grid, block, lds, st>>>(c, k.lanes);
   return int(hipGetLastError());
 }
 

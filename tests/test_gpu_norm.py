@@ -95,6 +95,25 @@ def test_many_rows(cols):
         ref.close(t, *want[name], name)
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=IDS)
+@pytest.mark.parametrize("cols", [513, 1000, 1024, 1025, 2047, 2056, 4095, 4097, 6000, 8192, 8199, 16383])
+def test_forward_of_many_rows(cols, dtype):
+    """Rows of one wave, of two and of four, from half of their columns on to all, more than the chip takes at once, on any
+    address; without w, without b, with both."""
+    rows = 2048 + 37 + 64 * (cols % 3)
+    g = seeded(14, cols)
+    for pad, shift, out, w, b in ((0, 0, dtype, True, True), (5, 3, torch.bfloat16, True, False), (8, 0, torch.float32, False, True)):
+        print("[gpu] norm of many rows", cols, dtype, pad, shift, flush=True)
+        x = matrix(g, rows, cols, dtype, 2.0, 0.7, pad, shift)
+        w = matrix(g, 1, cols, torch.float32, mean=1.0)[0] if w else None
+        b = matrix(g, 1, cols, torch.float16)[0] if b else None
+        y, stats = ar.ar_layer_norm_forward(x, w, b, out_dtype=out, stats=True)
+        want = tref.norm(x, w, b)
+        ref.close(y, *want["y"], "y")
+        ref.close(stats[:, 0], *want["mean"], "mean")
+        ref.close(stats[:, 1], *want["rstd"], "rstd")
+
+
 @pytest.mark.parametrize("cols", [77, 2000, 20000])
 def test_rows_far_from_zero_and_outlying_columns(cols):
     """The variance is about the mean: rows whose mean is 10^4 of their deviation, a first column 10^4 times the others, and
