@@ -684,8 +684,9 @@ def ar_orthogonalize(x, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
     ``coefficients`` is (a, b, c), or one such triple for each step.  y is
     ``out`` (which may be x or ``residual``: a weight updated in place) or a
     new tensor of ``out_dtype`` (default x's type; the residual has y's).
-    Towards bfloat16 the products take operands of 11 bits, towards the other
-    types of 22 in three products (see include/ar.h).  torch records no
+    Towards bfloat16 the products take operands of 11 bits (22 where a side is
+    at most 64), towards the other types of 22 in three products (see
+    include/ar.h).  torch records no
     gradient of the call: while it records, a tensor that requires one is
     refused."""
     steps = int(steps)

@@ -139,15 +139,16 @@ __global__ __launch_bounds__(kThreads) void ortho_load_kernel(OrthoShape s, Orth
 
 // ---- the products ----
 
-// The tiles of a pair of planes follow those of the pair before: low high, high
-// low, high high (the last are added to sums of their own size).
-template <int PLANES>
+// Where steps first, first + STRIDE, first + 2 STRIDE and so on of a tile lie.  The
+// steps of a pair of planes follow those of the pair before: low high, high low,
+// high high (the last are added to sums of their own size).
+template <int PLANES, int STRIDE>
 struct InPlanes {
-  int32_t first, each;
-  int64_t low_left, low_right;
+  int32_t first, each;           // each: the steps of a pair of planes
+  int64_t low_left, low_right;   // bytes from an operand's high plane to its low one
   template <typename Op>
   __device__ __forceinline__ const char* at(const Op& op, int32_t t) const {
-    int32_t u = first + t;
+    int32_t u = first + t * STRIDE;
     if constexpr (PLANES == 1) return op.base + u * op.step();
     const int32_t pair = u >= 2 * each ? 2 : u >= each ? 1 : 0;
     u -= pair * each;
@@ -157,7 +158,7 @@ struct InPlanes {
   }
   template <typename Op>
   __device__ __forceinline__ void move(const char*& p, const Op& op, int32_t t, int32_t whole) const {
-    if constexpr (PLANES == 1) p += t < whole ? op.step() : 0;
+    if constexpr (PLANES == 1) p += t < whole ? STRIDE * op.step() : 0;
     else if (t < whole) p = at(op, t);
   }
 };
@@ -354,7 +355,7 @@ __global__ __launch_bounds__(kThreads, MT * NT <= 16 ? 2 : 1) void ortho_product
     OpB b;
     a.init(static_cast<const f16*>(g.left) + int64_t(place.matrix) * g.batch_left, g.ld_left, m0, 0, g.M, g.K, tid);
     b.init(static_cast<const f16*>(g.right) + int64_t(place.matrix) * g.batch_right, g.ld_right, n0, 0, g.N, g.K, tid);
-    const InPlanes<PLANES> where{k0, g.K / OpA::kInner, g.plane_left * 2, g.plane_right * 2};
+    const InPlanes<PLANES, 1> where{k0, g.K / OpA::kInner, g.plane_left * 2, g.plane_right * 2};
     const Finish<KIND, PLANES, Y> finish(g, place);
     const int32_t m = m0 + wm * MT * 16 + (lane & 15), n = n0 + wn * NT * 16 + 8 * (lane >> 4);
     f32x4v acc[MT][NT];
@@ -444,8 +445,8 @@ __global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoProduct g) {
   finish(v, old, m, n);
 }
 
-// Tiles of 64 x 64, for products with few of them: the inner length is dealt out
-// over a workgroup's four waves, each with its own operands in LDS and the whole
+// Tiles of 64 x 64, for products with few of them: the steps are dealt out in turn
+// to a workgroup's four waves, each with its own operands in LDS and the whole
 // tile's sums in its registers, which meet in LDS in the order of the waves.
 constexpr int kSmallShare = ring_bytes(64);  // of LDS, for a wave
 // The LDS, all of a compute unit's, is asked for at the launch: a size that the
@@ -471,8 +472,8 @@ __global__ __launch_bounds__(kThreads, 2) void ortho_small_kernel(OrthoProduct g
   OpB b;
   a.init(static_cast<const f16*>(g.left) + int64_t(place.matrix) * g.batch_left, g.ld_left, m0, 0, g.M, g.K, lane);
   b.init(static_cast<const f16*>(g.right) + int64_t(place.matrix) * g.batch_right, g.ld_right, n0, 0, g.N, g.K, lane);
-  const int32_t each = (g.steps + 3) / 4, k0 = wave * each, left = g.steps - k0, whole = left < each ? left : each;
-  const InPlanes<PLANES> where{k0, g.K / OpA::kInner, g.plane_left * 2, g.plane_right * 2};
+  const int32_t whole = (g.steps - wave + 3) / 4;
+  const InPlanes<PLANES, 4> where{wave, g.K / OpA::kInner, g.plane_left * 2, g.plane_right * 2};
   // a wave finishes two of the tile's units
   const Finish<KIND, PLANES, Y> finish(g, place);
   typename Finish<KIND, PLANES, Y>::Old old[kUnits / 4];

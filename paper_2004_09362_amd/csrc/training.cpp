@@ -66,7 +66,16 @@ struct OrthoPlanPart {
 };
 
 // The fastest way by a model of what the kernels measured.  rows, cols: of the
-// result in units of 64, of which tiles divide them; steps of a tile.
+// result in units of 64, of which tiles divide them; steps of a tile.  Measured, us
+// a launch of many, tile: workgroups x steps of a symmetric product, and of X's:
+//   64:  1 x 1 3.4, 1 x 32 7.6, 1 x 128 17.9, 136 x 16 7.0, 136 x 64 15.2, 528 x 32 30;
+//        256 x 16 8.0, 416 x 39 21, 1024 x 16 28, 1536 x 8 33
+//   128: 10 x 8 7.5, 36 x 16 10.3, 36 x 64 31, 136 x 32 19.6, 240 x 8 9.3, 528 x 64 87;
+//        64 x 16 13.4, 256 x 16 17, 256 x 32 25, 384 x 8 18.5, 1024 x 64 122, 4096 x 64 519
+//   256: 36 x 32 42, 136 x 64 76, 136 x 256 264; 64 x 32 54, 256 x 64 101 to 116,
+//        1024 x 64 464, four tiles to a workgroup 413
+// Parts: 36 tiles of 128 x 64 steps over 128 workgroups 19.7, over 256 19.5; 136 tiles of
+// 256 x 256 steps over 256 workgroups 340 (264 whole).
 OrthoPlanPart plan_part(int64_t rows, int64_t cols, bool symmetric, int64_t batch, int64_t steps) {
   OrthoPlanPart best;
   for (const int64_t tile : {64, 128, 256}) {
@@ -123,7 +132,9 @@ OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
   double least = 0.0;
   for (const int64_t whole : {64, 128, 256}) {  // the sides' multiple
     OrthoPlan p;
-    p.planes = y == AR_BFLOAT16 ? 1 : 2;
+    // below 65 rows or columns the operands' roundings have few others to even out
+    // with (one element was off by 4e-3 of itself), and 22 bits cost 15 us of 69
+    p.planes = y == AR_BFLOAT16 && std::min(M, N) > 64 ? 1 : 2;
     p.s.rows = M;
     p.s.cols = N;
     p.s.batch = int32_t(batch);
