@@ -549,8 +549,8 @@ ar_status ar_dropout_backward(int64_t rows, int64_t cols, const ar_matrix* dy, c
  * [rows, 2] float32 receives (mean, rstd) of each row for the gradient (NULL:
  * not kept; cols = 0 has none: AR_ERR_INVALID_ARG).  Sums are in 32 bits, the
  * variance's about the mean.  y may be x where data, ld and type are the same.
- * eps: finite, at least 0 (AR_ERR_INVALID_ARG; a row of equal values with
- * eps = 0 gives NaN, as the formula says). */
+ * eps: finite in 32 bits, at least 0 (AR_ERR_INVALID_ARG; a row of equal values
+ * with eps = 0 gives NaN, as the formula says). */
 ar_status ar_layer_norm_forward(int64_t rows, int64_t cols, const ar_matrix* x, const ar_matrix* weight,
                                 const ar_matrix* bias, double eps, const ar_matrix* y, const ar_matrix* stats,
                                 hipStream_t stream);
@@ -596,7 +596,8 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,
  * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).
- * steps: 1 to 64.  AR_ERR_UNSUPPORTED: a shorter side above 32768, a longer one
+ * steps: 1 to 64; scale finite in 32 bits; eps finite, at least 0 (a matrix of
+ * zeros gives 0, and NaN with eps = 0).  AR_ERR_UNSUPPORTED: a shorter side above 32768, a longer one
  * above 2^21, 65536 matrices or more, more than 2^34 elements in all (sides
  * rounded up to 256).  Workspace (about 10 bytes an element, in whole tiles of 128
  * or 256) and errors as of ar_linear_forward. */

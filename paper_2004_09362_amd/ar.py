@@ -689,13 +689,17 @@ def ar_orthogonalize(x, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
     include/ar.h).  torch records no
     gradient of the call: while it records, a tensor that requires one is
     refused."""
-    steps = int(steps)
+    if type(steps) is not int or not 1 <= steps <= 64:
+        raise ArError(AR_ERR_INVALID_ARG, "steps", "steps must be in [1, 64], got %r" % (steps,))
+    wanted = "(a, b, c), or one such triple for each of %d steps" % steps
+    if not isinstance(coefficients, (tuple, list)):
+        raise ArError(AR_ERR_INVALID_ARG, "coefficients", wanted)
     flat = tuple(coefficients)
     if len(flat) == 3 and not any(isinstance(c, (tuple, list)) for c in flat):
-        flat = flat * max(steps, 0)
+        flat = flat * steps
     else:
         if len(flat) != steps or any(not isinstance(c, (tuple, list)) or len(c) != 3 for c in flat):
-            raise ArError(AR_ERR_INVALID_ARG, "coefficients", "(a, b, c), or one such triple for each of %d steps" % steps)
+            raise ArError(AR_ERR_INVALID_ARG, "coefficients", wanted)
         flat = tuple(v for c in flat for v in c)
     return _layer_call("ar_orthogonalize", _bind.orthogonalize,
                        (x, flat, eps, scale, residual, out, _float_code(out_dtype, "out_dtype")), stream)

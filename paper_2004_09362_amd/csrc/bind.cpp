@@ -504,6 +504,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 // A matrix or a stack of them (3 dimensions) as its first matrix; stride: elements from one to the next.
 ar_matrix stack(const at::Tensor& t, const char* name, at::IntArrayRef shape, const Place& at_, int64_t* stride) {
+  if (t.layout() != at::kStrided) throw Fault{std::string(name) + " must be a dense tensor"};
   if (t.dim() != int64_t(shape.size()) || (t.dim() == 3 && t.size(0) != shape[0]))
     throw Fault{std::string(name) + " must have x's shape"};
   *stride = 0;
@@ -524,7 +525,7 @@ PyObject* orthogonalize(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 9 || !g_orthogonalize) throw Fault{"orthogonalize takes 9 arguments"};
     const Place at_{number(args[7], "device"), number(args[8], "stream")};
     const at::Tensor& x = unrecorded(args[0], "x");
-    if (x.layout() != at::kStrided || x.dim() < 2 || x.dim() > 3) throw Fault{"x must be a matrix or a stack of matrices (2 or 3 dimensions)"};
+    if (x.dim() < 2 || x.dim() > 3) throw Fault{"x must be a matrix or a stack of matrices (2 or 3 dimensions)"};
     int64_t sx = 0, sr = 0, sy = 0;
     const ar_matrix mx = stack(x, "x", x.sizes(), at_, &sx);
     const bool one = x.dim() == 2;

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -239,7 +240,7 @@ ar_status ar_layer_norm_forward(int64_t rows, int64_t cols, const ar_matrix* x, 
     check_matrix("x", x, rows, cols);
     check_vector("weight", weight, cols);
     check_vector("bias", bias, cols);
-    if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(AR_ERR_INVALID_ARG, "eps must be finite and at least 0");
+    if (!(eps >= 0.0 && eps <= double(FLT_MAX))) refuse(AR_ERR_INVALID_ARG, "eps must be finite in 32 bits and at least 0");
     check_matrix("y", y, rows, cols);
     if (stats) check_stats(stats, rows);
     if (rows == 0 || cols == 0) {
@@ -384,7 +385,7 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
     double most = 1.0;
     for (int32_t k = 0; k < steps; ++k) check_coefficients(coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], most);
     if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(AR_ERR_INVALID_ARG, "eps must be finite and at least 0");
-    if (!std::isfinite(scale)) refuse(AR_ERR_INVALID_ARG, "scale must be finite");
+    if (!(std::fabs(scale) <= double(FLT_MAX))) refuse(AR_ERR_INVALID_ARG, "scale must be finite in 32 bits");
     if (batch == 0 || M == 0 || N == 0) return;
     const Extent ex = stack_extent(x, x_stride, batch, M, N), ey = stack_extent(y, y_stride, batch, M, N);
     const Extent er = stack_extent(residual, residual_stride, batch, M, N);

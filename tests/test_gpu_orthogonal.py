@@ -321,6 +321,7 @@ def test_refusals_of_device_tensors():
             (lambda: ar.ar_orthogonalize(x, steps=0), "steps must be"), (lambda: ar.ar_orthogonalize(x, steps=65), "steps must be"),
             (lambda: ar.ar_orthogonalize(x, coefficients=(4.0, 0.0, 0.0)), "past 2.5"),
             (lambda: ar.ar_orthogonalize(x, coefficients=(math.nan, 0.0, 0.0)), "must be finite"),
+            (lambda: ar.ar_orthogonalize(x, coefficients=("a", 0, 0)), "a coefficient must be a number"),
             (lambda: ar.ar_orthogonalize(x, eps=-1.0), "eps must be"), (lambda: ar.ar_orthogonalize(x, scale=math.inf), "scale must be"),
             (lambda: ar.ar_orthogonalize(x.clone().requires_grad_(True)), "x requires a gradient")):
         with pytest.raises(ar.ArError, match=text):

@@ -33,6 +33,7 @@ def norm(rows=4, cols=6, x=None, weight=None, bias=None, eps=1e-5, y=None, stats
     (INVALID, dict(bias=mat(None, 0)), "bias's data"), (UNSUPPORTED, dict(stats=mat(S, 2, F16)), "stats must be float32"),
     (INVALID, dict(stats=mat(S, 1, F32)), "stats's ld"), (INVALID, dict(eps=-1e-9), "eps must be"),
     (INVALID, dict(eps=math.inf), "eps must be"), (INVALID, dict(eps=math.nan), "eps must be"),
+    (INVALID, dict(eps=1e39), "eps must be"),
     (INVALID, dict(cols=0, stats=mat(S, 2, F32)), "no statistics"),
     (ALIAS, dict(y=mat(X + 2, 6)), "y overlaps x"), (ALIAS, dict(y=mat(X, 6, F16), x=mat(X, 6)), "y overlaps x"),
     (ALIAS, dict(y=mat(X, 8)), "y overlaps x"), (ALIAS, dict(weight=mat(Y, 0)), "y overlaps weight"),
@@ -159,6 +160,7 @@ def with_coefficients(*triples):
     (INVALID, dict(residual=mat(R, 6), residual_stride=-5), "residual's stride"),
     (INVALID, dict(steps=0), "steps must be"), (INVALID, dict(steps=65), "steps must be"), (INVALID, dict(co=None), "coefficients is NULL"),
     (INVALID, dict(eps=-1.0), "eps must be"), (INVALID, dict(eps=math.nan), "eps must be"), (INVALID, dict(scale=math.nan), "scale must be"),
+    (INVALID, dict(scale=1e39), "scale must be"), (INVALID, dict(scale=-math.inf), "scale must be"),
     (INVALID, with_coefficients((math.inf, 0, 0)), "must be finite"), (INVALID, with_coefficients((2.6, 0, 0)), "past 2.5"),
     (INVALID, with_coefficients((3.0, 0, 0)), "past 2.5"), (INVALID, with_coefficients((0, 5.0, 0)), "past 2.5"),
     # 2.4 after the first step, past 2.5 after the second
@@ -218,6 +220,8 @@ def test_orthogonalize_binding_refusals_without_a_gpu():
     with pytest.raises(ar.ArError, match="not on a GPU"):
         ar.ar_orthogonalize(x)
     for kw, text in ((dict(coefficients=(1.0, 2.0)), "one such triple for each"), (dict(coefficients=[(1, 0, 0)] * 4), "each of 5 steps"),
+                     (dict(coefficients=None), "one such triple for each"),
+                     (dict(steps=2.0), "steps must be"), (dict(steps=10 ** 12), "steps must be"), (dict(steps=0), "steps must be"),
                      (dict(out_dtype=torch.float64), "float32, float16 or bfloat16")):
         with pytest.raises(ar.ArError, match=text):
             ar.ar_orthogonalize(x, **kw)
@@ -225,3 +229,5 @@ def test_orthogonalize_binding_refusals_without_a_gpu():
         ar.ar_orthogonalize(torch.zeros(4, 8, requires_grad=True))
     with pytest.raises(ar.ArError, match="x must be a tensor"):
         ar.ar_orthogonalize("x")
+    with pytest.raises(ar.ArError, match="dense"):
+        ar.ar_orthogonalize(x.to_sparse())
