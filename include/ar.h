@@ -586,21 +586,23 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * through a s + b s^3 + c s^5, with (3.4445, -4.7750, 2.0315) five times to about
  * 0.7 to 1.2 from 0.004 up.
  *
- * X is held in 22 bits; products are summed in 32.  Towards a y of bfloat16 their
- * operands are rounded to 11 bits, which leaves X off by up to 2e-3 of its norm
- * before its rounding, whatever its rank; towards float32 and float16, and of
- * matrices with a side of at most 64, they are taken in 22 bits, in three products.  Coefficients that can take a singular
- * value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1, steps
- * after one another) are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN
- * gives NaN throughout; others of the batch do not see it.
+ * X is held in 22 bits, to 2^-38 at least; products are summed in 32.  Towards a y
+ * of bfloat16 their operands are rounded to 11 bits, which leaves X off by up to
+ * 2e-3 of its norm before its rounding, whatever its rank; towards float32 and
+ * float16, and of matrices with a side of at most 64, they are taken in 22 bits, in
+ * three products.  Coefficients that can take a singular value past 2.5 or
+ * |b s^2 + c s^4| past 15 (from singular values up to 1, steps after one another)
+ * are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN gives NaN throughout;
+ * others of the batch do not see it.
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,
  * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).
  * steps: 1 to 64; scale finite in 32 bits; eps finite, at least 0 (a matrix of
- * zeros gives 0, and NaN with eps = 0).  AR_ERR_UNSUPPORTED: a shorter side above 32768, a longer one
- * above 2^21, 65536 matrices or more, more than 2^34 elements in all (sides
- * rounded up to 256).  Workspace (about 10 bytes an element, in whole tiles of 128
- * or 256) and errors as of ar_linear_forward. */
+ * zeros gives 0, and NaN with eps = 0).  AR_ERR_UNSUPPORTED: a shorter side above
+ * 32768, a longer one above 2^21, 65536 matrices or more, more than 2^34 elements
+ * in all (sides rounded up to 256).  Workspace (8 bytes an element and 4 or 8 one of
+ * a square of the shorter side, in whole tiles of 64, 128 or 256, and parts of
+ * products) and errors as of ar_linear_forward. */
 ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix* x, int64_t x_stride, int32_t steps,
                            const double* coefficients, double eps, double scale, const ar_matrix* residual,
                            int64_t residual_stride, const ar_matrix* y, int64_t y_stride, void* workspace,
