@@ -590,9 +590,9 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * of bfloat16 their operands are rounded to 11 bits, which leaves X off by up to
  * 2e-3 of its norm before its rounding, whatever its rank; towards float32 and
  * float16, and of matrices with a side of at most 64, they are taken in 22 bits, in
- * three products.  Coefficients that can take a singular value past 2.5 or
- * |b s^2 + c s^4| past 15 (from singular values up to 1, steps after one another)
- * are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN gives NaN throughout;
+ * three products.  Coefficients that are not finite in 32 bits, or can take a
+ * singular value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1,
+ * steps after one another, with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN gives NaN throughout;
  * others of the batch do not see it.
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,

@@ -201,30 +201,39 @@ Extent stack_extent(const ar_matrix* m, int64_t stride, int64_t batch, int64_t M
 }
 
 // The coefficients of a step keep singular values that are at most `most` within
-// the range that the halves hold; `most` becomes the bound after the step.
-void check_coefficients(double a, double b, double c, double& most) {
-  if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) refuse(AR_ERR_INVALID_ARG, "the coefficients must be finite");
+// the range that the halves hold; `most` becomes the bound after the step: the
+// polynomial's, and what the roundings of X, A and Q to `rounding` of their size
+// add where they all fall the same way, so that steps which magnify it are seen.
+void check_coefficients(const double* step, double rounding, double& most) {
+  // as the kernels take them
+  const double a = float(step[0]), b = float(step[1]), c = float(step[2]);
+  if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) refuse(AR_ERR_INVALID_ARG, "the coefficients must be finite in 32 bits");
   const double end = most * most;
-  double value = 0.0, q = 0.0;
+  double value = 0.0, q = 0.0, slope = 0.0;
   auto look = [&](double s) {  // s: a square
     if (!(s >= 0.0 && s <= end)) return;
     value = std::max(value, std::sqrt(s) * std::fabs(a + s * (b + s * c)));
     q = std::max(q, std::fabs(s * (b + s * c)));
+    slope = std::max(slope, std::fabs(s * (b + 2.0 * s * c)));
   };
   look(end);
   if (c != 0.0) {
-    const double root = 9.0 * b * b - 20.0 * a * c;
-    if (root >= 0.0) {  // the ends of a + 3 b s + 5 c s^2
-      look((-3.0 * b + std::sqrt(root)) / (10.0 * c));
-      look((-3.0 * b - std::sqrt(root)) / (10.0 * c));
-    }
     look(-b / (2.0 * c));
-  } else if (b != 0.0) {
-    look(-a / (3.0 * b));
+    look(-b / (4.0 * c));
+  }
+  // The ends of a + 3 b s + 5 c s^2, of which neither is a difference of numbers
+  // of one size: for c next to 0 the second one is still -a / (3 b).
+  const double root = 9.0 * b * b - 20.0 * a * c;
+  if (root >= 0.0) {
+    const double r = -0.5 * (3.0 * b + std::copysign(std::sqrt(root), b));
+    if (c != 0.0) look(r / (5.0 * c));
+    if (r != 0.0) look(a / r);
   }
   if (!(value <= 2.5) || !(q <= 15.0))
     refuse(AR_ERR_INVALID_ARG, "the coefficients take a singular value past 2.5, or |b s + c s^2| of its square s past 15");
-  most = value;
+  // X's rounding enters A twice, A's once, each with b s + 2 c s^2; Q's, and X's in
+  // the product with Q, with b s + c s^2; the halves end at 2^-39 of an element
+  most = value + rounding * (value + (3.0 * slope + 2.0 * q) * most) + 0x1p-22;
 }
 
 }  // namespace
@@ -383,7 +392,7 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
     if (steps < 1 || steps > kMaxSteps) refuse(AR_ERR_INVALID_ARG, "steps must be in [1, 64]");
     if (!coefficients) refuse(AR_ERR_INVALID_ARG, "coefficients is NULL");
     double most = 1.0;
-    for (int32_t k = 0; k < steps; ++k) check_coefficients(coefficients[3 * k], coefficients[3 * k + 1], coefficients[3 * k + 2], most);
+    for (int32_t k = 0; k < steps; ++k) check_coefficients(coefficients + 3 * k, 0x1p-21, most);
     if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(AR_ERR_INVALID_ARG, "eps must be finite and at least 0");
     if (!(std::fabs(scale) <= double(FLT_MAX))) refuse(AR_ERR_INVALID_ARG, "scale must be finite in 32 bits");
     if (batch == 0 || M == 0 || N == 0) return;
