@@ -589,8 +589,9 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * X is held in 22 bits, to 2^-38 at least; products are summed in 32.  Towards a y
  * of bfloat16 their operands are rounded to 11 bits, which leaves X off by up to
  * 2e-3 of its norm before its rounding, whatever its rank; towards float32 and
- * float16, and of matrices with a side of at most 64, they are taken in 22 bits, in
- * three products.  Coefficients that are not finite in 32 bits, or can take a
+ * float16, of matrices with a side of at most 64, and where the steps could magnify
+ * the rounding out of the range below, they are taken in 22 bits, in three
+ * products.  Coefficients that are not finite in 32 bits, or can take a
  * singular value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1,
  * steps after one another, with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN gives NaN throughout;
  * others of the batch do not see it.
@@ -600,7 +601,7 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * steps: 1 to 64; scale finite in 32 bits; eps finite, at least 0 (a matrix of
  * zeros gives 0, and NaN with eps = 0).  AR_ERR_UNSUPPORTED: a shorter side above
  * 32768, a longer one above 2^21, 65536 matrices or more, more than 2^34 elements
- * in all (sides rounded up to 256).  Workspace (8 bytes an element and 4 or 8 one of
+ * in all (sides rounded up to 256).  Workspace (8 bytes an element and 8 one of
  * a square of the shorter side, in whole tiles of 64, 128 or 256, and parts of
  * products) and errors as of ar_linear_forward. */
 ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix* x, int64_t x_stride, int32_t steps,

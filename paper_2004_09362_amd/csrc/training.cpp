@@ -128,14 +128,17 @@ struct OrthoPlan {
   int64_t total() const { return sums + 2 * x + 2 * a + diag + parts; }
 };
 
-OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
+// Whether products towards y may take operands of 11 bits: below 65 rows or columns
+// their roundings have few others to even out with (one element was off by 4e-3 of
+// itself), and 22 bits cost 15 us of 69.
+bool may_round(int64_t M, int64_t N, ar_dtype y) { return y == AR_BFLOAT16 && std::min(M, N) > 64; }
+
+OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, int32_t planes) {
   OrthoPlan best;
   double least = 0.0;
   for (const int64_t whole : {64, 128, 256}) {  // the sides' multiple
     OrthoPlan p;
-    // below 65 rows or columns the operands' roundings have few others to even out
-    // with (one element was off by 4e-3 of itself), and 22 bits cost 15 us of 69
-    p.planes = y == AR_BFLOAT16 && std::min(M, N) > 64 ? 1 : 2;
+    p.planes = planes;
     p.s.rows = M;
     p.s.cols = N;
     p.s.batch = int32_t(batch);
@@ -161,6 +164,12 @@ OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
     best = p;
   }
   return best;
+}
+
+// The workspace of a call, whose coefficients say which of the two it is.
+int64_t ortho_bytes(int64_t batch, int64_t M, int64_t N, ar_dtype y) {
+  const int64_t two = plan_ortho(batch, M, N, 2).total();
+  return may_round(M, N, y) ? std::max(two, plan_ortho(batch, M, N, 1).total()) : two;
 }
 
 void check_ortho_sizes(int64_t batch, int64_t M, int64_t N, const ar_matrix* y) {
@@ -200,14 +209,13 @@ Extent stack_extent(const ar_matrix* m, int64_t stride, int64_t batch, int64_t M
   return e;
 }
 
-// The coefficients of a step keep singular values that are at most `most` within
-// the range that the halves hold; `most` becomes the bound after the step: the
-// polynomial's, and what the roundings of X, A and Q to `rounding` of their size
+// Whether the coefficients of a step keep singular values that are at most `most`
+// within the range that the halves hold; `most` becomes the bound after the step:
+// the polynomial's, and what the roundings of X, A and Q to `rounding` of their size
 // add where they all fall the same way, so that steps which magnify it are seen.
-void check_coefficients(const double* step, double rounding, double& most) {
+bool within_range(const double* step, double rounding, double& most) {
   // as the kernels take them
   const double a = float(step[0]), b = float(step[1]), c = float(step[2]);
-  if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) refuse(AR_ERR_INVALID_ARG, "the coefficients must be finite in 32 bits");
   const double end = most * most;
   double value = 0.0, q = 0.0, slope = 0.0;
   auto look = [&](double s) {  // s: a square
@@ -229,11 +237,16 @@ void check_coefficients(const double* step, double rounding, double& most) {
     if (c != 0.0) look(r / (5.0 * c));
     if (r != 0.0) look(a / r);
   }
-  if (!(value <= 2.5) || !(q <= 15.0))
-    refuse(AR_ERR_INVALID_ARG, "the coefficients take a singular value past 2.5, or |b s + c s^2| of its square s past 15");
   // X's rounding enters A twice, A's once, each with b s + 2 c s^2; Q's, and X's in
   // the product with Q, with b s + c s^2; the halves end at 2^-39 of an element
   most = value + rounding * (value + (3.0 * slope + 2.0 * q) * most) + 0x1p-22;
+  return value <= 2.5 && q <= 15.0;
+}
+bool all_within_range(const double* coefficients, int32_t steps, double rounding) {
+  double most = 1.0;
+  for (int32_t k = 0; k < steps; ++k)
+    if (!within_range(coefficients + 3 * k, rounding, most)) return false;
+  return true;
 }
 
 }  // namespace
@@ -373,7 +386,7 @@ ar_status ar_orthogonalize_workspace(int64_t batch, int64_t M, int64_t N, const 
     if (!bytes) refuse(AR_ERR_INVALID_ARG, "bytes is NULL");
     *bytes = 0;
     check_ortho_sizes(batch, M, N, y);
-    if (batch > 0 && M > 0 && N > 0) *bytes = plan_ortho(batch, M, N, y->dtype).total();
+    if (batch > 0 && M > 0 && N > 0) *bytes = ortho_bytes(batch, M, N, y->dtype);
   });
 }
 
@@ -391,8 +404,10 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
     }
     if (steps < 1 || steps > kMaxSteps) refuse(AR_ERR_INVALID_ARG, "steps must be in [1, 64]");
     if (!coefficients) refuse(AR_ERR_INVALID_ARG, "coefficients is NULL");
-    double most = 1.0;
-    for (int32_t k = 0; k < steps; ++k) check_coefficients(coefficients + 3 * k, 0x1p-21, most);
+    for (int32_t i = 0; i < 3 * steps; ++i)
+      if (!std::isfinite(float(coefficients[i]))) refuse(AR_ERR_INVALID_ARG, "the coefficients must be finite in 32 bits");
+    if (!all_within_range(coefficients, steps, 0x1p-21))
+      refuse(AR_ERR_INVALID_ARG, "the coefficients take a singular value past 2.5, or |b s + c s^2| of its square s past 15");
     if (!(eps >= 0.0) || !std::isfinite(eps)) refuse(AR_ERR_INVALID_ARG, "eps must be finite and at least 0");
     if (!(std::fabs(scale) <= double(FLT_MAX))) refuse(AR_ERR_INVALID_ARG, "scale must be finite in 32 bits");
     if (batch == 0 || M == 0 || N == 0) return;
@@ -401,8 +416,10 @@ ar_status ar_orthogonalize(int64_t batch, int64_t M, int64_t N, const ar_matrix*
     auto same = [&](const ar_matrix* m, int64_t stride) { return same_place(m, y, M) && (batch == 1 || stride == y_stride); };
     if (!same(x, x_stride)) check_apart("y", ey, "x", ex);
     if (residual && !same(residual, residual_stride)) check_apart("y", ey, "residual", er);
-    const OrthoPlan p = plan_ortho(batch, M, N, y->dtype);
-    const Extent ews = check_workspace(workspace, workspace_bytes, p.total());
+    // Steps that magnify 11 bits' rounding out of the range take 22 (eight published
+    // steps that hold 1 at the edge gave infinities from equal entries).
+    const OrthoPlan p = plan_ortho(batch, M, N, may_round(M, N, y->dtype) && all_within_range(coefficients, steps, 0x1p-11) ? 1 : 2);
+    const Extent ews = check_workspace(workspace, workspace_bytes, ortho_bytes(batch, M, N, y->dtype));
     check_apart("the workspace", ews, "x", ex);
     check_apart("the workspace", ews, "y", ey);
     check_apart("the workspace", ews, "residual", er);
