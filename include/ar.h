@@ -587,14 +587,18 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * 0.7 to 1.2 from 0.004 up.
  *
  * X is held in 22 bits, to 2^-38 at least; products are summed in 32.  Towards a y
- * of bfloat16 their operands are rounded to 11 bits, which leaves X off by up to
- * 2e-3 of its norm before its rounding, whatever its rank; towards float32 and
- * float16, of matrices with a side of at most 64, and where the steps could magnify
- * the rounding out of the range below, they are taken in 22 bits, in three
- * products.  Coefficients that are not finite in 32 bits, or can take a
- * singular value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1,
- * steps after one another, with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with an infinity or NaN gives NaN throughout;
- * others of the batch do not see it.
+ * of bfloat16 their operands are rounded to 11 bits.  Five steps of the triple above
+ * then leave X off by 2e-4 to 2.5e-3 of its norm before its rounding where the
+ * entries differ, whatever the rank; by up to 4e-3 where few entries are not zero or
+ * the singular values are all equal; and by up to 2.6e-2 where the entries that are
+ * not zero are equal too (identities, blocks of ones), whose roundings all fall the
+ * same way.  Towards float32 and float16, of matrices with a side of at most 64, and
+ * where the steps could magnify the rounding out of the range below, operands have 22
+ * bits, in three products: X is as near as 32-bit arithmetic gives, of equal entries
+ * within 8e-5.  Coefficients that are not finite in 32 bits, or can take a singular
+ * value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1, steps after
+ * one another, with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with
+ * an infinity or NaN gives NaN throughout; others of the batch do not see it.
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,
  * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).

@@ -685,8 +685,10 @@ def ar_orthogonalize(x, *, steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315
     ``out`` (which may be x or ``residual``: a weight updated in place) or a
     new tensor of ``out_dtype`` (default x's type; the residual has y's).
     Towards bfloat16 the products take operands of 11 bits (22 where a side is
-    at most 64), towards the other types of 22 in three products (see
-    include/ar.h).  torch records no
+    at most 64, or the steps would magnify the rounding too far), towards the
+    other types of 22 in three products: include/ar.h says how far off the
+    former are, mostly less than bfloat16's own rounding, but more for
+    matrices of equal entries.  torch records no
     gradient of the call: while it records, a tensor that requires one is
     refused."""
     if type(steps) is not int or not 1 <= steps <= 64:

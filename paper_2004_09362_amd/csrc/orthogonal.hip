@@ -9,10 +9,13 @@
 // operands all the same: with E the rounding of X's high half, (Q + E_Q)(X + E)
 // is off by E_Q X, which lies in X's row space, and by Q E, which lies in its
 // column space, and neither grows with the gain.  So one product of high halves
-// serves results in bfloat16 (off by 3e-4 to 2e-3 of the result before its
-// rounding of 1.7e-3, of low and of full rank), and three products (high high, high
-// low, low high) the others, to about what 32-bit arithmetic gives.  The diagonal
-// of Q, a quarter of the roundings' effect, stays in 32 bits beside it.
+// serves results in bfloat16: off by 2e-4 to 2.5e-3 of the result before its
+// rounding of 1.7e-3, of low and of full rank, as long as the roundings even out.
+// They do not where entries are equal: a block of ones rounds all of X, A and Q the
+// same way, and each step's slope adds that up, to 2.6e-2 at worst (four blocks of
+// 318 x 544; sparse rows and equal singular values 4e-3).  Three products (high high,
+// high low, low high) serve the others, to about what 32-bit arithmetic gives.  The
+// diagonal of Q, a quarter of the roundings' effect, stays in 32 bits beside it.
 // Halves are stored times 2^13 (Q: 2^12), so that values far below a matrix' norm
 // keep their bits; the entry point admits only coefficients that keep |X| below
 // 2.5 and |Q| below 15.
