@@ -594,11 +594,11 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * not zero are equal too (identities, blocks of ones), whose roundings all fall the
  * same way.  Towards float32 and float16, of matrices with a side of at most 64, and
  * where the steps could magnify the rounding out of the range below, operands have 22
- * bits, in three products: X is as near as 32-bit arithmetic gives, of equal entries
- * within 8e-5.  Coefficients that are not finite in 32 bits, or can take a singular
- * value past 2.5 or |b s^2 + c s^4| past 15 (from singular values up to 1, steps after
- * one another, with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with
- * an infinity or NaN gives NaN throughout; others of the batch do not see it.
+ * bits, in three products: X is about as near as 32-bit arithmetic gives.
+ * Coefficients that are not finite in 32 bits, or can take a singular value past 2.5
+ * or |b s^2 + c s^4| past 15 (from singular values up to 1, steps after one another,
+ * with 22 bits' rounding at each) are AR_ERR_INVALID_ARG.  A matrix with an infinity
+ * or NaN gives NaN throughout; others of the batch do not see it.
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,
  * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).
