@@ -335,7 +335,7 @@ template <int KIND, int PLANES, typename Y, int MT, int NT>
 __global__ __launch_bounds__(kThreads, MT * NT <= 16 ? 2 : 1) void ortho_product_kernel(OrthoProduct g) {
   constexpr bool BK = KIND != kOrthoApply;
   constexpr int TM = 2 * MT * 16, TN = 2 * NT * 16, kPairs = NT / 2;
-  constexpr bool kPinned = MT * NT == 64;
+  constexpr bool kPinned = MT * NT == 64, kSplits = ortho_splits(KIND, PLANES, TM);
   __shared__ __attribute__((aligned(1024))) char lds[ring_bytes(TM)];
   using OpA = Side<Operand<f16, true, false, TM, kThreads>, false>;
   using OpB = Side<Operand<f16, BK, true, TN, kThreads>, true>;
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(kThreads, MT * NT <= 16 ? 2 : 1) void ortho_product
         __builtin_amdgcn_sched_barrier(0);
       }, std::make_integer_sequence<int, MT * kPairs>{});
     };
-    if (whole == g.steps) {
+    if (!kSplits || whole == g.steps) {
       // the values there of some units are on their way while others are finished
       constexpr int kUnits = MT * kPairs, kAhead = KIND == kOrthoGram ? 0 : 8;
       typename Finish<KIND, PLANES, Y>::Old old[kAhead + 1];
@@ -424,8 +424,9 @@ __global__ __launch_bounds__(kThreads, MT * NT <= 16 ? 2 : 1) void ortho_product
 
 // The tiles whose steps several workgroups took: one unit of a tile a workgroup,
 // the parts summed in the order of the inner length.
-template <int KIND, int PLANES, typename Y, int MT, int NT>
+template <int KIND, int PLANES, int MT, int NT>
 __global__ __launch_bounds__(kThreads) void ortho_join_kernel(OrthoProduct g) {
+  using Y = void;  // the last product of all is not split
   constexpr int TM = 2 * MT * 16, TN = 2 * NT * 16, kPairs = NT / 2, kUnits = MT * kPairs;
   const uint32_t tile = blockIdx.x / kUnits;
   const int u = int(blockIdx.x - tile * kUnits), i = u / kPairs, j = u % kPairs;
@@ -533,11 +534,16 @@ __global__ __launch_bounds__(kThreads, 2) void ortho_small_kernel(OrthoProduct g
 
 template <int KIND, int PLANES, typename Y, int MT, int NT>
 int launch_product_of(const OrthoProduct& g, hipStream_t st) {
+  constexpr bool kSplits = ortho_splits(KIND, PLANES, 32 * MT);
+  const bool split = g.share % g.steps != 0;
+  if (split && !kSplits) return int(hipErrorInvalidValue);
   ortho_product_kernel<KIND, PLANES, Y, MT, NT><<<dim3(uint32_t(g.workgroups)), dim3(kThreads), 0, st>>>(g);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || g.share % g.steps == 0) return int(e);
-  const uint32_t units = uint32_t(g.batch) * uint32_t(g.tiles) * uint32_t(MT * NT / 2);
-  ortho_join_kernel<KIND, PLANES, Y, MT, NT><<<dim3(units), dim3(kThreads), 0, st>>>(g);
+  if (e != hipSuccess || !split) return int(e);
+  if constexpr (kSplits) {
+    const uint32_t units = uint32_t(g.batch) * uint32_t(g.tiles) * uint32_t(MT * NT / 2);
+    ortho_join_kernel<KIND, PLANES, MT, NT><<<dim3(units), dim3(kThreads), 0, st>>>(g);
+  }
   return int(hipGetLastError());
 }
 
@@ -547,6 +553,7 @@ int launch_product_kind(const OrthoProduct& g, int32_t tile, hipStream_t st) {
     case 256: return launch_product_of<KIND, PLANES, Y, 8, 8>(g, st);
     case 128: return launch_product_of<KIND, PLANES, Y, 4, 4>(g, st);
     case 64:
+      if (g.share != g.steps) return int(hipErrorInvalidValue);
       ortho_small_kernel<KIND, PLANES, Y><<<dim3(uint32_t(g.workgroups)), dim3(kThreads), 4 * kSmallShare, st>>>(g);
       return int(hipGetLastError());
   }

@@ -77,7 +77,8 @@ struct OrthoPlanPart {
 //        1024 x 64 464, four tiles to a workgroup 413
 // Parts: 36 tiles of 128 x 64 steps over 128 workgroups 19.7, over 256 19.5; 136 tiles of
 // 256 x 256 steps over 256 workgroups 340 (264 whole).
-OrthoPlanPart plan_part(int64_t rows, int64_t cols, bool symmetric, int64_t batch, int64_t steps) {
+OrthoPlanPart plan_part(int64_t rows, int64_t cols, int32_t kind, int32_t planes, int64_t batch, int64_t steps) {
+  const bool symmetric = kind != ar::kOrthoApply;
   OrthoPlanPart best;
   for (const int64_t tile : {64, 128, 256}) {
     const int64_t unit = tile / 64;
@@ -112,7 +113,7 @@ OrthoPlanPart plan_part(int64_t rows, int64_t cols, bool symmetric, int64_t batc
     offer(steps);
     if (tile == 64) continue;
     if (tile == 256 && tiles * batch > kCus) offer(steps * ceil_div(tiles * batch, kCus));
-    if (tiles * batch <= kCus) {
+    if (ar::ortho_splits(kind, planes, int32_t(tile)) && tiles * batch <= kCus) {
       for (const int64_t w : {kCus, kCus / 2, kCus / 4})
         if (ceil_div(all, w) >= 4 && ceil_div(all, w) < steps) offer(ceil_div(all, w));
     }
@@ -147,9 +148,9 @@ OrthoPlan plan_ortho(int64_t batch, int64_t M, int64_t N, int32_t planes) {
     p.s.mp = round_up(std::min(M, N), whole);
     p.s.np = round_up(std::max(M, N), whole);
     const int64_t m = p.s.mp / 64, n = p.s.np / 64;
-    p.part[ar::kOrthoGram] = plan_part(m, m, true, batch, pairs * n);
-    p.part[ar::kOrthoSquare] = plan_part(m, m, true, batch, pairs * m);
-    p.part[ar::kOrthoApply] = plan_part(m, n, false, batch, pairs * m);
+    p.part[ar::kOrthoGram] = plan_part(m, m, ar::kOrthoGram, planes, batch, pairs * n);
+    p.part[ar::kOrthoSquare] = plan_part(m, m, ar::kOrthoSquare, planes, batch, pairs * m);
+    p.part[ar::kOrthoApply] = plan_part(m, n, ar::kOrthoApply, planes, batch, pairs * m);
     const double micros = p.part[0].micros + p.part[1].micros + p.part[2].micros;
     if (least > 0.0 && micros >= least) continue;
     least = micros;

@@ -87,12 +87,19 @@ enum OrthoKind : int32_t {
   kOrthoApply = 2    // X = a X + (Q + diag) X, or y of it
 };
 
+// Whether a product's tiles may be split: the first, which has the longest inner
+// length and the fewest tiles, and the second on tiles of 128 with three products
+// each.  Of the others plan_part's model finds none faster so, at any of 400 000 sizes.
+constexpr bool ortho_splits(int32_t kind, int32_t planes, int32_t tile) {
+  return tile != 64 && (kind == kOrthoGram || (kind == kOrthoSquare && planes == 2 && tile == 128));
+}
+
 // One product of each of `batch` matrices: out[m][n] of sums over k of
 // left(m, k) right(n, k), or of left(m, k) right(k, n) for kOrthoApply.  Tiles are
 // dealt out as steps (128 bytes of inner length of one tile and pair of planes):
 // workgroup w takes steps [w share, (w + 1) share) of all.  A tile that lies in
-// one share is finished there; of others the parts go to `parts` and are joined
-// by a second launch.
+// one share is finished there; of others (ortho_splits) the parts go to `parts` and
+// are joined by a second launch.
 struct OrthoProduct {
   const void* left;
   const void* right;
@@ -114,7 +121,7 @@ struct OrthoProduct {
   int32_t turned;
   float scale;
 };
-// tile: 256, 128, or 64 (whole tiles only: share = steps).
+// tile: 256, 128, or 64 (share = steps).
 int launch_ortho_product(const OrthoProduct& g, int32_t kind, int32_t planes, int32_t tile, void* stream);
 
 }  // namespace ar
