@@ -601,7 +601,8 @@ ar_status ar_layer_norm_backward_workspace(int64_t rows, int64_t cols, const ar_
  * or NaN gives NaN throughout; others of the batch do not see it.
  *
  * residual (NULL: none) has y's type; y may be residual or x where data, ld,
- * stride and type are the same; matrices of y do not overlap (AR_ERR_INVALID_ARG).
+ * stride and type are the same; matrices of y do not share an element, but may lie
+ * side by side or row by row in turn (AR_ERR_INVALID_ARG otherwise).
  * steps: 1 to 64; scale finite in 32 bits; eps finite, at least 0 (a matrix of
  * zeros gives 0, and NaN with eps = 0).  AR_ERR_UNSUPPORTED: a shorter side above
  * 32768, a longer one above 2^21, 65536 matrices or more, more than 2^34 elements

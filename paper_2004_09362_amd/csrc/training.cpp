@@ -187,6 +187,18 @@ void check_ortho_sizes(int64_t batch, int64_t M, int64_t N, const ar_matrix* y) 
     refuse(AR_ERR_UNSUPPORTED, "the matrices have more than 2^34 elements in whole tiles");
 }
 
+// Whether matrices of M > 1 rows share an element: two that are d apart do where d
+// strides are within N elements of fewer than M rows.
+bool matrices_overlap(int64_t ld, int64_t stride, int64_t batch, int64_t M, int64_t N) {
+  if (stride >= N && (batch - 1) * stride + N <= ld) return false;  // side by side
+  for (int64_t d = 1; d < batch; ++d) {
+    const int64_t row = d * stride / ld, past = d * stride % ld;
+    if (row >= M) return false;
+    if (past < N || (ld - past < N && row + 1 < M)) return true;
+  }
+  return false;
+}
+
 // `batch` matrices, `stride` elements from one to the next.
 void check_stack(const char* name, const ar_matrix* m, int64_t stride, int64_t batch, int64_t M, int64_t N, bool written) {
   check_matrix(name, m, batch == 0 ? 0 : M, N);
@@ -194,7 +206,8 @@ void check_stack(const char* name, const ar_matrix* m, int64_t stride, int64_t b
   const int64_t covers = (M > 1 ? (M - 1) * m->ld : 0) + N;
   if (stride < 0 || stride > (int64_t(1) << 44))
     refuse(AR_ERR_INVALID_ARG, std::string(name) + "'s stride must be in [0, 2^44]");
-  if (written && stride < covers) refuse(AR_ERR_INVALID_ARG, std::string(name) + "'s matrices overlap: the stride must be at least " + std::to_string(covers));
+  if (written && stride < covers && (M == 1 || matrices_overlap(m->ld, stride, batch, M, N)))
+    refuse(AR_ERR_INVALID_ARG, std::string(name) + "'s matrices overlap");
 }
 Extent stack_extent(const ar_matrix* m, int64_t stride, int64_t batch, int64_t M, int64_t N) {
   if (!m || batch == 0) return Extent();
@@ -202,6 +215,11 @@ Extent stack_extent(const ar_matrix* m, int64_t stride, int64_t batch, int64_t M
   if (batch == 1 || e.empty()) return e;
   if (M > 1 && stride == M * m->ld) {  // rows of one pitch throughout
     e.rows = batch * M;
+    return e;
+  }
+  if (stride >= N && (M == 1 || stride * batch == m->ld)) {  // the same, rows of the matrices in turn
+    e.rows = batch * M;
+    e.pitch = stride * size_of(m->dtype);
     return e;
   }
   const int64_t bytes = int64_t(e.end() - e.at) + (batch - 1) * stride * size_of(m->dtype);
