@@ -549,8 +549,9 @@ ar_status ar_dropout_backward(int64_t rows, int64_t cols, const ar_matrix* dy, c
  * [rows, 2] float32 receives (mean, rstd) of each row for the gradient (NULL:
  * not kept; cols = 0 has none: AR_ERR_INVALID_ARG).  Sums are in 32 bits, the
  * variance's about the mean.  y may be x where data, ld and type are the same.
- * eps: finite in 32 bits, at least 0 (AR_ERR_INVALID_ARG; a row of equal values
- * with eps = 0 gives NaN, as the formula says). */
+ * eps: finite in 32 bits, at least 0, and not so small that it is 0 there unless it
+ * is 0 (AR_ERR_INVALID_ARG; a row of equal values with eps = 0 gives NaN, as the
+ * formula says; a row whose squares pass 32 bits' range has rstd 0). */
 ar_status ar_layer_norm_forward(int64_t rows, int64_t cols, const ar_matrix* x, const ar_matrix* weight,
                                 const ar_matrix* bias, double eps, const ar_matrix* y, const ar_matrix* stats,
                                 hipStream_t stream);

@@ -281,7 +281,8 @@ ar_status ar_layer_norm_forward(int64_t rows, int64_t cols, const ar_matrix* x, 
     check_matrix("x", x, rows, cols);
     check_vector("weight", weight, cols);
     check_vector("bias", bias, cols);
-    if (!(eps >= 0.0 && eps <= double(FLT_MAX))) refuse(AR_ERR_INVALID_ARG, "eps must be finite in 32 bits and at least 0");
+    if (!(eps >= 0.0 && eps <= double(FLT_MAX)) || (eps > 0.0 && float(eps) == 0.0f))
+      refuse(AR_ERR_INVALID_ARG, "eps must be finite in 32 bits and at least 0, and 0 there only if it is 0");
     check_matrix("y", y, rows, cols);
     if (stats) check_stats(stats, rows);
     if (rows == 0 || cols == 0) {
